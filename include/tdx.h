@@ -243,6 +243,151 @@ int tdx_conv2d_bias_relu_ex(int64_t N, int64_t H, int64_t W, int64_t Cin, int64_
                             int relu, void* y, void* stream, const tdx_config* cfg);
 
 /*
+ * Operators of a state-space layer.  The projections of such a layer are tdx_gemm (or, with 4-bit weights, tdx_gemm_w4);
+ * between them stand a short causal convolution and a selective scan, each with its backward pass and its form for single
+ * tokens.  (The paper's language-model case studies name no such layer; these entry points follow the formulas below.)
+ *
+ * Each call takes a block of arguments that a program fills once and passes with every call.  Fields that a call does not
+ * use are ignored.  Conventions of all of them, beside those at the top of this file:
+ *  - Activations (x, dt, B, C, z, outputs, their gradients) are TDX_F32 or TDX_BF16, channels contiguous, one row per token,
+ *    rows `ld_*` elements apart, so that a slice of a projection is passed as it is.  Any alignment and any ld >= the row's
+ *    width is accepted; 16-byte aligned rows are fastest.  Parameters, their gradients and scan states are fp32.
+ *  - Sequences: seq_offsets = NULL is a dense batch of `batch` sequences of max_len rows each (rows = batch * max_len).
+ *    Otherwise sequence b has the rows seq_offsets[b] .. seq_offsets[b + 1] - 1 (device memory, batch + 1 values, ascending),
+ *    none longer than max_len; empty ones are allowed, and rows outside every sequence are neither read nor written.  A
+ *    sequence that leaves [0, rows) or exceeds max_len is skipped and reported by tdx_check_device_status (TDX_ERR_BOUNDS).
+ *  - States: the state of sequence b is in slot slots[b] (device memory; NULL: slot b) of a tensor of n_slots slots that are
+ *    state_stride elements apart (0: dense).  A negative slot means that the sequence has no state: nothing is read (zeros
+ *    are taken) or written.  A slot >= n_slots is treated like a negative one and reported as above.  No two sequences
+ *    of a call may share a slot.  state_in = NULL: zero states.  state_out = NULL: not written.  state_out may be state_in;
+ *    no other output may overlap an input.
+ *  - Sums and states are fp32, and every sum is taken in a fixed order: the same call gives the same bits.
+ *  - No call allocates device memory: scratch is the caller's `workspace` (256-byte aligned, of at least the size that the
+ *    *_workspace_size function reports for the same block of arguments), so calls on different streams need different ones.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT (element alignment; workspace), WORKSPACE, CUDA.
+ */
+
+/*
+ * Short causal depthwise convolution: with e = the width - 1 rows of the sequence's state, then the rows of x,
+ *
+ *   pre[t, d] = bias[d] + sum_{k < width} weight[d, k] * e[t + k, d],    y = pre * sigmoid(pre) if silu, else pre.
+ *
+ * The state after a sequence is the last width - 1 rows of e.  The rows in front of a sequence are never materialised.
+ */
+typedef struct {
+    int64_t batch, max_len, rows, channels;
+    int width;                    /* 1 .. 8                                                     */
+    int dtype;                    /* tdx_dtype                                                  */
+    int silu;                     /* 0 or 1                                                     */
+    const void* x; int64_t ld_x;          /* rows x channels                                    */
+    const float* weight;                  /* channels x width, dense                            */
+    const float* bias;                    /* channels, or NULL                                  */
+    void* y; int64_t ld_y;                /* rows x channels                                    */
+    const int32_t* seq_offsets;
+    const void* state_in;                 /* n_slots x (width - 1) x channels, oldest row first */
+    void* state_out;
+    int64_t state_stride;
+    const int32_t* slots; int64_t n_slots;
+    const void* dy; int64_t ld_dy;        /* gradients: rows x channels                         */
+    void* dx; int64_t ld_dx;
+    float* dweight;                       /* channels x width, overwritten; NULL: not wanted    */
+    float* dbias;                         /* channels, overwritten; NULL: not wanted            */
+    const void* dstate_out;               /* gradient of the state after, or NULL               */
+    void* dstate_in;                      /* gradient of the state before, or NULL              */
+    void* workspace; size_t workspace_bytes;
+} tdx_conv1d_args;
+
+/* y and state_out. */
+int tdx_causal_conv1d(const tdx_conv1d_args* args, void* stream);
+/* dx, dweight, dbias, dstate_in from x, weight, bias, state_in, dy and dstate_out; pre is computed again.  Needs a workspace. */
+int tdx_causal_conv1d_bwd(const tdx_conv1d_args* args, void* stream);
+/* One token for each of `batch` rows of x and y: seq_offsets, max_len and rows are not used, state_in and state_out are
+ * needed (width > 1), and a row without a slot is padding whose y is zero. */
+int tdx_causal_conv1d_step(const tdx_conv1d_args* args, void* stream);
+/* Workspace of tdx_causal_conv1d_bwd (host only). */
+int tdx_causal_conv1d_workspace_size(const tdx_conv1d_args* args, size_t* bytes);
+
+/*
+ * Selective scan: with dt' = softplus(dt + dt_bias) (dt_softplus = 1) or dt + dt_bias, and B, C of the channel's group,
+ *
+ *   h[t, d, n] = exp(dt'[t, d] * A[d, n]) * h[t - 1, d, n] + dt'[t, d] * x[t, d] * B[t, n]
+ *   y[t, d]    = sum_n C[t, n] * h[t, d, n] + D[d] * x[t, d],     out = y * silu(z), or y without z.
+ *
+ * channels is a multiple of groups; group g holds the channels g * channels / groups and up.  1 <= states <= 128.
+ */
+typedef struct {
+    int64_t batch, max_len, rows, channels;
+    int states, groups;
+    int dtype;                    /* tdx_dtype                                                   */
+    int dt_softplus;              /* 0 or 1                                                      */
+    const void* x; int64_t ld_x;          /* rows x channels                                     */
+    const void* dt; int64_t ld_dt;        /* rows x channels                                     */
+    const float* A;                       /* channels x states, dense                            */
+    const void* B; int64_t ld_B;          /* rows x (groups * states)                            */
+    const void* C; int64_t ld_C;          /* rows x (groups * states)                            */
+    const float* D;                       /* channels, or NULL                                   */
+    const void* z; int64_t ld_z;          /* rows x channels, or NULL                            */
+    const float* dt_bias;                 /* channels, or NULL                                   */
+    void* out; int64_t ld_out;            /* rows x channels                                     */
+    const int32_t* seq_offsets;
+    const float* state_in;                /* n_slots x channels x states                         */
+    float* state_out;
+    int64_t state_stride;
+    const int32_t* slots; int64_t n_slots;
+    float* saved; size_t saved_bytes;     /* states that the forward pass keeps for the backward one (16-byte aligned); */
+                                          /* NULL in the forward pass: not kept                  */
+    const void* dout; int64_t ld_dout;    /* gradients: rows x channels                          */
+    void* dx; int64_t ld_dx;
+    void* ddt; int64_t ld_ddt;
+    void* dB; int64_t ld_dB;
+    void* dC; int64_t ld_dC;
+    void* dz; int64_t ld_dz;              /* needed with z                                       */
+    float* dA;                            /* channels x states, overwritten                      */
+    float* dD;                            /* channels, overwritten; NULL: not wanted             */
+    float* ddt_bias;                      /* channels, overwritten; NULL: not wanted             */
+    const float* dstate_out;              /* gradient of the state after, or NULL                */
+    float* dstate_in;                     /* gradient of the state before, or NULL               */
+    void* workspace; size_t workspace_bytes;
+} tdx_scan_args;
+
+/* out, state_out and (for a later backward pass) saved.  Needs a workspace when tdx_selective_scan_workspace_size is not 0. */
+int tdx_selective_scan(const tdx_scan_args* args, void* stream);
+/* All gradients, from the forward pass's inputs, `saved` and dout (and dstate_out).  Needs a workspace. */
+int tdx_selective_scan_bwd(const tdx_scan_args* args, void* stream);
+/* One token for each of `batch` rows: seq_offsets, max_len and rows are not used, state_in and state_out are needed, and a
+ * row without a slot is padding whose out is zero. */
+int tdx_selective_scan_step(const tdx_scan_args* args, void* stream);
+/* Bytes of `saved`, and of the workspace that covers tdx_selective_scan and (when args->saved is set) tdx_selective_scan_bwd
+ * (host only; the workspace depends on the current device's SM count, or on a B200's where there is no device). */
+int tdx_selective_scan_saved_size(const tdx_scan_args* args, size_t* bytes);
+int tdx_selective_scan_workspace_size(const tdx_scan_args* args, size_t* bytes);
+
+/*
+ * Product with 4-bit weights: y[m, n] = sum_k x[m, k] * scales[n, k / group_size] * (q[n, k] - zeros[n, k / group_size]),
+ * M of one token or a few (any M is accepted).  fp32 sums of the exact products, one rounding to the type of y; K = 0: y = 0.
+ */
+typedef struct {
+    int64_t M, N, K;
+    int group_size;               /* >= 1; 32, 64 and 128 that divide K run on the tensor cores      */
+    int dtype;                    /* tdx_dtype of x, scales and y                                */
+    const void* x; int64_t ld_x;          /* M x K                                               */
+    const uint8_t* weight;                /* N rows of ceil(K / 2) bytes: q[n, k], the even k in the low half of a byte */
+    const void* scales;                   /* N x ceil(K / group_size), dense                     */
+    const uint8_t* zeros;                 /* N x ceil(K / group_size), dense; NULL: 8 everywhere */
+    void* y; int64_t ld_y;                /* M x N                                               */
+} tdx_w4_args;
+
+int tdx_gemm_w4(const tdx_w4_args* args, void* stream);
+/*
+ * Weights for it from w (N x K, rows ld_w elements apart, in the type `dtype`, which the scales get too).  zeros = NULL: scale =
+ * max |w| / 7 of the group and q = round(w / scale) + 8; else scale = (max(w, 0) - min(w, 0)) / 15, zero = round(-min / scale), q =
+ * round(w / scale) + zero, limited to 0 .. 15.  Halves round to even; an all-zero group gets the scale 1.  group_size is even or
+ * at least K.
+ */
+int tdx_w4_quantize(int64_t N, int64_t K, int group_size, int dtype, const void* w, int64_t ld_w, uint8_t* weight, void* scales,
+                    uint8_t* zeros, void* stream);
+
+/*
  * Host-buffer variants: A, B, C (x, w, bias, y) are HOST pointers (pinned memory gives the best
  * copy rate).  The call copies the inputs to device staging buffers owned by the library, runs the
  * same kernels as above, copies the result back and returns after the stream has drained.
@@ -394,7 +539,7 @@ int tdx_tune_clear(void);
 /*
  * Synchronises `stream`, reads and clears the device status word.  TDX_OK, or TDX_ERR_TIMEOUT if a
  * kernel abandoned a bounded wait since the last check (its outputs are then unspecified), or TDX_ERR_BOUNDS if the
- * bounds-checked debug mode skipped an access.
+ * bounds-checked debug mode skipped an access or a sequence operator met an offset or a slot outside the caller's tensors.
  */
 int tdx_check_device_status(void* stream);
 

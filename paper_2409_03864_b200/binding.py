@@ -51,6 +51,50 @@ class tdx_config(ctypes.Structure):
         return "tdx_config(" + ", ".join(f"{k}={v}" for k, v in self.as_dict().items()) + ")"
 
 
+class _Args(ctypes.Structure):
+    """A block of arguments: fields by keyword, pointers as tensors, integers or None.  It holds addresses only, so the
+    tensors must outlive it."""
+
+    def __init__(self, **fields):
+        super().__init__()
+        self.set(**fields)
+
+    def set(self, **fields):
+        for name, value in fields.items():
+            if name not in self._names:
+                raise TypeError(f"{type(self).__name__} has no field {name!r}")
+            setattr(self, name, _ptr(value) if name in self._pointers else value)
+        return self
+
+
+def _fields(text):
+    """'i64 a b; int c; ptr d' -> the fields of a ctypes structure, in order."""
+    types = {"i64": ctypes.c_int64, "int": ctypes.c_int, "ptr": ctypes.c_void_p, "size": ctypes.c_size_t}
+    return [(name, types[group.split()[0]]) for group in text.split(";") for name in group.split()[1:]]
+
+
+class tdx_conv1d_args(_Args):
+    _fields_ = _fields("i64 batch max_len rows channels; int width dtype silu; ptr x; i64 ld_x; ptr weight bias y; i64 ld_y;"
+                       "ptr seq_offsets state_in state_out; i64 state_stride; ptr slots; i64 n_slots; ptr dy; i64 ld_dy; ptr dx;"
+                       "i64 ld_dx; ptr dweight dbias dstate_out dstate_in workspace; size workspace_bytes")
+
+
+class tdx_scan_args(_Args):
+    _fields_ = _fields("i64 batch max_len rows channels; int states groups dtype dt_softplus; ptr x; i64 ld_x; ptr dt; i64 ld_dt;"
+                       "ptr A B; i64 ld_B; ptr C; i64 ld_C; ptr D z; i64 ld_z; ptr dt_bias out; i64 ld_out; ptr seq_offsets state_in"
+                       " state_out; i64 state_stride; ptr slots; i64 n_slots; ptr saved; size saved_bytes; ptr dout; i64 ld_dout;"
+                       "ptr dx; i64 ld_dx; ptr ddt; i64 ld_ddt; ptr dB; i64 ld_dB; ptr dC; i64 ld_dC; ptr dz; i64 ld_dz;"
+                       "ptr dA dD ddt_bias dstate_out dstate_in workspace; size workspace_bytes")
+
+
+class tdx_w4_args(_Args):
+    _fields_ = _fields("i64 M N K; int group_size dtype; ptr x; i64 ld_x; ptr weight scales zeros y; i64 ld_y")
+
+
+for _cls in (tdx_conv1d_args, tdx_scan_args, tdx_w4_args):
+    _cls._names = frozenset(n for n, _ in _cls._fields_)
+    _cls._pointers = frozenset(n for n, t in _cls._fields_ if t is ctypes.c_void_p)
+
 _lib = None
 
 
@@ -101,6 +145,12 @@ def lib() -> ctypes.CDLL:
         L.tdx_tune_gemm_space.argtypes = [i64, i64, i64, ci, ci, ci, ctypes.c_char_p, ci, ci, cfgp, fp, cfgp, fp, ci, ip, ip, vp]
         L.tdx_gemm_k_balanced_plan.argtypes = [i64, i64, i64, ci, ci, ci, ip, ci, ip, ip, ip]
         L.tdx_gemm_splitk_static.argtypes = [i64, i64, i64, ci, ci, cf, vp, vp, vp, ci, ci, vp]
+        for op in ("causal_conv1d", "causal_conv1d_bwd", "causal_conv1d_step", "selective_scan", "selective_scan_bwd",
+                   "selective_scan_step", "gemm_w4"):
+            getattr(L, "tdx_" + op).argtypes = [vp, vp]
+        for op in ("causal_conv1d_workspace_size", "selective_scan_workspace_size", "selective_scan_saved_size"):
+            getattr(L, "tdx_" + op).argtypes = [vp, ctypes.POINTER(sz)]
+        L.tdx_w4_quantize.argtypes = [i64, i64, ci, ci, vp, i64, vp, vp, vp, vp]
         L.tdx_check_device_status.argtypes = [vp]
         L.tdx_selftest_bounded_wait.argtypes = [ci, vp]
         L.tdx_selftest_bounds_check.argtypes = [vp]
@@ -128,6 +178,9 @@ EXPORTS = (
     "tdx_enum_conv2d_configs", "tdx_default_gemm_config", "tdx_default_conv2d_config", "tdx_tune_save",
     "tdx_tune_load", "tdx_tune_clear", "tdx_set_autotune", "tdx_gemm_tile_plan", "tdx_gemm_k_balanced_plan", "tdx_enum_gemm_space", "tdx_tune_gemm_space", "tdx_tune_conv2d_guided", "tdx_model_conv2d_us", "tdx_gemm_splitk_static", "tdx_check_device_status", "tdx_selftest_bounded_wait", "tdx_selftest_bounds_check", "tdx_kernel_launch_count", "tdx_last_error",
     "tdx_version",
+    "tdx_causal_conv1d", "tdx_causal_conv1d_bwd", "tdx_causal_conv1d_step", "tdx_causal_conv1d_workspace_size",
+    "tdx_selective_scan", "tdx_selective_scan_bwd", "tdx_selective_scan_step", "tdx_selective_scan_saved_size",
+    "tdx_selective_scan_workspace_size", "tdx_gemm_w4", "tdx_w4_quantize",
 )
 
 
@@ -401,6 +454,65 @@ def tdx_gemm_splitk_static(M, N, K, transA, transB, alpha, A, B, C, tile_n=0, sp
     on the GPU race on that array; keep them ordered on one stream."""
     return lib().tdx_gemm_splitk_static(M, N, K, transA, transB, alpha, _ptr(A), _ptr(B), _ptr(C), tile_n, split_k,
                                         _stream(stream))
+
+
+def tdx_causal_conv1d(args: tdx_conv1d_args, stream=None) -> int:
+    """Short causal convolution of packed sequences: y, and the states after them."""
+    return lib().tdx_causal_conv1d(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_causal_conv1d_bwd(args: tdx_conv1d_args, stream=None) -> int:
+    return lib().tdx_causal_conv1d_bwd(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_causal_conv1d_step(args: tdx_conv1d_args, stream=None) -> int:
+    """One token per batch row; the states move on by one row."""
+    return lib().tdx_causal_conv1d_step(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_selective_scan(args: tdx_scan_args, stream=None) -> int:
+    """Selective scan of packed sequences: out, the states after them, and what the backward pass needs (saved)."""
+    return lib().tdx_selective_scan(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_selective_scan_bwd(args: tdx_scan_args, stream=None) -> int:
+    return lib().tdx_selective_scan_bwd(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_selective_scan_step(args: tdx_scan_args, stream=None) -> int:
+    """One token per batch row; the states move on by one row."""
+    return lib().tdx_selective_scan_step(ctypes.addressof(args), _stream(stream))
+
+
+def _args_size(fn, args):
+    out = ctypes.c_size_t(0)
+    st = fn(ctypes.addressof(args), ctypes.byref(out))
+    return st, int(out.value)
+
+
+def tdx_causal_conv1d_workspace_size(args: tdx_conv1d_args):
+    """Returns (status, bytes)."""
+    return _args_size(lib().tdx_causal_conv1d_workspace_size, args)
+
+
+def tdx_selective_scan_workspace_size(args: tdx_scan_args):
+    """Returns (status, bytes)."""
+    return _args_size(lib().tdx_selective_scan_workspace_size, args)
+
+
+def tdx_selective_scan_saved_size(args: tdx_scan_args):
+    """Returns (status, bytes)."""
+    return _args_size(lib().tdx_selective_scan_saved_size, args)
+
+
+def tdx_gemm_w4(args: tdx_w4_args, stream=None) -> int:
+    """y = x . W^T with 4-bit weights W and a scale (and zero) per group of them."""
+    return lib().tdx_gemm_w4(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_w4_quantize(N, K, group_size, dtype, w, ld_w, weight, scales, zeros=None, stream=None) -> int:
+    """4-bit weights, scales and (unless None) zeros from an N x K matrix."""
+    return lib().tdx_w4_quantize(N, K, group_size, dtype, _ptr(w), ld_w, _ptr(weight), _ptr(scales), _ptr(zeros), _stream(stream))
 
 
 def tdx_check_device_status(stream=None) -> int:

@@ -1,0 +1,196 @@
+// What the kernels of the sequence operators (causal convolution, selective scan, 4-bit products) share: element
+// conversion, the elementwise functions, packed fp32 pairs, and the rows and state slots of a sequence.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace tdx {
+
+// recorded in the device status word (see kStatusBounds in simt_kernels.cuh): a sequence offset or a state slot that
+// lies outside the caller's tensors; that sequence or state is skipped
+enum : int { kStatusSequence = 9 };
+
+// ---------------------------------------------------------------- elements
+__device__ __forceinline__ float seq_to_float(float v) { return v; }
+__device__ __forceinline__ float seq_to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ T seq_from_float(float v);
+template <>
+__device__ __forceinline__ float seq_from_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 seq_from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// VEC elements that move as one access: 16, 8, 4 or 2 bytes
+template <int BYTES> struct SeqBits;
+template <> struct SeqBits<16> { typedef uint4 type; };
+template <> struct SeqBits<8> { typedef uint2 type; };
+template <> struct SeqBits<4> { typedef uint32_t type; };
+template <> struct SeqBits<2> { typedef uint16_t type; };
+template <typename T, int VEC>
+struct SeqVec {
+    typedef typename SeqBits<VEC * sizeof(T)>::type bits_t;
+    union { bits_t bits; T v[VEC]; };
+    __device__ __forceinline__ SeqVec() {}
+};
+template <typename T, int VEC>
+__device__ __forceinline__ SeqVec<T, VEC> seq_load(const T* p) {
+    SeqVec<T, VEC> r;
+    r.bits = __ldg(reinterpret_cast<const typename SeqVec<T, VEC>::bits_t*>(p));
+    return r;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void seq_store(T* p, const float (&f)[VEC]) {
+    SeqVec<T, VEC> r;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) r.v[i] = seq_from_float<T>(f[i]);
+    *reinterpret_cast<typename SeqVec<T, VEC>::bits_t*>(p) = r.bits;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void seq_unpack(const SeqVec<T, VEC>& r, float (&f)[VEC]) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) f[i] = seq_to_float(r.v[i]);
+}
+
+// ---------------------------------------------------------------- elementwise functions
+constexpr float kLog2e = 1.4426950408889634f;
+// 2^x by the special-function unit (error about 2^-22 of the result; results under 2^-126 are 0)
+__device__ __forceinline__ float fast_exp2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float sigmoid_f(float v) { return fast_rcp(1.0f + expf(-v)); }
+// log(1 + exp(v)) = max(v, 0) + log1p(u), u = exp(-|v|) in (0, 1], and log1p(u) = 2 atanh(s), s = u / (2 + u) <= 1/3:
+// no cancellation for any v, so the result keeps its relative accuracy where it is tiny.  atanh(s) / s is a polynomial of
+// degree 4 in s^2, fitted by least squares in relative error over [0, 1/9] (7.6e-9 with these coefficients).
+__device__ __forceinline__ float log1p_unit(float u) {
+    const float s = u * fast_rcp(2.0f + u), q = s * s;
+    float p = fmaf(q, 0.14080727f, 0.13982172f);
+    p = fmaf(q, p, 0.20012326f);
+    p = fmaf(q, p, 0.3333316f);
+    p = fmaf(q, p, 1.0f);
+    return 2.0f * s * p;
+}
+__device__ __forceinline__ float softplus_f(float v) { return fmaxf(v, 0.0f) + log1p_unit(expf(-fabsf(v))); }
+
+// the same with its derivative, the sigmoid of v, from the same exponential
+__device__ __forceinline__ float softplus_grad_f(float v, float& grad) {
+    const float u = expf(-fabsf(v));
+    grad = (v >= 0.0f ? 1.0f : u) * fast_rcp(1.0f + u);
+    return fmaxf(v, 0.0f) + log1p_unit(u);
+}
+// sum of N consecutive floats of shared memory, in ascending order (16-byte loads where N allows)
+template <int N>
+__device__ __forceinline__ float sum_row(const float* p, float s) {
+    if (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(p + i);
+            s += (v.x + v.y) + (v.z + v.w);
+        }
+    } else if (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 v = *reinterpret_cast<const float2*>(p + i);
+            s += v.x + v.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s += p[i];
+    }
+    return s;
+}
+
+// ---------------------------------------------------------------- pairs of fp32 (one instruction for two values)
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// ---------------------------------------------------------------- sequences
+// Sequence b occupies rows [first, first + len).  Without offsets the batch is dense.  Offsets live on the device, so the
+// kernels check them: a sequence that leaves [0, rows) or is longer than max_len is reported and treated as empty.
+struct SeqRange { long long first; int len; };
+__device__ __forceinline__ SeqRange seq_range(const int* __restrict__ offsets, long long b, long long max_len, long long rows, int* status) {
+    SeqRange r;
+    if (offsets == nullptr) {
+        r.first = b * max_len;
+        r.len = static_cast<int>(max_len);
+        return r;
+    }
+    const int lo = __ldg(offsets + b), hi = __ldg(offsets + b + 1);
+    if (lo < 0 || hi < lo || hi > rows || hi - lo > max_len) {
+        atomicCAS(status, 0, kStatusSequence);
+        r.first = 0;
+        r.len = 0;
+        return r;
+    }
+    r.first = lo;
+    r.len = hi - lo;
+    return r;
+}
+// Sequences are cut into pieces of `piece` rows, each worked on by a block (or a few).  A dense batch has `dense` pieces per
+// sequence.  Packed ones share rows / piece + batch numbers: sequence b starts at number offsets[b] / piece + b, which leaves
+// room for ceil(len / piece) of them and at least one, whatever the lengths are; the few numbers left over are pieces with no
+// rows.  Number i belongs to the last sequence that starts at or before i.
+constexpr int kNoPiece = 1 << 29;
+struct SeqPiece { long long b; int index; };
+__host__ __device__ __forceinline__ long long seq_pieces(bool packed, long long batch, long long rows, long long dense, long long piece) {
+    return packed ? rows / piece + batch : batch * dense;
+}
+__device__ __forceinline__ SeqPiece seq_piece(const int* __restrict__ offsets, long long batch, long long dense, long long piece, long long i) {
+    SeqPiece r;
+    if (offsets == nullptr) {
+        r.b = i / dense;
+        r.index = static_cast<int>(i - r.b * dense);
+        return r;
+    }
+    long long lo = 0, hi = batch - 1;
+    while (lo < hi) {
+        const long long mid = (lo + hi + 1) / 2;
+        if (__ldg(offsets + mid) / piece + mid <= i) lo = mid;
+        else hi = mid - 1;
+    }
+    r.b = lo;
+    const long long index = i - (__ldg(offsets + lo) / piece + lo);
+    r.index = index < 0 || index > kNoPiece ? kNoPiece : static_cast<int>(index);   // in front of the first sequence: no rows
+    return r;
+}
+// Slot of sequence (or batch row) b in the state tensors; negative: it has no state.
+__device__ __forceinline__ long long state_slot(const int* __restrict__ slots, long long b, long long n_slots, int* status) {
+    const long long s = slots == nullptr ? b : __ldg(slots + b);
+    if (s >= n_slots) {
+        atomicCAS(status, 0, kStatusSequence);
+        return -1;
+    }
+    return s;
+}
+
+__device__ __forceinline__ void seq_grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void seq_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+}  // namespace tdx

@@ -4,6 +4,7 @@
 // tile plans), host_launch.cuh (launches).
 #include "host_launch.cuh"
 #include "host_space.cuh"
+#include "seq_common.cuh"
 
 #include <array>
 #include <tuple>
@@ -1709,6 +1710,8 @@ int tdx_check_device_status(void* stream) {
     TDX_CUDA(cudaMemcpy(&v, ctx->status_ptr, sizeof v, cudaMemcpyDeviceToHost));
     if (v != 0) {
         TDX_CUDA(cudaMemset(ctx->status_ptr, 0, sizeof v));
+        if (v == tdx::kStatusSequence)
+            return fail(TDX_ERR_BOUNDS, "a sequence offset or a state slot lies outside the caller's tensors (that sequence or state was skipped)");
         if (v == tdx::kStatusBounds)
             return fail(TDX_ERR_BOUNDS, "the bounds-checked debug mode caught an index outside its operand (the access was skipped)");
         return fail(TDX_ERR_TIMEOUT, "a kernel abandoned a bounded wait (role code %d)", v);
@@ -1888,3 +1891,5 @@ const char* tdx_last_error(void) { return g_err.c_str(); }
 const char* tdx_version(void) { return "tdx 0.1.0 (sm_100a)"; }
 
 }  // extern "C"
+
+#include "seq_api.cuh"

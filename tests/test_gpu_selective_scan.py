@@ -1,0 +1,374 @@
+"""GPU parity of the selective scan (forward, backward, single tokens) with its 64-bit definition."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2409_03864_b200 as tdx
+import seq_reference as ref
+from seq_util import DT, EPS, Rows, assert_close, f32, i32, offsets_of, seeded, workspace
+
+pytestmark = pytest.mark.gpu
+
+
+def factors(longest, states, channels, rows, reach):
+    """What rounding may do, in units of the sums' magnitudes.  A decay is off by 2^-22 (the exponential) and by |dt' A| <= reach times
+    the 10 EPS of dt' A; a state carries the errors of at most `longest` of them.  Gradients carry those of h, dh and y."""
+    decay = longest * (2.0 ** -22 + 10 * reach * EPS)
+    forward = decay + (longest + states + 24) * EPS
+    return {"out": forward, "state": forward, "grad": 3 * forward, "over_channels": 3 * forward + channels * EPS, "over_rows": 3 * forward + rows * EPS}
+
+
+class Problem:
+    def __init__(self, dtype, states, channels, lengths, packed, groups=1, softplus=1, z=True, D=True, bias=True, with_states=True, seed=0, pad=0,
+                 lead=0, order=None):
+        rng = np.random.default_rng(seed)
+        n, d, rows = states, channels, int(sum(lengths))
+        self.dtype, self.n, self.d, self.rows, self.groups, self.softplus = dtype, n, d, rows, groups, softplus
+        self.lengths, batch = list(lengths), len(lengths)
+        longest = max(self.lengths, default=0)
+        self.offsets = offsets_of(lengths) if packed else None
+        seqs = ref.pieces(batch, longest, self.offsets)
+        self.v = {
+            "x": seeded(rng, (rows, d), dtype), "dt": seeded(rng, (rows, d), dtype, 0.5) if softplus else seeded(rng, (rows, d), dtype, lo=0.01, hi=0.3),
+            "A": -seeded(rng, (d, n), "f32", lo=0.1, hi=4.0), "B": seeded(rng, (rows, groups * n), dtype), "C": seeded(rng, (rows, groups * n), dtype),
+            "D": seeded(rng, (d,), "f32") * bool(D), "z": seeded(rng, (rows, d), dtype) if z else None,
+            "dt_bias": (seeded(rng, (d,), "f32", lo=-5.0, hi=-1.0) if softplus else seeded(rng, (d,), "f32", lo=0.0, hi=0.1)) * bool(bias),
+            "use_softplus": softplus, "groups": groups, "seqs": seqs, "state": seeded(rng, (batch, d, n), "f32") if with_states else np.zeros((batch, d, n))}
+        v = self.v
+        self.dout, self.dstate = seeded(rng, (rows, d), dtype), seeded(rng, (batch, d, n), "f32")
+        self.slots = list(range(batch)) if order is None else order
+        self.n_slots = max(self.slots, default=-1) + 2
+        self.all_states = np.full((self.n_slots, d, n), 3.0)
+        for b, s in enumerate(self.slots):
+            if s >= 0:
+                self.all_states[s] = v["state"][b]
+            else:
+                v["state"][b] = 0.0
+        step = ref.softplus(v["dt"] + v["dt_bias"]) if softplus else np.abs(v["dt"] + v["dt_bias"])
+        reach = float((step.max(0)[:, None] * np.abs(v["A"])).max()) if rows else 1.0
+        self.f = factors(longest, n, d, rows, reach)
+        self.dev = {k: Rows(v[k], dtype, pad, lead) for k in ("x", "dt", "B", "C") + (("z",) if z else ())}
+        self.par = {k: f32(v[k]) for k in ("A",) + (("D",) if D else ()) + (("dt_bias",) if bias else ())}
+        self.dev_state = Rows(self.all_states, "f32")
+        self.dev_offsets, self.dev_slots = i32(self.offsets), None if order is None else i32(order)
+        self.args = tdx.tdx_scan_args(
+            batch=batch, max_len=longest, rows=rows, channels=d, states=n, groups=groups, dtype=DT[dtype], dt_softplus=softplus,
+            **{k: t.ptr for k, t in self.dev.items()}, **{"ld_" + k: t.ld for k, t in self.dev.items()}, **self.par, seq_offsets=self.dev_offsets,
+            state_in=self.dev_state.ptr if with_states else None, slots=self.dev_slots, n_slots=self.n_slots)
+
+    def forward(self, pad=0, lead=0, in_place=False, save=False):
+        self.out = Rows(np.zeros((self.rows, self.d)), self.dtype, pad, lead, fill=float("nan"))
+        self.new_state = self.dev_state if in_place else Rows(np.full_like(self.all_states, 5.0), "f32")
+        self.args.set(out=self.out.ptr, ld_out=self.out.ld, state_out=self.new_state.ptr)
+        if save:
+            self.saved = workspace(tdx.tdx_selective_scan_saved_size(self.args))
+            self.args.set(saved=self.saved, saved_bytes=self.saved.numel())
+        self.ws = workspace(tdx.tdx_selective_scan_workspace_size(self.args))
+        self.args.set(workspace=self.ws, workspace_bytes=self.ws.numel())
+        tdx.check(tdx.tdx_selective_scan(self.args))
+        torch.cuda.synchronize()
+
+    def check_forward(self):
+        o, m = ref.scan(**self.v), ref.scan(**self.v, magnitude=True)
+        assert_close("out", self.out.host(), o["out"], m["out"], self.f["out"], self.dtype)
+        new, old = self.new_state.host(), self.all_states if self.new_state is self.dev_state else np.full_like(self.all_states, 5.0)
+        for b, s in enumerate(self.slots):
+            if s >= 0:
+                assert_close("state", new[s], o["state"][b], m["state"][b], self.f["state"])
+        for s in set(range(self.n_slots)) - set(self.slots):
+            assert np.array_equal(new[s], old[s])
+        assert self.out.guards_intact() and self.new_state.guards_intact()
+        assert tdx.tdx_check_device_status() == 0
+
+    def backward(self, pad=0, lead=0, with_state=True):
+        g = self.groups * self.n
+        shape = {"dx": self.d, "ddt": self.d, "dB": g, "dC": g} | ({"dz": self.d} if "z" in self.dev else {})
+        self.g = {k: Rows(np.zeros((self.rows, w)), self.dtype, pad, lead, fill=float("nan")) for k, w in shape.items()}
+        self.p = {"dA": f32(np.full((self.d, self.n), np.nan)), "dD": f32(np.full(self.d, np.nan)), "ddt_bias": f32(np.full(self.d, np.nan))}
+        given = np.zeros_like(self.all_states)
+        for b, s in enumerate(self.slots):
+            if s >= 0:
+                given[s] = self.dstate[b]
+            else:
+                self.dstate[b] = 0.0
+        if not with_state:
+            self.dstate[:] = 0.0
+        self.dev_dout, self.dev_dstate = Rows(self.dout, self.dtype, pad), Rows(given, "f32")
+        self.dstate_in = Rows(np.zeros_like(self.all_states), "f32", fill=float("nan"))
+        self.args.set(dout=self.dev_dout.ptr, ld_dout=self.dev_dout.ld, **{k: t.ptr for k, t in self.g.items()},
+                      **{"ld_" + k: t.ld for k, t in self.g.items()}, **self.p, dstate_out=self.dev_dstate.ptr if with_state else None,
+                      dstate_in=self.dstate_in.ptr if with_state else None)
+        self.ws.fill_(0xFF)
+        tdx.check(tdx.tdx_selective_scan_bwd(self.args))
+        torch.cuda.synchronize()
+
+    def check_backward(self, with_state=True):
+        extra = {"dout": self.dout, "dstate": self.dstate}
+        o, m = ref.scan(**self.v, **extra), ref.scan(**self.v, **extra, magnitude=True)
+        kind = {"dx": "grad", "ddt": "grad", "dz": "grad", "dB": "over_channels", "dC": "over_channels"}
+        for k, t in self.g.items():
+            assert_close(k, t.host(), o[k], m[k], self.f[kind[k]], self.dtype)
+            assert t.guards_intact(), k
+        for k, t in self.p.items():
+            assert_close(k, t.double().cpu().numpy(), o[k], m[k], self.f["over_rows"])
+        if with_state:
+            got = self.dstate_in.host()
+            for b, s in enumerate(self.slots):
+                if s >= 0:
+                    assert_close("dstate", got[s], o["dstate"][b], m["dstate"][b], self.f["grad"])
+            for s in set(range(self.n_slots)) - set(self.slots):
+                assert np.isnan(got[s]).all()
+        assert tdx.tdx_check_device_status() == 0
+
+
+SHAPES = [
+    # states, channels, lengths, packed, groups
+    (16, 64, [37], False, 1),
+    (16, 32, [8, 8], False, 1),              # one backward tile, one channel tile
+    (16, 33, [9, 1, 0, 70], True, 1),        # odd channels, an empty sequence
+    (16, 40, [300], False, 1),               # cut into chunks: few channels, a long sequence
+    (16, 48, [200, 0, 3, 150], True, 2),     # cut, packed, two groups
+    (4, 130, [33, 20], True, 1),
+    (3, 10, [1, 1, 1], False, 1),            # single tokens, states that do not fill a thread
+    (8, 96, [65, 64], True, 3),
+    (1, 5, [40], False, 5),                  # one state, a group per channel
+    (20, 24, [31], False, 1),
+    (64, 12, [70, 2], True, 2),
+    (128, 6, [40], False, 1),
+    (100, 9, [3, 129], True, 3),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_forward_and_backward(shape, dtype):
+    n, d, lengths, packed, groups = shape
+    p = Problem(dtype, n, d, lengths, packed, groups)
+    p.forward(save=True)
+    p.check_forward()
+    p.backward()
+    p.check_backward()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("without", ["z", "D", "bias", "softplus", "states", "all"])
+def test_optional_parts(dtype, without):
+    off = lambda k: without not in (k, "all")  # noqa: E731
+    p = Problem(dtype, 16, 72, [50, 0, 21], True, softplus=int(off("softplus")), z=off("z"), D=off("D"), bias=off("bias"), with_states=off("states"))
+    p.forward(save=True)
+    p.check_forward()
+    p.backward(with_state=off("states"))
+    p.check_backward(with_state=off("states"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,lead", [(32, 0), (0, 32), (3, 0), (0, 1)])
+def test_slices_of_wider_tensors(dtype, pad, lead):
+    p = Problem(dtype, 16, 64, [40, 25], True, pad=pad, lead=lead)
+    p.forward(pad, lead, save=True)
+    p.check_forward()
+    p.backward(pad, lead)
+    p.check_backward()
+
+
+@pytest.mark.parametrize("lengths", [[2, 0, 60, 1, 3], [200, 0, 260, 1, 3]])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_states_in_slots(in_place, lengths):
+    p = Problem("f32", 16, 40, lengths, True, order=[5, 2, 0, -1, 3])
+    p.forward(in_place=in_place, save=True)
+    p.check_forward()
+    if not in_place:
+        p.backward()
+        p.check_backward()
+
+
+def test_a_forward_pass_that_saves_nothing_gives_the_same_bits():
+    p = Problem("bf16", 16, 64, [100, 31], True)
+    p.forward()
+    first = p.out.view.clone(), p.new_state.view.clone()
+    p.forward(save=True)
+    assert torch.equal(first[0], p.out.view) and torch.equal(first[1], p.new_state.view)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d,groups", [(16, 64, 1), (16, 37, 1), (5, 33, 3), (1, 16, 1), (8, 100, 2), (32, 40, 1), (128, 8, 1), (64, 7, 7)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_single_tokens_follow_a_sequence(n, d, groups, dtype, in_place):
+    batch, length, slots = 4, 5, [4, 0, 6, 2]
+    p = Problem(dtype, n, d, [length] * batch, False, groups, with_states=False)
+    o, m = ref.scan(**p.v), ref.scan(**p.v, magnitude=True)
+    state = [Rows(np.zeros((7, d, n)), "f32") for _ in range(2)]
+    out = Rows(np.zeros((batch, d)), dtype, 1)
+    order = i32(slots)
+    for t in range(length):
+        now, after = (state[0], state[0]) if in_place else (state[t % 2], state[1 - t % 2])
+        rows = {k: Rows(p.v[k].reshape(batch, length, -1)[:, t], dtype, 1) for k in ("x", "dt", "B", "C", "z")}
+        a = tdx.tdx_scan_args(batch=batch, channels=d, states=n, groups=groups, dtype=DT[dtype], dt_softplus=1, **{k: r.ptr for k, r in rows.items()},
+                              **{"ld_" + k: r.ld for k, r in rows.items()}, **p.par, out=out.ptr, ld_out=out.ld, state_in=now.ptr, state_out=after.ptr,
+                              slots=order, n_slots=7)
+        tdx.check(tdx.tdx_selective_scan_step(a))
+        torch.cuda.synchronize()
+        assert_close("out", out.host(), o["out"].reshape(batch, length, d)[:, t], m["out"].reshape(batch, length, d)[:, t], p.f["out"], dtype)
+    assert_close("state", after.host()[slots], o["state"], m["state"], p.f["state"])
+    assert out.guards_intact() and all(s.guards_intact() for s in state) and tdx.tdx_check_device_status() == 0
+
+
+def test_padding_rows_of_a_step_and_slots_out_of_range():
+    d, n = 40, 16
+    state = Rows(np.ones((3, d, n)), "f32")
+    state.view[1] = float("nan")
+    rows = {k: Rows(np.full((4, w), np.nan), "f32") for k, w in (("x", d), ("dt", d), ("B", n), ("C", n))}
+    for r in rows.values():
+        r.view[0] = 1.0
+    out = Rows(np.zeros((4, d)), "f32", fill=float("nan"))
+    A, slots = f32(np.zeros((d, n))), i32([2, -1, -7, -1])
+    a = tdx.tdx_scan_args(batch=4, channels=d, states=n, groups=1, dtype=tdx.TDX_F32, dt_softplus=0, **{k: r.ptr for k, r in rows.items()},
+                          **{"ld_" + k: r.ld for k, r in rows.items()}, A=A, out=out.ptr, ld_out=d, state_in=state.ptr, state_out=state.ptr, slots=slots,
+                          n_slots=3)
+    tdx.check(tdx.tdx_selective_scan_step(a))
+    torch.cuda.synchronize()
+    assert (out.host()[0] == 2 * n).all() and (out.host()[1:] == 0).all()
+    assert (state.host()[2] == 2).all() and (state.host()[0] == 1).all() and np.isnan(state.host()[1]).all()
+    assert tdx.tdx_check_device_status() == 0
+    slots2 = i32([0, 3, 2, -1])
+    a.set(slots=slots2)
+    tdx.check(tdx.tdx_selective_scan_step(a))
+    assert tdx.tdx_check_device_status() == tdx.TDX_ERR_BOUNDS
+    assert (out.host()[1] == 0).all()
+
+
+@pytest.mark.parametrize("long", [False, True])
+def test_what_lies_outside_the_sequences_is_neither_read_nor_written(long):
+    k = 150 if long else 15
+    lengths, front, back = [6, 0, k], 4, 5
+    inner = Problem("f32", 16, 40, lengths, True, with_states=False)
+    rows = front + inner.rows + back
+    offsets = offsets_of(lengths) + front
+
+    def widened(v, fill):
+        w = np.full((rows, v.shape[1]), fill)
+        w[front:front + inner.rows] = v
+        return Rows(w, "f32")
+
+    dev = {key: widened(inner.v[key], np.nan) for key in ("x", "dt", "B", "C", "z")}
+    dout = widened(inner.dout, np.inf)
+    outs = {key: widened(np.full((inner.rows, w), 9.0), 9.0) for key, w in
+            (("out", 40), ("dx", 40), ("ddt", 40), ("dz", 40), ("dB", 16), ("dC", 16))}
+    par = {key: f32(np.full(s, np.nan)) for key, s in (("dA", (40, 16)), ("dD", 40), ("ddt_bias", 40))}
+    off = i32(offsets)
+    a = tdx.tdx_scan_args(batch=3, max_len=max(lengths), rows=rows, channels=40, states=16, groups=1, dtype=tdx.TDX_F32, dt_softplus=1, seq_offsets=off,
+                          **{key: t.ptr for key, t in {**dev, **outs, "dout": dout}.items()},
+                          **{"ld_" + key: t.ld for key, t in {**dev, **outs, "dout": dout}.items()}, **inner.par, **par)
+    saved = workspace(tdx.tdx_selective_scan_saved_size(a))
+    a.set(saved=saved, saved_bytes=saved.numel())
+    ws = workspace(tdx.tdx_selective_scan_workspace_size(a))
+    a.set(workspace=ws, workspace_bytes=ws.numel())
+    tdx.check(tdx.tdx_selective_scan(a))
+    tdx.check(tdx.tdx_selective_scan_bwd(a))
+    torch.cuda.synchronize()
+    o, m = ref.scan(**inner.v, dout=inner.dout), ref.scan(**inner.v, dout=inner.dout, magnitude=True)
+    for key, t in outs.items():
+        got = t.host()
+        factor = inner.f["out" if key == "out" else "over_channels" if key in ("dB", "dC") else "grad"]
+        assert_close(key, got[front:front + inner.rows], o[key], m[key], factor)
+        assert (got[:front] == 9).all() and (got[front + inner.rows:] == 9).all(), key
+    for key, t in par.items():
+        assert_close(key, t.double().cpu().numpy(), o[key], m[key], inner.f["over_rows"])
+
+
+def test_bad_offsets_are_reported_and_their_sequences_skipped():
+    d, n = 32, 16
+    rows = {k: Rows(np.ones((10, w)), "f32") for k, w in (("x", d), ("dt", d), ("B", n), ("C", n))}
+    out = Rows(np.full((10, d), 9.0), "f32")
+    A = f32(np.zeros((d, n)))
+    for offsets, good in (([0, 4, 11], slice(0, 4)), ([0, 4, 3], slice(0, 4)), ([0, 9, 10], slice(9, 10)), ([-2, 4, 8], slice(4, 8))):
+        out.view[:] = 9.5
+        off = i32(offsets)
+        a = tdx.tdx_scan_args(batch=2, max_len=6, rows=10, channels=d, states=n, groups=1, dtype=tdx.TDX_F32, dt_softplus=0,
+                              **{k: r.ptr for k, r in rows.items()}, **{"ld_" + k: r.ld for k, r in rows.items()}, A=A, out=out.ptr, ld_out=d, seq_offsets=off)
+        tdx.check(tdx.tdx_selective_scan(a))
+        assert tdx.tdx_check_device_status() == tdx.TDX_ERR_BOUNDS
+        got, rest = out.host(), np.ones(10, dtype=bool)
+        rest[good] = False
+        assert (got[good] != 9.5).all() and (got[rest] == 9.5).all()
+
+
+def test_extreme_steps():
+    """A step so long that the state is forgotten, one of zero (an exact copy of the state), and decays that underflow."""
+    d, n = 32, 16
+    rng = np.random.default_rng(5)
+    dt = np.zeros((3, d))
+    dt[1] = 1e4                                             # exp(-1e4 * A) = 0
+    v = {"x": rng.standard_normal((3, d)), "dt": dt, "B": rng.standard_normal((3, n)), "C": rng.standard_normal((3, n))}
+    v["x"][1] *= 1e-4
+    rows = {k: Rows(t, "f32") for k, t in v.items()}
+    out, state, A = Rows(np.zeros((3, d)), "f32"), Rows(np.ones((1, d, n)), "f32"), f32(-rng.uniform(0.5, 2, (d, n)))
+    a = tdx.tdx_scan_args(batch=1, max_len=3, rows=3, channels=d, states=n, groups=1, dtype=tdx.TDX_F32, dt_softplus=0,
+                          **{k: r.ptr for k, r in rows.items()}, **{"ld_" + k: r.ld for k, r in rows.items()}, A=A, out=out.ptr, ld_out=d,
+                          state_in=state.ptr, state_out=state.ptr, n_slots=1)
+    tdx.check(tdx.tdx_selective_scan(a))
+    torch.cuda.synchronize()
+    f = {k: r.host() for k, r in rows.items()}
+    assert np.allclose(out.host()[0], f["C"][0].sum(), rtol=0, atol=1e-5)
+    want = (f["dt"][1] * f["x"][1])[:, None] * f["B"][1]
+    assert np.allclose(state.host()[0], want, rtol=1e-6, atol=0)
+    assert np.allclose(out.host()[2], (want * f["C"][2]).sum(1), rtol=1e-5, atol=1e-5)
+
+
+def test_gradients_against_differences_of_the_forward_pass():
+    """Central differences of the fp32 forward pass: a step of 1e-2 leaves a truncation error of about 1e-4 of the sums' size and a
+    rounding error of about 1e-5 / 1e-2."""
+    p = Problem("f32", 16, 48, [60], False, with_states=False)
+    p.forward(save=True)
+    p.backward(with_state=False)
+    rng = np.random.default_rng(9)
+    grads = {k[1:]: t.host() for k, t in p.g.items()} | {k[1:]: t.double().cpu().numpy() for k, t in p.p.items()}
+    for name in ("x", "dt", "B", "C", "z", "A", "D", "dt_bias"):
+        direction = rng.standard_normal(p.v[name].shape)
+        direction *= 1e-2 / np.sqrt(np.mean(direction ** 2))
+        buf = p.dev[name].view if name in p.dev else p.par[name]
+        kept, sums = buf.clone(), []
+        for sign in (1, -1):
+            buf[:] = kept + torch.from_numpy(sign * direction.reshape(tuple(buf.shape))).cuda().float()
+            tdx.check(tdx.tdx_selective_scan(p.args))
+            torch.cuda.synchronize()
+            sums.append((p.out.host() * p.dout).sum())
+        buf[:] = kept
+        want, got = (sums[0] - sums[1]) / 2, (grads[name] * direction).sum()
+        size = np.sqrt(((grads[name] * direction) ** 2).sum())
+        assert abs(got - want) < 2e-2 * max(size, abs(want)), (name, got, want)
+
+
+def test_same_bits_every_time_on_another_stream_and_in_a_graph():
+    p = Problem("bf16", 16, 64, [300, 3, 90], True)
+    p.forward(save=True)
+    p.backward()
+    outs = [p.out.view, *(t.view for t in p.g.values()), *p.p.values()]
+    first = [t.clone() for t in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        p.dev["x"].view[:] = p.dev["x"].view * 1.0
+        tdx.check(tdx.tdx_selective_scan(p.args, side))
+        tdx.check(tdx.tdx_selective_scan_bwd(p.args, side))
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, outs))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        stream = torch.cuda.current_stream()
+        tdx.check(tdx.tdx_selective_scan(p.args, stream))
+        tdx.check(tdx.tdx_selective_scan_bwd(p.args, stream))
+    for t in outs:
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, outs))
+
+
+def test_empty_problems():
+    p = Problem("f32", 16, 16, [0, 0, 0], True)
+    p.forward(save=True)
+    p.check_forward()
+    p.backward()
+    p.check_backward()
+    assert all((t == 0).all() for t in p.p.values())
