@@ -250,8 +250,8 @@ int tdx_conv2d_bias_relu_ex(int64_t N, int64_t H, int64_t W, int64_t Cin, int64_
  * Each call takes a block of arguments that a program fills once and passes with every call.  Fields that a call does not
  * use are ignored.  Conventions of all of them, beside those at the top of this file:
  *  - Activations (x, dt, B, C, z, outputs, their gradients) are TDX_F32 or TDX_BF16, channels contiguous, one row per token,
- *    rows `ld_*` elements apart, so that a slice of a projection is passed as it is.  Any alignment and any ld >= the row's
- *    width is accepted; 16-byte aligned rows are fastest.  Parameters, their gradients and scan states are fp32.
+ *    rows `ld_*` elements apart, so that a slice of a projection is passed as it is.  Any alignment and any ld from the row's
+ *    width up to 2^24 is accepted; 16-byte aligned rows are fastest.  Parameters, their gradients and scan states are fp32.
  *  - Sequences: seq_offsets = NULL is a dense batch of `batch` sequences of max_len rows each (rows = batch * max_len).
  *    Otherwise sequence b has the rows seq_offsets[b] .. seq_offsets[b + 1] - 1 (device memory, batch + 1 values, ascending),
  *    none longer than max_len; empty ones are allowed, and rows outside every sequence are neither read nor written.  A

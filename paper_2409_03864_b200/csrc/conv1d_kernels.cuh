@@ -86,7 +86,6 @@ __device__ __forceinline__ void conv_load_weights(const Conv1dParams& p, long lo
 // state_in.
 template <typename T, int VEC, int KW>
 __global__ void __launch_bounds__(128) conv1d_fwd_kernel(const __grid_constant__ Conv1dParams p) {
-    seq_launch_dependents();
     seq_grid_wait();
     const long long bid = blockIdx.x;
     const int ct = static_cast<int>(bid % p.channel_tiles);
@@ -131,7 +130,7 @@ __global__ void __launch_bounds__(128) conv1d_fwd_kernel(const __grid_constant__
                     for (int k = 0; k < KW - 1; ++k)
                         if (conv_tap<KW>(k, p.width)) acc = fmaf(w[k][i], win[k][i], acc);
                     acc = fmaf(w[KW - 1][i], now[i], acc);
-                    out[i] = p.silu ? acc * sigmoid_f(acc) : acc;
+                    out[i] = p.silu ? acc * sigmoid_f<T>(acc) : acc;
 #pragma unroll
                     for (int k = 0; k + 1 < KW - 1; ++k) win[k][i] = win[k + 1][i];
                     win[KW - 2][i] = now[i];
@@ -151,9 +150,10 @@ __global__ void __launch_bounds__(128) conv1d_fwd_kernel(const __grid_constant__
     }
 }
 
+template <typename T>
 __device__ __forceinline__ float conv_act_grad(float pre, int silu) {
     if (!silu) return 1.0f;
-    const float s = sigmoid_f(pre);
+    const float s = sigmoid_f<T>(pre);
     return s * fmaf(pre, 1.0f - s, 1.0f);
 }
 
@@ -166,7 +166,6 @@ template <typename T, int VEC, int KW>
 __global__ void __launch_bounds__(128) conv1d_bwd_kernel(const __grid_constant__ Conv1dParams p) {
     constexpr int kSums = VEC * (KW + 1);
     __shared__ float sums[kConvRuns][32][kSums + 1];
-    seq_launch_dependents();
     seq_grid_wait();
     const long long bid = blockIdx.x;
     const int ct = static_cast<int>(bid % p.channel_tiles);
@@ -238,7 +237,7 @@ __global__ void __launch_bounds__(128) conv1d_bwd_kernel(const __grid_constant__
                             for (int k = 0; k < KW - 1; ++k)
                                 if (conv_tap<KW>(k, p.width)) pre = fmaf(w[k][v], win[k][v], pre);
                             pre = fmaf(w[KW - 1][v], now[v], pre);
-                            g[v] *= conv_act_grad(pre, p.silu);
+                            g[v] *= conv_act_grad<T>(pre, p.silu);
                         }
                         if (own) {
 #pragma unroll
@@ -337,7 +336,7 @@ __global__ void __launch_bounds__(128) conv1d_step_kernel(const __grid_constant_
 #pragma unroll
             for (int k = 0; k < KW; ++k)
                 if (conv_tap<KW>(k, p.width)) acc = fmaf(w[k][i], win[k][i], acc);
-            out[i] = p.silu ? acc * sigmoid_f(acc) : acc;
+            out[i] = p.silu ? acc * sigmoid_f<T>(acc) : acc;
         }
 #pragma unroll
         for (int k = 1; k < KW; ++k)

@@ -4,9 +4,12 @@
 //   h[t] = exp(dt'[t, d] A[d, n]) h[t - 1] + dt'[t, d] x[t, d] B[t, n]
 //   y[t, d] = sum_n C[t, n] h[t, d, n] + D[d] x[t, d],   out = y * silu(z)  (or y)
 //
-// A thread keeps four states of one channel in registers, TPC threads hold a channel's states (up to 4 * TPC; the rest are
-// zero), and a block of 128 threads walks 128 / TPC channels of one group through a sequence, or through one chunk of it, in
-// tiles of a few dozen rows: the elementwise work of a tile is spread over all threads and goes through shared memory.
+// The recurrence runs over rows in registers: a thread keeps four states of one channel, N / 4 threads hold a channel's states
+// (N: the number of states rounded up to a power of two, the surplus stays zero), and a block of 128 threads walks 512 / N
+// channels of one group through a sequence, or through one chunk of it.  It goes in tiles of a few dozen rows: the
+// elementwise work of a tile (softplus, silu, the products with x) is spread over all threads and goes through shared memory,
+// and so do the sums over a channel's threads.  Neighbouring lanes hold neighbouring channels of the same states, so B and C
+// are read once per warp.
 #pragma once
 #include "seq_common.cuh"
 
@@ -30,7 +33,7 @@ struct ScanParams {
     long long state_stride;
     const int* slots;
     long long n_slots;
-    float* saved;                    // [saved_rows][channels][4 * TPC]: the state before every kScanSave-th row
+    float* saved;                    // per kScanSave rows of a sequence: the state before them (see scan_state_at)
     const void* dout; long long ld_dout;
     void* dx; long long ld_dx;
     void* ddt; long long ld_ddt;
@@ -45,10 +48,11 @@ struct ScanParams {
     long long chunk, dense;          // rows of a chunk, chunks per sequence of a dense batch
     int cut;                         // some sequence has more than one chunk
     int channel_tiles;               // per group
-    float* carry;                    // [chunk number][channels][4 * TPC]: a chunk's own contribution to the state behind it
+    int sum_tiles;                   // channel tiles that have sums of dB and dC of their own, per group
+    float* carry;                    // per chunk: its own contribution to the state (or gradient) behind it
     float* carry_dt;                 // [chunk number][channels]: the sum of dt' over a chunk
-    float* part_bc;                  // [channel_tiles][rows][groups][2][4 * TPC]
-    float* part_a;                   // [chunk number][channels][4 * TPC]
+    float* part_bc;                  // [sum_tiles][rows][groups][2][N]
+    float* part_a;                   // per chunk: its sums of dA
     float* part_d;                   // [chunk number][2][channels]: dD, ddt_bias
     int* status;
 };
@@ -56,19 +60,42 @@ struct ScanParams {
 constexpr int kScanSave = 8;         // rows between two saved states; also the rows of a backward tile
 constexpr int kScanThreads = 128;
 
-template <int TPC>
+constexpr int kScanStates = 4;       // of a thread
+
+template <int N>
 struct ScanShape {
-    static constexpr int kChannels = kScanThreads / TPC;
-    static constexpr int kStates = 4 * TPC;
-    static constexpr int kRows = TPC == 1 ? 8 : TPC == 2 ? 16 : TPC <= 8 ? 32 : TPC == 16 ? 16 : 8;   // rows of a forward tile
+    static constexpr int kPer = N / kScanStates;                          // threads of a channel
+    static constexpr int kChannels = kScanThreads / kPer;
+    static constexpr int kRows = kChannels >= 128 ? 8 : kChannels >= 64 ? 16 : N <= 32 ? 32 : N == 64 ? 16 : 8;   // rows of a forward tile
 };
 
-// Where a block works: channels [c0, c0 + live) of group g, rows [t0, t1) of sequence b.
+// Scratch and saved states: [number][state / 4][channel][state % 4], so that a warp reads and writes 512 bytes in one piece.
+template <int N>
+__device__ __forceinline__ long long scan_state_at(long long number, long long channels, long long c, int n0) {
+    return ((number * (N / 4) + n0 / 4) * channels + c) * 4 + n0 % 4;
+}
+__device__ __forceinline__ void scan_load_states(const float* p, float (&h)[4]) {
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    h[0] = v.x; h[1] = v.y; h[2] = v.z; h[3] = v.w;
+}
+__device__ __forceinline__ void scan_store_states(float* p, const f32x2 (&h)[2]) { *reinterpret_cast<ulonglong2*>(p) = make_ulonglong2(h[0], h[1]); }
+// four neighbouring floats of shared memory as pairs
+__device__ __forceinline__ void scan_load_pairs(const float* p, f32x2 (&v)[2]) {
+    const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(p);
+    v[0] = q.x; v[1] = q.y;
+}
+__device__ __forceinline__ f32x2 exp2_pair(f32x2 e) {
+    float lo, hi;
+    unpack2(e, lo, hi);
+    return pack2(fast_exp2(lo), fast_exp2(hi));
+}
+
+// Where a block works: channels [c0, c0 + live) of a group, a chunk of sequence b.
 struct ScanPlace {
     long long b, c0, number;     // number: of the chunk, over all sequences
     int chunk, group, live, tile;
 };
-template <int TPC>
+template <int CHANNELS>
 __device__ __forceinline__ ScanPlace scan_place(const ScanParams& p) {
     ScanPlace r;
     const long long bid = blockIdx.x;
@@ -80,9 +107,9 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanParams& p) {
     r.chunk = piece.index;
     r.group = ct / p.channel_tiles;
     r.tile = ct - r.group * p.channel_tiles;
-    const int in_group = r.tile * ScanShape<TPC>::kChannels;
+    const int in_group = r.tile * CHANNELS;
     r.c0 = static_cast<long long>(r.group) * p.group_channels + in_group;
-    r.live = min(ScanShape<TPC>::kChannels, p.group_channels - in_group);
+    r.live = min(CHANNELS, p.group_channels - in_group);
     return r;
 }
 // First saved state of a sequence that starts at row `first`: no two sequences overlap, and rows / kScanSave + batch
@@ -96,6 +123,37 @@ __device__ __forceinline__ void scan_load_a(const ScanParams& p, long long c, in
 #pragma unroll
     for (int i = 0; i < 4; ++i) a[i] = live && n0 + i < p.states ? __ldg(p.A + c * p.states + n0 + i) * kLog2e : 0.0f;
 }
+// The caller's state tensors: n_slots x channels x states
+__device__ __forceinline__ void scan_read_state(const ScanParams& p, const float* state, long long slot, long long c, int n0, float (&h)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (n0 + i < p.states) h[i] = state[slot * p.state_stride + c * p.states + n0 + i];
+}
+__device__ __forceinline__ void scan_write_state(const ScanParams& p, float* state, long long slot, long long c, int n0, const f32x2 (&h)[2]) {
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) unpack2(h[i / 2], v[i], v[i + 1]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (n0 + i < p.states) state[slot * p.state_stride + c * p.states + n0 + i] = v[i];
+}
+// The sum of a channel's threads' values, a row of kPer * kRows * kChannels floats [thread][row][channel]; VEC neighbouring channels
+template <int PER, int STRIDE, int VEC>
+__device__ __forceinline__ void scan_sum(const float* p, float (&s)[VEC]) {
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        if (VEC == 2) {
+            const float2 v = *reinterpret_cast<const float2*>(p + q * STRIDE);
+            s[0] += v.x;
+            s[VEC - 1] += v.y;
+        } else {
+            s[0] += p[q * STRIDE];
+        }
+    }
+}
+
+struct ScanYes { static constexpr bool value = true; };
+struct ScanNo { static constexpr bool value = false; };
 
 enum ScanMode { kScanFull = 0, kScanState = 1, kScanAdjoint = 2 };
 
@@ -104,19 +162,24 @@ enum ScanMode { kScanFull = 0, kScanState = 1, kScanAdjoint = 2 };
 //   effect on an incoming state is then exp(A * sum dt').)  Run first when a sequence is cut into chunks, for all chunks but
 //   the last; chunk 0 starts from the caller's state.
 // kScanAdjoint: the same for the gradient, from the last row to the first: q <- exp(dt' A) (q + C dy).
-template <typename T, int TPC, int MODE>
+//
+// VEC neighbouring channels (2 where the rows' alignment allows) are one element of the elementwise work, which is as long as the
+// recurrence itself unless its addresses and checks are kept cheap: a thread's offsets in a tile are computed once, and a full
+// tile is read without checks.
+template <typename T, int N, int MODE, int VEC>
 __global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(const __grid_constant__ ScanParams p) {
-    typedef ScanShape<TPC> S;
-    constexpr int kRows = S::kRows, kCh = S::kChannels, kN = S::kStates;
-    constexpr int kEl = (kRows * kCh + kScanThreads - 1) / kScanThreads;       // elements of a tile per thread
-    constexpr int kBc = (kRows * kN + kScanThreads - 1) / kScanThreads;
-    __shared__ float2 s_dt[kRows][kCh];                  // dt', dt' x   (kScanAdjoint: dt', dy)
-    __shared__ __align__(16) float s_b[kRows][kN];
-    __shared__ __align__(16) float s_c[kRows][kN];
-    __shared__ __align__(16) float s_y[MODE == kScanFull ? kRows : 1][kScanThreads];
-    seq_launch_dependents();
+    typedef ScanShape<N> Shape;
+    typedef SeqVec<T, VEC> raw_t;
+    constexpr int kRows = Shape::kRows, kCh = Shape::kChannels, kPer = Shape::kPer, S = kScanStates, P = S / 2;
+    constexpr int kAcross = kCh / VEC, kStep = kScanThreads / kAcross;                    // threads along a row, rows between a thread's elements
+    constexpr int kEl = (kRows + kStep - 1) / kStep;
+    constexpr int kBcStep = N >= kScanThreads ? 1 : kScanThreads / N, kBc = (kRows + kBcStep - 1) / kBcStep;
+    __shared__ float4 s_dt[kRows][kCh];                  // dt', dt', dt' x, dt' x   (kScanAdjoint: dy for dt' x)
+    __shared__ __align__(16) float s_b[kRows][N];
+    __shared__ __align__(16) float s_c[MODE == kScanFull ? kRows : 1][N];
+    __shared__ __align__(16) float s_y[MODE == kScanFull ? kPer : 1][kRows][kCh];
     seq_grid_wait();
-    const ScanPlace at = scan_place<TPC>(p);
+    const ScanPlace at = scan_place<kCh>(p);
     const SeqRange seq = seq_range(p.offsets, at.b, p.max_len, p.rows, p.status);
     const int tid = threadIdx.x;
     const int chunk = static_cast<int>(p.chunk), last = seq.len > 0 ? (seq.len - 1) / chunk : 0;
@@ -124,176 +187,281 @@ __global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(const __grid_con
     if (MODE == kScanFull && t0 >= seq.len && at.chunk > 0) return;
     if (MODE == kScanState && t1 >= seq.len && at.chunk > 0) return;
     if (MODE == kScanAdjoint && (t0 >= seq.len || at.chunk == 0)) return;
-    const int ch = tid / TPC, n0 = (tid % TPC) * 4;
+    const int ch = tid % kCh, per = tid / kCh, n0 = per * S;
     const bool live = ch < at.live;
     const long long c = at.c0 + (live ? ch : 0);
     const long long slot = MODE != kScanAdjoint && (p.state_in || p.state_out) ? state_slot(p.slots, at.b, p.n_slots, p.status) : -1;
-    float a[4], h[4] = {0.f, 0.f, 0.f, 0.f};
-    scan_load_a(p, c, n0, live, a);
-    const long long carry_row = at.number * p.channels + c;
+    float av[S], hv[S];
+    scan_load_a(p, c, n0, live, av);
+#pragma unroll
+    for (int i = 0; i < S; ++i) hv[i] = 0.0f;
     // The state before chunk 0.  When a sequence is cut, the first launch keeps a copy of it where the last chunk's sum would
     // stand (which nobody needs): in the second launch the last chunk may write state_out over state_in before chunk 0 reads it.
     if (MODE != kScanAdjoint && at.chunk == 0 && p.state_in && slot >= 0 && live) {
-        const long long kept = ((at.number + last) * p.channels + c) * kN + n0;
+        float* kept = p.carry + scan_state_at<N>(at.number + last, p.channels, c, n0);
         if (MODE == kScanFull && p.cut) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) h[i] = p.carry[kept + i];
+            scan_load_states(kept, hv);
         } else {
+            scan_read_state(p, p.state_in, slot, c, n0, hv);
+            if (MODE == kScanState) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (n0 + i < p.states) h[i] = p.state_in[slot * p.state_stride + c * p.states + n0 + i];
-            if (MODE == kScanState) *reinterpret_cast<float4*>(p.carry + kept) = make_float4(h[0], h[1], h[2], h[3]);
+                for (int i = 0; i < S; ++i) kept[i] = hv[i];
+            }
         }
     }
     if (MODE == kScanState && t1 >= seq.len) return;
     if (MODE == kScanFull && at.chunk > 0 && live) {
         for (int k = 0; k < at.chunk; ++k) {
-            const long long row = (at.number - at.chunk + k) * p.channels + c;
-            const float4 add = *reinterpret_cast<const float4*>(p.carry + row * kN + n0);
-            const float sum = k == 0 ? 0.0f : p.carry_dt[row];
-            h[0] = fmaf(h[0], fast_exp2(a[0] * sum), add.x);
-            h[1] = fmaf(h[1], fast_exp2(a[1] * sum), add.y);
-            h[2] = fmaf(h[2], fast_exp2(a[2] * sum), add.z);
-            h[3] = fmaf(h[3], fast_exp2(a[3] * sum), add.w);
+            const long long number = at.number - at.chunk + k;
+            float add[S];
+            scan_load_states(p.carry + scan_state_at<N>(number, p.channels, c, n0), add);
+            const float sum = k == 0 ? 0.0f : p.carry_dt[number * p.channels + c];
+#pragma unroll
+            for (int i = 0; i < S; ++i) hv[i] = fmaf(hv[i], fast_exp2(av[i] * sum), add[i]);
         }
     }
-    f32x2 h01 = pack2(h[0], h[1]), h23 = pack2(h[2], h[3]);
-    const f32x2 a01 = pack2(a[0], a[1]), a23 = pack2(a[2], a[3]);
+    f32x2 h[P], a[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        h[i] = pack2(hv[2 * i], hv[2 * i + 1]);
+        a[i] = pack2(av[2 * i], av[2 * i + 1]);
+    }
 
-    const T* x = static_cast<const T*>(MODE == kScanAdjoint ? p.dout : p.x) + seq.first * (MODE == kScanAdjoint ? p.ld_dout : p.ld_x) + at.c0;
-    const long long ld_x = MODE == kScanAdjoint ? p.ld_dout : p.ld_x;
-    const T* dt = static_cast<const T*>(p.dt) + seq.first * p.ld_dt + at.c0;
-    const bool gated = p.z != nullptr && MODE != kScanState;
-    const T* z = gated ? static_cast<const T*>(p.z) + seq.first * p.ld_z + at.c0 : nullptr;
-    const T* B = static_cast<const T*>(MODE == kScanAdjoint ? p.C : p.B) + seq.first * (MODE == kScanAdjoint ? p.ld_c : p.ld_b) + at.group * p.states;
-    const long long ld_b = MODE == kScanAdjoint ? p.ld_c : p.ld_b;
-    const T* C = static_cast<const T*>(p.C) + seq.first * p.ld_c + at.group * p.states;
+    const long long ld_x = MODE == kScanAdjoint ? p.ld_dout : p.ld_x, ld_b = MODE == kScanAdjoint ? p.ld_c : p.ld_b;
+    float* saved = MODE == kScanFull && p.saved && live ? p.saved + scan_state_at<N>(saved_base(p, at.b, seq.first) + t0 / kScanSave, p.channels, c, n0) : nullptr;
+    const long long save_step = static_cast<long long>(N) * p.channels;
 
-    T rx[kEl], rdt[kEl], rz[kEl], rb[kBc], rc[kBc];
-    auto fetch = [&](int row0) {
+    // This thread's elements of a tile: channels cc .. cc + VEC - 1, rows er, er + kStep, ...; and its values of B and C.  Pointers
+    // move on from tile to tile, offsets inside a tile fit 32 bits (ld <= 2^24).
+    constexpr bool kBack = MODE == kScanAdjoint;
+    const int tiles = (t1 - t0 + kRows - 1) / kRows, first_row = t0 + (kBack ? tiles - 1 : 0) * kRows;
+    const int cc = (tid % kAcross) * VEC, er = tid / kAcross, bn = tid % N, br = tid / N;
+    const bool col_live = cc < at.live;                  // VEC divides the live channels
+    const T* px = static_cast<const T*>(kBack ? p.dout : p.x) + (seq.first + first_row + er) * ld_x + at.c0 + cc;
+    const T* pdt = static_cast<const T*>(p.dt) + (seq.first + first_row + er) * p.ld_dt + at.c0 + cc;
+    const T* pz = static_cast<const T*>(p.z) + (seq.first + first_row + er) * p.ld_z + at.c0 + cc;
+    const T* pb = static_cast<const T*>(kBack ? p.C : p.B) + (seq.first + first_row + br) * ld_b + at.group * p.states + bn;
+    const T* pc = static_cast<const T*>(p.C) + (seq.first + first_row + br) * p.ld_c + at.group * p.states + bn;
+    T* pout = static_cast<T*>(p.out) + (seq.first + first_row + er) * p.ld_out + at.c0 + cc;
+    const uint32_t step_x = static_cast<uint32_t>(kStep * ld_x), step_dt = static_cast<uint32_t>(kStep * p.ld_dt), step_z = static_cast<uint32_t>(kStep * p.ld_z),
+                   step_out = static_cast<uint32_t>(kStep * p.ld_out), step_b = static_cast<uint32_t>(kBcStep * ld_b), step_c = static_cast<uint32_t>(kBcStep * p.ld_c);
+    raw_t rx[kEl], rdt[kEl], rz[kEl];
+    T rb[kBc], rc[kBc];
+    // GATED and CHECKED are compile-time in the loops below: a branch per element would keep the elements from overlapping
+    auto fetch_as = [&](auto gated, auto checked, int left) {
 #pragma unroll
         for (int i = 0; i < kEl; ++i) {
-            const int e = tid + i * kScanThreads, r = e / kCh, cc = e % kCh, t = row0 + r;
-            if (r < kRows && t >= t0 && t < t1 && cc < at.live) {
-                rx[i] = x[t * ld_x + cc];
-                rdt[i] = dt[t * p.ld_dt + cc];
-                if (gated) rz[i] = z[t * p.ld_z + cc];
+            if (!decltype(checked)::value || (er + i * kStep < left && col_live)) {
+                rx[i] = seq_load<T, VEC>(px + i * step_x);
+                rdt[i] = seq_load<T, VEC>(pdt + i * step_dt);
+                if (decltype(gated)::value) rz[i] = seq_load<T, VEC>(pz + i * step_z);
             }
         }
 #pragma unroll
         for (int i = 0; i < kBc; ++i) {
-            const int e = tid + i * kScanThreads, r = e / kN, n = e % kN, t = row0 + r;
-            if (r < kRows && t >= t0 && t < t1 && n < p.states) {
-                rb[i] = B[t * ld_b + n];
-                if (MODE == kScanFull) rc[i] = C[t * p.ld_c + n];
+            if (!decltype(checked)::value || (br + i * kBcStep < left && bn < p.states)) {
+                rb[i] = __ldg(pb + i * step_b);
+                if (MODE == kScanFull) rc[i] = __ldg(pc + i * step_c);
             }
         }
     };
-
-    // every element of a thread belongs to the same channel where 128 is a multiple of the tile's channels
-    float bias[kEl], skip[kEl];
+    const bool gated = p.z != nullptr && MODE != kScanState;
+    const bool whole = at.live == kCh && p.states == N && kRows % kStep == 0 && kRows % kBcStep == 0;
+    auto fetch = [&](int row0) {
+        const int left = min(t1 - row0, kRows);
+        if (whole && left == kRows) {
+            if (gated) fetch_as(ScanYes(), ScanNo(), left);
+            else fetch_as(ScanNo(), ScanNo(), left);
+        } else {
+            if (gated) fetch_as(ScanYes(), ScanYes(), left);
+            else fetch_as(ScanNo(), ScanYes(), left);
+        }
+        const long long move = kBack ? -kRows : kRows;
+        px += move * ld_x;
+        pdt += move * p.ld_dt;
+        if (gated) pz += move * p.ld_z;
+        pb += move * ld_b;
+        pc += move * p.ld_c;
+    };
+    float bias[VEC], skip[VEC];
 #pragma unroll
-    for (int i = 0; i < kEl; ++i) {
-        const int cc = (tid + i * kScanThreads) % kCh;
-        bias[i] = p.dt_bias && cc < at.live ? __ldg(p.dt_bias + at.c0 + cc) : 0.0f;
-        skip[i] = MODE == kScanFull && p.D && cc < at.live ? __ldg(p.D + at.c0 + cc) : 0.0f;
+    for (int v = 0; v < VEC; ++v) {
+        bias[v] = p.dt_bias && col_live ? __ldg(p.dt_bias + at.c0 + cc + v) : 0.0f;
+        skip[v] = MODE == kScanFull && p.D && col_live ? __ldg(p.D + at.c0 + cc + v) : 0.0f;
     }
-    float sum_dt = 0.0f;
-    const int tiles = (t1 - t0 + kRows - 1) / kRows;
-    constexpr bool kBack = MODE == kScanAdjoint;
-    if (tiles > 0) fetch(t0 + (kBack ? tiles - 1 : 0) * kRows);
-    for (int tile = 0; tile < tiles; ++tile) {
-        const int row0 = t0 + (kBack ? tiles - 1 - tile : tile) * kRows;
-        float ex[kEl], ez[kEl];
+    float ex[kEl][VEC], ez[kEl][VEC];
+    auto elementwise_as = [&](auto gated, auto softplus, int left) {
 #pragma unroll
         for (int i = 0; i < kEl; ++i) {
-            const int e = tid + i * kScanThreads, r = e / kCh, cc = e % kCh;
-            const bool there = r < kRows && row0 + r < t1 && cc < at.live;
-            float d = 0.0f, v = 0.0f;
-            ex[i] = 0.0f;
-            ez[i] = 1.0f;
-            if (there) {
-                d = seq_to_float(rdt[i]) + bias[i];
-                if (p.softplus) d = softplus_f(d);
-                ex[i] = seq_to_float(rx[i]);
-                if (gated) {
-                    const float zz = seq_to_float(rz[i]);
-                    ez[i] = zz * sigmoid_f(zz);
+            const int r = er + i * kStep;
+            if (kRows % kStep == 0 || r < kRows) {
+                const bool there = r < left && col_live;
+                float f[VEC], zf[VEC];
+                seq_unpack<T, VEC>(rx[i], ex[i]);
+                seq_unpack<T, VEC>(rdt[i], f);
+                if (decltype(gated)::value) seq_unpack<T, VEC>(rz[i], zf);
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) {
+                    float d = f[v] + bias[v];
+                    if (decltype(softplus)::value) d = softplus_f<T>(d);
+                    ez[i][v] = decltype(gated)::value ? zf[v] * sigmoid_f<T>(zf[v]) : 1.0f;
+                    float w = kBack ? ex[i][v] * ez[i][v] : d * ex[i][v];
+                    if (!there) d = w = 0.0f;
+                    s_dt[r][cc + v] = make_float4(d, d, w, w);
                 }
-                v = MODE == kScanAdjoint ? ex[i] * ez[i] : d * ex[i];
             }
-            if (r < kRows) s_dt[r][cc] = make_float2(d, v);
+        }
+    };
+    float sum_dt = 0.0f;
+    // The recurrence over four rows, and beside it the decays of the four rows behind them and the loads of the four behind
+    // those: decays and inputs do not depend on the state, and the special-function unit (one exponential per state and row, 16 a
+    // cycle on an SM) is the narrowest part, so a warp alone should keep it busy.
+    constexpr int kAhead = 4, kGroups = kRows / kAhead;
+    ulonglong2 dv[2][kAhead];
+    f32x2 bv[2][kAhead][P], cv[2][kAhead][P], w[2][kAhead][P], u[2][kAhead][P];
+    auto load_row = [&](int r, ulonglong2& d, f32x2 (&b)[P]) {
+        const int row = kBack ? kRows - 1 - r : r;
+        d = *reinterpret_cast<const ulonglong2*>(&s_dt[row][ch]);
+        scan_load_pairs(&s_b[row][n0], b);
+    };
+    auto decay_row = [&](int r, const ulonglong2& d, const f32x2 (&b)[P], f32x2 (&ww)[P], f32x2 (&uu)[P], f32x2 (&c4)[P]) {
+        if (MODE == kScanFull) scan_load_pairs(&s_c[r][n0], c4);
+        else sum_dt += __uint_as_float(static_cast<uint32_t>(d.x));
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            ww[i] = exp2_pair(mul2(d.x, a[i]));
+            uu[i] = mul2(d.y, b[i]);
+        }
+    };
+    auto walk_row = [&](int r, const f32x2 (&ww)[P], const f32x2 (&uu)[P], const f32x2 (&c4)[P]) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) h[i] = kBack ? mul2(ww[i], add2(uu[i], h[i])) : fma2(ww[i], h[i], uu[i]);
+        if (MODE == kScanFull) {
+            f32x2 y = mul2(h[0], c4[0]);
+#pragma unroll
+            for (int i = 1; i < P; ++i) y = fma2(h[i], c4[i], y);
+            float lo, hi;
+            unpack2(y, lo, hi);
+            s_y[per][r][ch] = lo + hi;
+        }
+    };
+    if (tiles > 0) fetch(first_row);
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int row0 = kBack ? first_row - tile * kRows : first_row + tile * kRows, left = min(t1 - row0, kRows);
+        if (p.softplus) {
+            if (gated) elementwise_as(ScanYes(), ScanYes(), left);
+            else elementwise_as(ScanNo(), ScanYes(), left);
+        } else {
+            if (gated) elementwise_as(ScanYes(), ScanNo(), left);
+            else elementwise_as(ScanNo(), ScanNo(), left);
         }
 #pragma unroll
         for (int i = 0; i < kBc; ++i) {
-            const int e = tid + i * kScanThreads, r = e / kN, n = e % kN;
-            const bool there = row0 + r < t1 && n < p.states;
-            if (r < kRows) {
-                s_b[r][n] = there ? seq_to_float(rb[i]) : 0.0f;
-                if (MODE == kScanFull) s_c[r][n] = there ? seq_to_float(rc[i]) : 0.0f;
+            const int r = br + i * kBcStep;
+            if (kRows % kBcStep == 0 || r < kRows) {
+                const bool there = r < left && bn < p.states;
+                s_b[r][bn] = there ? seq_to_float(rb[i]) : 0.0f;
+                if (MODE == kScanFull) s_c[r][bn] = there ? seq_to_float(rc[i]) : 0.0f;
             }
         }
         __syncthreads();
-        if (tile + 1 < tiles) fetch(t0 + (kBack ? tiles - 2 - tile : tile + 1) * kRows);
-#pragma unroll 8
-        for (int k = 0; k < kRows; ++k) {
-            const int r = kBack ? kRows - 1 - k : k;
-            if (MODE == kScanFull && r % kScanSave == 0) {
-                if (p.saved != nullptr && row0 + r < t1 && live) {
-                    float4 keep;
-                    unpack2(h01, keep.x, keep.y);
-                    unpack2(h23, keep.z, keep.w);
-                    *reinterpret_cast<float4*>(p.saved + ((saved_base(p, at.b, seq.first) + (row0 + r) / kScanSave) * p.channels + c) * kN + n0) = keep;
-                }
+        if (tile + 1 < tiles) fetch(kBack ? row0 - kRows : row0 + kRows);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) load_row(k, dv[0][k], bv[0][k]);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            load_row(kAhead + k, dv[1][k], bv[1][k]);
+            decay_row(k, dv[0][k], bv[0][k], w[0][k], u[0][k], cv[0][k]);
+        }
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int now = g & 1, next = now ^ 1;
+            if (MODE == kScanFull && g * kAhead % kScanSave == 0 && saved) {
+                if (g * kAhead < left) scan_store_states(saved, h);
+                saved += save_step;
             }
-            const float2 dv = s_dt[r][ch];
-            const ulonglong2 bb = *reinterpret_cast<const ulonglong2*>(&s_b[r][n0]);
-            const f32x2 d2 = pack2(dv.x, dv.x), v2 = pack2(dv.y, dv.y);
-            float e0, e1, e2, e3;
-            unpack2(mul2(d2, a01), e0, e1);
-            unpack2(mul2(d2, a23), e2, e3);
-            const f32x2 w01 = pack2(fast_exp2(e0), fast_exp2(e1)), w23 = pack2(fast_exp2(e2), fast_exp2(e3));
-            if (kBack) {
-                h01 = mul2(w01, fma2(v2, bb.x, h01));
-                h23 = mul2(w23, fma2(v2, bb.y, h23));
-            } else {
-                h01 = fma2(w01, h01, mul2(v2, bb.x));
-                h23 = fma2(w23, h23, mul2(v2, bb.y));
-            }
-            if (MODE == kScanFull) {
-                const ulonglong2 cc = *reinterpret_cast<const ulonglong2*>(&s_c[r][n0]);
-                float lo, hi;
-                unpack2(fma2(h23, cc.y, mul2(h01, cc.x)), lo, hi);
-                s_y[r][tid] = lo + hi;
-            } else {
-                sum_dt += dv.x;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (g + 2 < kGroups) load_row((g + 2) * kAhead + k, dv[now][k], bv[now][k]);
+                if (g + 1 < kGroups) decay_row((g + 1) * kAhead + k, dv[next][k], bv[next][k], w[next][k], u[next][k], cv[next][k]);
+                walk_row(g * kAhead + k, w[now][k], u[now][k], cv[now][k]);
             }
         }
         __syncthreads();
         if (MODE == kScanFull) {
-            T* out = static_cast<T*>(p.out) + (seq.first + row0) * p.ld_out + at.c0;
 #pragma unroll
             for (int i = 0; i < kEl; ++i) {
-                const int e = tid + i * kScanThreads, r = e / kCh, cc = e % kCh;
-                if (r < kRows && row0 + r < t1 && cc < at.live) {
-                    const float y = sum_row<TPC>(&s_y[r][cc * TPC], skip[i] * ex[i]);
-                    out[r * p.ld_out + cc] = seq_from_float<T>(y * ez[i]);
+                const int r = er + i * kStep;
+                if (r < left && col_live) {
+                    float y[VEC];
+#pragma unroll
+                    for (int v = 0; v < VEC; ++v) y[v] = skip[v] * ex[i][v];
+                    scan_sum<kPer, kRows * kCh, VEC>(&s_y[0][r][cc], y);
+#pragma unroll
+                    for (int v = 0; v < VEC; ++v) y[v] *= ez[i][v];
+                    seq_store<T, VEC>(pout + i * step_out, y);
                 }
             }
+            pout += kRows * p.ld_out;
         }
     }
-    unpack2(h01, h[0], h[1]);
-    unpack2(h23, h[2], h[3]);
     if (MODE != kScanFull) {
         if (live) {
-            *reinterpret_cast<float4*>(p.carry + carry_row * kN + n0) = make_float4(h[0], h[1], h[2], h[3]);
-            if (n0 == 0) p.carry_dt[carry_row] = sum_dt;
+            scan_store_states(p.carry + scan_state_at<N>(at.number, p.channels, c, n0), h);
+            if (per == 0) p.carry_dt[at.number * p.channels + c] = sum_dt;
         }
     } else if (p.state_out && slot >= 0 && live && t1 >= seq.len) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n0 + i < p.states) p.state_out[slot * p.state_stride + c * p.states + n0 + i] = h[i];
+        scan_write_state(p, p.state_out, slot, c, n0, h);
     }
+}
+
+// dB and dC are sums over channels, that is, over a warp's lanes (groups of CHANNELS lanes where a warp holds several sets of
+// states).  Four rows' terms of a warp go through shared memory: eight lists of 32 x four states, each summed by four lanes, an
+// eighth of 16-byte loads apart so that no two lanes of a quarter-warp meet in a bank.  (Two other ways were measured on the
+// backward pass of 8192 rows x 2048 channels x 16 states: sums on the tensor cores, with terms cut into two tf32 parts, were
+// bound by the rate of mma.m16n8k8 there, 8 cycles for 64 terms; butterflies of shuffles by their selects.)
+constexpr int kScanSumPitch = 33;      // 16-byte places per list
+template <int CHANNELS>
+__device__ __forceinline__ void scan_sum_lanes(const float4* list, int lane, float* to, long long row_step, int n_states, int rows) {
+    const int v = lane / 4, part = lane % 4, row = v / 2, which = v % 2;       // lists: [row][dB, dC]
+    const float4* from = list + v * kScanSumPitch;
+    float* out = to + row * row_step + which * n_states;
+    const bool there = row < rows;
+    if (CHANNELS == 4) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 q = from[part * 8 + half * 4 + i];
+                s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
+            }
+            if (there) *reinterpret_cast<float4*>(out + (part * 2 + half) * 4) = s;
+        }
+        return;
+    }
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float4 q = from[part * 8 + ((i + 2 * part) & 7)];
+        s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
+    }
+    if (CHANNELS == 8) {
+        if (there) *reinterpret_cast<float4*>(out + part * 4) = s;
+        return;
+    }
+    // lanes with bit 0 go on with the last two states, the others with the first two
+    const bool odd = lane & 1;
+    float x = odd ? s.z : s.x, y = odd ? s.w : s.y;
+    x += __shfl_xor_sync(0xffffffffu, odd ? s.x : s.z, 1);
+    y += __shfl_xor_sync(0xffffffffu, odd ? s.y : s.w, 1);
+    if (CHANNELS == 16) {
+        if (there) *reinterpret_cast<float2*>(out + part / 2 * 4 + 2 * odd) = make_float2(x, y);
+        return;
+    }
+    const bool second = lane & 2;
+    const float mine = (second ? y : x) + __shfl_xor_sync(0xffffffffu, second ? x : y, 2);
+    if (there) out[2 * odd + second] = mine;
 }
 
 // Backward.  With g = dout * silu(z) (or dout), for one channel and state
@@ -304,251 +472,271 @@ __global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(const __grid_con
 // front of the tile, recomputes the tile's states and decays into registers, and then goes back through them.  Sums over
 // states and over the block's channels go through shared memory; sums over blocks are left to scan_bwd_join_kernel, so every
 // sum has a fixed order.
-template <int TPC>
-struct ScanBwdSmem {
-    float4 red[2 * kScanSave][kScanThreads];      // per thread: its channel's share of dB and dC
-    float sum[3][kScanSave][kScanThreads];        // per thread: its states' share of y, sum dlog A2, sum dh B
-    float b[kScanSave][ScanShape<TPC>::kStates];
-    float c[kScanSave][ScanShape<TPC>::kStates];
-    float2 dt[kScanSave][ScanShape<TPC>::kChannels];   // dt', dt' x
-    float g[kScanSave][ScanShape<TPC>::kChannels];
-};
-template <typename T, int TPC>
+template <typename T, int N, int VEC>
 __global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(const __grid_constant__ ScanParams p) {
-    typedef ScanShape<TPC> S;
-    constexpr int kRows = kScanSave, kCh = S::kChannels, kN = S::kStates;
-    constexpr int kEl = (kRows * kCh + kScanThreads - 1) / kScanThreads;
-    constexpr int kBc = (kRows * kN + kScanThreads - 1) / kScanThreads;
-    extern __shared__ __align__(16) unsigned char scan_bwd_smem[];
-    ScanBwdSmem<TPC>& sm = *reinterpret_cast<ScanBwdSmem<TPC>*>(scan_bwd_smem);
-    seq_launch_dependents();
+    typedef ScanShape<N> Shape;
+    typedef SeqVec<T, VEC> raw_t;
+    constexpr int kRows = kScanSave, kCh = Shape::kChannels, kPer = Shape::kPer, S = kScanStates, P = S / 2;
+    constexpr int kAcross = kCh / VEC, kStep = kScanThreads / kAcross;
+    constexpr int kEl = (kRows + kStep - 1) / kStep;
+    constexpr int kBcStep = N >= kScanThreads ? 1 : kScanThreads / N, kBc = (kRows + kBcStep - 1) / kBcStep;
+    constexpr int kSubs = kCh > 32 ? kCh / 32 : 1;         // warps that share their states
+    // dt', dt' x and g, each twice, so that they load as pairs (once where there would be too much of it: N = 4)
+    constexpr bool kTwice = kCh <= 64;
+    __shared__ float4 s_dt[kRows][kTwice ? kCh : kCh / 2];
+    __shared__ float2 s_g[kRows][kTwice ? kCh : kCh / 2];
+    auto dt_at = [&](int r, int c) {
+        if (kTwice) return *reinterpret_cast<const ulonglong2*>(&s_dt[r][c]);
+        const float2 v = reinterpret_cast<const float2*>(&s_dt[r][0])[c];
+        return make_ulonglong2(pack2(v.x, v.x), pack2(v.y, v.y));
+    };
+    auto g_at = [&](int r, int c) {
+        if (kTwice) return *reinterpret_cast<const f32x2*>(&s_g[r][c]);
+        const float v = reinterpret_cast<const float*>(&s_g[r][0])[c];
+        return pack2(v, v);
+    };
+    __shared__ __align__(16) float s_b[kRows][N];
+    __shared__ __align__(16) float s_c[kRows][N];
+    __shared__ float4 s_list[kScanThreads / 32][8][kScanSumPitch];      // see scan_sum_lanes
+    __shared__ __align__(16) float s_sum[3][kPer][kRows][kCh];         // per thread: its states' share of y, sum dlog A2, sum dh B
     seq_grid_wait();
-    const ScanPlace at = scan_place<TPC>(p);
+    const ScanPlace at = scan_place<kCh>(p);
     const SeqRange seq = seq_range(p.offsets, at.b, p.max_len, p.rows, p.status);
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31;
     const int chunk = static_cast<int>(p.chunk), last = seq.len > 0 ? (seq.len - 1) / chunk : 0;
     const int t0 = min(at.chunk, last + 1) * chunk, t1 = min(seq.len, t0 + chunk);
-    const int ch = tid / TPC, n0 = (tid % TPC) * 4;
+    const int ch = tid % kCh, per = tid / kCh, n0 = per * S;
     const bool live = ch < at.live;
     const long long c = at.c0 + (live ? ch : 0);
     const long long slot = p.dstate_in || p.dstate_out ? state_slot(p.slots, at.b, p.n_slots, p.status) : -1;
-    float a[4], h[4];
-    scan_load_a(p, c, n0, live, a);
+    float av[S], qv[S];
+    scan_load_a(p, c, n0, live, av);
     // the gradient that comes from behind the chunk
-    float q[4] = {0.f, 0.f, 0.f, 0.f};
-    if (p.dstate_out && slot >= 0 && live) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n0 + i < p.states) q[i] = __ldg(p.dstate_out + slot * p.state_stride + c * p.states + n0 + i);
-    }
+    for (int i = 0; i < S; ++i) qv[i] = 0.0f;
     if (live) {
+        if (p.dstate_out && slot >= 0) scan_read_state(p, p.dstate_out, slot, c, n0, qv);
         for (int k = last; k > at.chunk; --k) {
-            const long long row = (at.number - at.chunk + k) * p.channels + c;
-            const float4 add = *reinterpret_cast<const float4*>(p.carry + row * kN + n0);
-            const float sum = p.carry_dt[row];
-            q[0] = fmaf(q[0], fast_exp2(a[0] * sum), add.x);
-            q[1] = fmaf(q[1], fast_exp2(a[1] * sum), add.y);
-            q[2] = fmaf(q[2], fast_exp2(a[2] * sum), add.z);
-            q[3] = fmaf(q[3], fast_exp2(a[3] * sum), add.w);
+            const long long number = at.number - at.chunk + k;
+            float add[S];
+            scan_load_states(p.carry + scan_state_at<N>(number, p.channels, c, n0), add);
+            const float sum = p.carry_dt[number * p.channels + c];
+#pragma unroll
+            for (int i = 0; i < S; ++i) qv[i] = fmaf(qv[i], fast_exp2(av[i] * sum), add[i]);
         }
     }
-    f32x2 q01 = pack2(q[0], q[1]), q23 = pack2(q[2], q[3]);
-    const f32x2 a01 = pack2(a[0], a[1]), a23 = pack2(a[2], a[3]);
-    f32x2 da01 = pack2(0.f, 0.f), da23 = pack2(0.f, 0.f);
-
+    f32x2 q[P], a[P], da[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        q[i] = pack2(qv[2 * i], qv[2 * i + 1]);
+        a[i] = pack2(av[2 * i], av[2 * i + 1]);
+        da[i] = pack2(0.f, 0.f);
+    }
     const T* x = static_cast<const T*>(p.x) + seq.first * p.ld_x + at.c0;
     const T* dt = static_cast<const T*>(p.dt) + seq.first * p.ld_dt + at.c0;
     const T* z = p.z ? static_cast<const T*>(p.z) + seq.first * p.ld_z + at.c0 : nullptr;
     const T* dout = static_cast<const T*>(p.dout) + seq.first * p.ld_dout + at.c0;
     const T* B = static_cast<const T*>(p.B) + seq.first * p.ld_b + at.group * p.states;
     const T* C = static_cast<const T*>(p.C) + seq.first * p.ld_c + at.group * p.states;
-    const float* saved = p.saved + (saved_base(p, at.b, seq.first) * p.channels + c) * kN + n0;
+    const float* saved = p.saved + scan_state_at<N>(saved_base(p, at.b, seq.first), p.channels, c, n0);
 
-    T rx[kEl], rdt[kEl], rz[kEl], rg[kEl], rb[kBc], rc[kBc];
-    float4 rh;
+    // this thread's elements of a tile: channels cc .. cc + VEC - 1, rows er, er + kStep, ...; offsets fit 32 bits (ld <= 2^24)
+    const int cc = (tid % kAcross) * VEC, er = tid / kAcross, bn = tid % N, br = tid / N;
+    const bool col_live = cc < at.live;                    // VEC divides the live channels
+    raw_t rx[kEl], rdt[kEl], rz[kEl], rg[kEl];
+    T rb[kBc], rc[kBc];
+    float rh[S];
     auto fetch = [&](int row0) {
+        const T* xt = x + row0 * p.ld_x;
+        const T* dtt = dt + row0 * p.ld_dt;
+        const T* gt = dout + row0 * p.ld_dout;
+        const T* zt = z + row0 * p.ld_z;
+        const T* bt = B + row0 * p.ld_b;
+        const T* ct = C + row0 * p.ld_c;
+        const int left = min(t1 - row0, kRows);
 #pragma unroll
         for (int i = 0; i < kEl; ++i) {
-            const int e = tid + i * kScanThreads, r = e / kCh, cc = e % kCh, t = row0 + r;
-            if (r < kRows && t < t1 && cc < at.live) {
-                rx[i] = x[t * p.ld_x + cc];
-                rdt[i] = dt[t * p.ld_dt + cc];
-                rg[i] = dout[t * p.ld_dout + cc];
-                if (z) rz[i] = z[t * p.ld_z + cc];
+            const int r = er + i * kStep;
+            if (r < left && col_live) {
+                rx[i] = seq_load<T, VEC>(xt + static_cast<uint32_t>(r * p.ld_x + cc));
+                rdt[i] = seq_load<T, VEC>(dtt + static_cast<uint32_t>(r * p.ld_dt + cc));
+                rg[i] = seq_load<T, VEC>(gt + static_cast<uint32_t>(r * p.ld_dout + cc));
+                if (z) rz[i] = seq_load<T, VEC>(zt + static_cast<uint32_t>(r * p.ld_z + cc));
             }
         }
 #pragma unroll
         for (int i = 0; i < kBc; ++i) {
-            const int e = tid + i * kScanThreads, r = e / kN, n = e % kN, t = row0 + r;
-            if (r < kRows && t < t1 && n < p.states) {
-                rb[i] = B[t * p.ld_b + n];
-                rc[i] = C[t * p.ld_c + n];
+            const int r = br + i * kBcStep;
+            if (r < left && bn < p.states) {
+                rb[i] = bt[static_cast<uint32_t>(r * p.ld_b + bn)];
+                rc[i] = ct[static_cast<uint32_t>(r * p.ld_c + bn)];
             }
         }
-        rh = live ? __ldg(reinterpret_cast<const float4*>(saved + (row0 / kRows) * p.channels * kN)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (live) scan_load_states(saved + row0 / kRows * (N * p.channels), rh);
     };
-    const int my_cc = tid % kCh;                           // the channel of all elements of this thread
-    const bool my_live = my_cc < at.live;
-    const float bias = p.dt_bias && my_live ? __ldg(p.dt_bias + at.c0 + my_cc) : 0.0f;
-    const float skip = p.D && my_live ? __ldg(p.D + at.c0 + my_cc) : 0.0f;
-    float sum_d = 0.0f, sum_bias = 0.0f;
+#pragma unroll
+    for (int i = 0; i < S; ++i) rh[i] = 0.0f;
+    float bias[VEC], skip[VEC], sum_d[VEC], sum_bias[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+        bias[v] = p.dt_bias && col_live ? __ldg(p.dt_bias + at.c0 + cc + v) : 0.0f;
+        skip[v] = p.D && col_live ? __ldg(p.D + at.c0 + cc + v) : 0.0f;
+        sum_d[v] = sum_bias[v] = 0.0f;
+    }
+    const long long sum_tile = at.tile * kSubs + (kCh > 32 ? tid % kCh / 32 : 0);
+    const long long bc_step = static_cast<long long>(p.groups) * 2 * N;            // from row to row
+    float* part_bc = p.part_bc + (sum_tile * p.rows + seq.first) * bc_step + at.group * 2 * N + (kCh >= 32 ? n0 : tid / 32 * (32 / kCh) * S);
+    float4* list = &s_list[tid / 32][0][0];
 
     const int tiles = (max(t1 - t0, 0) + kRows - 1) / kRows;
     if (tiles > 0) fetch(t0 + (tiles - 1) * kRows);
     for (int tile = tiles - 1; tile >= 0; --tile) {
-        const int row0 = t0 + tile * kRows;
-        float ex[kEl], ed[kEl], eds[kEl], ez[kEl], ezs[kEl], eo[kEl];   // x, dt', d dt' / d dt, z, sigmoid(z), dout
+        const int row0 = t0 + tile * kRows, left = min(t1 - row0, kRows);
+        // x, dt', d dt' / d dt, z, sigmoid(z), dout, g
+        float ex[kEl][VEC], ed[kEl][VEC], eds[kEl][VEC], ez[kEl][VEC], ezs[kEl][VEC], eo[kEl][VEC], eg[kEl][VEC];
 #pragma unroll
         for (int i = 0; i < kEl; ++i) {
-            const int e = tid + i * kScanThreads, r = e / kCh, cc = e % kCh;
-            const bool there = r < kRows && row0 + r < t1 && cc < at.live;
-            ex[i] = ed[i] = ez[i] = ezs[i] = eo[i] = 0.0f;
-            eds[i] = 1.0f;
-            float g = 0.0f;
-            if (there) {
-                ed[i] = seq_to_float(rdt[i]) + bias;
-                if (p.softplus) ed[i] = softplus_grad_f(ed[i], eds[i]);
-                ex[i] = seq_to_float(rx[i]);
-                eo[i] = g = seq_to_float(rg[i]);
-                if (z) {
-                    ez[i] = seq_to_float(rz[i]);
-                    ezs[i] = sigmoid_f(ez[i]);
-                    g *= ez[i] * ezs[i];
+            const int r = er + i * kStep;
+            if (kRows % kStep == 0 || r < kRows) {
+                const bool there = r < left && col_live;
+                seq_unpack<T, VEC>(rx[i], ex[i]);
+                seq_unpack<T, VEC>(rdt[i], ed[i]);
+                seq_unpack<T, VEC>(rg[i], eo[i]);
+                seq_unpack<T, VEC>(rz[i], ez[i]);
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) {
+                    ed[i][v] += bias[v];
+                    const float soft = softplus_grad_f<T>(ed[i][v], eds[i][v]);
+                    ed[i][v] = p.softplus ? soft : ed[i][v];
+                    eds[i][v] = p.softplus ? eds[i][v] : 1.0f;
+                    ezs[i][v] = sigmoid_f<T>(ez[i][v]);
+                    eg[i][v] = z ? eo[i][v] * (ez[i][v] * ezs[i][v]) : eo[i][v];
+                    float w = ed[i][v] * ex[i][v];
+                    if (!there) ed[i][v] = w = eg[i][v] = 0.0f;
+                    if (kTwice) {
+                        s_dt[r][cc + v] = make_float4(ed[i][v], ed[i][v], w, w);
+                        s_g[r][cc + v] = make_float2(eg[i][v], eg[i][v]);
+                    } else {
+                        reinterpret_cast<float2*>(&s_dt[r][0])[cc + v] = make_float2(ed[i][v], w);
+                        reinterpret_cast<float*>(&s_g[r][0])[cc + v] = eg[i][v];
+                    }
                 }
-            }
-            if (r < kRows) {
-                sm.dt[r][cc] = make_float2(ed[i], ed[i] * ex[i]);
-                sm.g[r][cc] = g;
             }
         }
 #pragma unroll
         for (int i = 0; i < kBc; ++i) {
-            const int e = tid + i * kScanThreads, r = e / kN, n = e % kN;
-            const bool there = row0 + r < t1 && n < p.states;
-            if (r < kRows) {
-                sm.b[r][n] = there ? seq_to_float(rb[i]) : 0.0f;
-                sm.c[r][n] = there ? seq_to_float(rc[i]) : 0.0f;
+            const int r = br + i * kBcStep;
+            if (kRows % kBcStep == 0 || r < kRows) {
+                const bool there = r < left && bn < p.states;
+                s_b[r][bn] = there ? seq_to_float(rb[i]) : 0.0f;
+                s_c[r][bn] = there ? seq_to_float(rc[i]) : 0.0f;
             }
         }
-        f32x2 hs01[kRows + 1], hs23[kRows + 1], w01[kRows], w23[kRows];
-        hs01[0] = pack2(rh.x, rh.y);
-        hs23[0] = pack2(rh.z, rh.w);
+        f32x2 hs[kRows + 1][P], w[kRows][P];
+#pragma unroll
+        for (int i = 0; i < P; ++i) hs[0][i] = pack2(rh[2 * i], rh[2 * i + 1]);
         __syncthreads();
         if (tile > 0) fetch(row0 - kRows);
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            const float2 dv = sm.dt[r][ch];
-            const ulonglong2 bb = *reinterpret_cast<const ulonglong2*>(&sm.b[r][n0]);
-            const f32x2 d2 = pack2(dv.x, dv.x), v2 = pack2(dv.y, dv.y);
-            float e0, e1, e2, e3;
-            unpack2(mul2(d2, a01), e0, e1);
-            unpack2(mul2(d2, a23), e2, e3);
-            w01[r] = pack2(fast_exp2(e0), fast_exp2(e1));
-            w23[r] = pack2(fast_exp2(e2), fast_exp2(e3));
-            hs01[r + 1] = fma2(w01[r], hs01[r], mul2(v2, bb.x));
-            hs23[r + 1] = fma2(w23[r], hs23[r], mul2(v2, bb.y));
+            const ulonglong2 dv = dt_at(r, ch);
+            f32x2 b[P];
+            scan_load_pairs(&s_b[r][n0], b);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                w[r][i] = exp2_pair(mul2(dv.x, a[i]));
+                hs[r + 1][i] = fma2(w[r][i], hs[r][i], mul2(dv.y, b[i]));
+            }
         }
+        f32x2 ta[P];
+#pragma unroll
+        for (int i = 0; i < P; ++i) ta[i] = pack2(0.f, 0.f);
 #pragma unroll
         for (int r = kRows - 1; r >= 0; --r) {
-            const float2 dv = sm.dt[r][ch];
-            const float g = sm.g[r][ch];
-            const ulonglong2 bb = *reinterpret_cast<const ulonglong2*>(&sm.b[r][n0]);
-            const ulonglong2 cc = *reinterpret_cast<const ulonglong2*>(&sm.c[r][n0]);
-            const f32x2 d2 = pack2(dv.x, dv.x), v2 = pack2(dv.y, dv.y), g2 = pack2(g, g);
+            const ulonglong2 dv = dt_at(r, ch);
+            const f32x2 g2 = g_at(r, ch);
+            f32x2 b[P], cv[P], db[P], dc[P], y, du, dl;
+            scan_load_pairs(&s_b[r][n0], b);
+            scan_load_pairs(&s_c[r][n0], cv);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const f32x2 dh = fma2(g2, cv[i], q[i]);
+                q[i] = mul2(w[r][i], dh);
+                const f32x2 dlog = mul2(q[i], hs[r][i]);
+                ta[i] = fma2(dlog, dv.x, ta[i]);
+                y = i == 0 ? mul2(hs[r + 1][i], cv[i]) : fma2(hs[r + 1][i], cv[i], y);
+                du = i == 0 ? mul2(dh, b[i]) : fma2(dh, b[i], du);
+                dl = i == 0 ? mul2(dlog, a[i]) : fma2(dlog, a[i], dl);
+                db[i] = mul2(dh, dv.y);
+                dc[i] = mul2(hs[r + 1][i], g2);
+            }
             float lo, hi;
-            unpack2(fma2(hs23[r + 1], cc.y, mul2(hs01[r + 1], cc.x)), lo, hi);
-            sm.sum[0][r][tid] = lo + hi;
-            const f32x2 dh01 = fma2(g2, cc.x, q01), dh23 = fma2(g2, cc.y, q23);
-            unpack2(fma2(dh23, bb.y, mul2(dh01, bb.x)), lo, hi);
-            sm.sum[2][r][tid] = lo + hi;
-            q01 = mul2(w01[r], dh01);
-            q23 = mul2(w23[r], dh23);
-            const f32x2 l01 = mul2(q01, hs01[r]), l23 = mul2(q23, hs23[r]);
-            unpack2(fma2(l23, a23, mul2(l01, a01)), lo, hi);
-            sm.sum[1][r][tid] = lo + hi;
-            da01 = fma2(l01, d2, da01);
-            da23 = fma2(l23, d2, da23);
-            ulonglong2 keep;
-            keep.x = mul2(dh01, v2);
-            keep.y = mul2(dh23, v2);
-            *reinterpret_cast<ulonglong2*>(&sm.red[2 * r][tid]) = keep;
-            keep.x = mul2(hs01[r + 1], g2);
-            keep.y = mul2(hs23[r + 1], g2);
-            *reinterpret_cast<ulonglong2*>(&sm.red[2 * r + 1][tid]) = keep;
-        }
-        __syncthreads();
-        // dB and dC of the tile: sums over the block's channels.  kParts neighbouring threads share an output of four states.
-        {
-            constexpr int kParts = TPC <= 8 ? 8 / TPC : 1, kOut = 2 * kRows * TPC, kPer = kCh / kParts;
-#pragma unroll
-            for (int o0 = 0; o0 < kOut * kParts; o0 += kScanThreads) {
-                const int o = (o0 + tid) / kParts, part = tid % kParts, rw = o / TPC, qq = o % TPC;
-                float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const float4 v = sm.red[rw][(part + kParts * i) * TPC + qq];
-                    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-                }
-#pragma unroll
-                for (int m = 1; m < kParts; m *= 2) {
-                    s.x += __shfl_xor_sync(0xffffffffu, s.x, m);
-                    s.y += __shfl_xor_sync(0xffffffffu, s.y, m);
-                    s.z += __shfl_xor_sync(0xffffffffu, s.z, m);
-                    s.w += __shfl_xor_sync(0xffffffffu, s.w, m);
-                }
-                const int r = rw >> 1;
-                if (part == 0 && row0 + r < t1) {
-                    const long long row = static_cast<long long>(at.tile) * p.rows + seq.first + row0 + r;
-                    *reinterpret_cast<float4*>(p.part_bc + ((row * p.groups + at.group) * 2 + (rw & 1)) * kN + qq * 4) = s;
-                }
+            unpack2(y, lo, hi);
+            s_sum[0][per][r][ch] = lo + hi;
+            unpack2(dl, lo, hi);
+            s_sum[1][per][r][ch] = lo + hi;
+            unpack2(du, lo, hi);
+            s_sum[2][per][r][ch] = lo + hi;
+            *reinterpret_cast<ulonglong2*>(&list[(r % 4 * 2) * kScanSumPitch + lane]) = make_ulonglong2(db[0], db[1]);
+            *reinterpret_cast<ulonglong2*>(&list[(r % 4 * 2 + 1) * kScanSumPitch + lane]) = make_ulonglong2(dc[0], dc[1]);
+            if (r % 4 == 0) {
+                __syncwarp();
+                scan_sum_lanes<kCh>(list, lane, part_bc + (row0 + r) * bc_step, bc_step, N, left - r);
+                __syncwarp();
             }
         }
+#pragma unroll
+        for (int i = 0; i < P; ++i) da[i] = add2(da[i], ta[i]);           // a tile's sum first: shorter chains of roundings
+        __syncthreads();
 #pragma unroll
         for (int i = 0; i < kEl; ++i) {
-            const int e = tid + i * kScanThreads, r = e / kCh, cc = e % kCh;
-            if (r < kRows && row0 + r < t1 && cc < at.live) {
-                const float y = sum_row<TPC>(&sm.sum[0][r][cc * TPC], skip * ex[i]);
-                const float dlog = sum_row<TPC>(&sm.sum[1][r][cc * TPC], 0.0f), du = sum_row<TPC>(&sm.sum[2][r][cc * TPC], 0.0f);
-                const float g = sm.g[r][cc];
-                const long long row = seq.first + row0 + r, col = at.c0 + cc;
-                static_cast<T*>(p.dx)[row * p.ld_dx + col] = seq_from_float<T>(fmaf(du, ed[i], skip * g));
-                float dd = fmaf(dlog, 0.6931471805599453f, du * ex[i]);
-                dd *= eds[i];
-                static_cast<T*>(p.ddt)[row * p.ld_ddt + col] = seq_from_float<T>(dd);
-                if (z) {
-                    static_cast<T*>(p.dz)[row * p.ld_dz + col] = seq_from_float<T>(eo[i] * y * ezs[i] * fmaf(ez[i], 1.0f - ezs[i], 1.0f));
+            const int r = er + i * kStep;
+            if (r < left && col_live) {
+                float dx[VEC], ddt[VEC], dz[VEC], y[VEC], dl[VEC], du[VEC];
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) {
+                    y[v] = skip[v] * ex[i][v];
+                    dl[v] = du[v] = 0.0f;
                 }
-                sum_d = fmaf(g, ex[i], sum_d);
-                sum_bias += dd;
+                scan_sum<kPer, kRows * kCh, VEC>(&s_sum[1][0][r][cc], dl);
+                scan_sum<kPer, kRows * kCh, VEC>(&s_sum[2][0][r][cc], du);
+                if (z) scan_sum<kPer, kRows * kCh, VEC>(&s_sum[0][0][r][cc], y);
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) {
+                    dx[v] = fmaf(du[v], ed[i][v], skip[v] * eg[i][v]);
+                    ddt[v] = fmaf(dl[v], 0.6931471805599453f, du[v] * ex[i][v]) * eds[i][v];      // a holds A log2(e)
+                    if (z) dz[v] = eo[i][v] * y[v] * ezs[i][v] * fmaf(ez[i][v], 1.0f - ezs[i][v], 1.0f);
+                    sum_d[v] = fmaf(eg[i][v], ex[i][v], sum_d[v]);
+                    sum_bias[v] += ddt[v];
+                }
+                const long long row = seq.first + row0 + r, col = at.c0 + cc;
+                seq_store<T, VEC>(static_cast<T*>(p.dx) + row * p.ld_dx + col, dx);
+                seq_store<T, VEC>(static_cast<T*>(p.ddt) + row * p.ld_ddt + col, ddt);
+                if (z) seq_store<T, VEC>(static_cast<T*>(p.dz) + row * p.ld_dz + col, dz);
             }
         }
     }
-    const long long part = at.number * p.channels;
     if (live) {
-        float v[4];
-        unpack2(da01, v[0], v[1]);
-        unpack2(da23, v[2], v[3]);
-        *reinterpret_cast<float4*>(p.part_a + (part + c) * kN + n0) = make_float4(v[0], v[1], v[2], v[3]);
-        unpack2(q01, q[0], q[1]);
-        unpack2(q23, q[2], q[3]);
-        if (p.dstate_in && slot >= 0 && at.chunk == 0) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (n0 + i < p.states) p.dstate_in[slot * p.state_stride + c * p.states + n0 + i] = q[i];
-        }
+        scan_store_states(p.part_a + scan_state_at<N>(at.number, p.channels, c, n0), da);
+        if (p.dstate_in && slot >= 0 && at.chunk == 0) scan_write_state(p, p.dstate_in, slot, c, n0, q);
     }
     __syncthreads();
-    sm.sum[0][0][tid] = sum_d;
-    sm.sum[1][0][tid] = sum_bias;
+    // per channel, the sums of the kStep threads that shared it
+    float* sums = &s_sum[0][0][0][0];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+        sums[er * kCh + cc + v] = sum_d[v];
+        sums[kStep * kCh + er * kCh + cc + v] = sum_bias[v];
+    }
     __syncthreads();
-    if (tid < kCh && my_live) {
+    if (tid < at.live) {
         float d = 0.0f, v = 0.0f;
 #pragma unroll
-        for (int k = 0; k < TPC; ++k) {
-            d += sm.sum[0][0][tid + k * kCh];
-            v += sm.sum[1][0][tid + k * kCh];
+        for (int k = 0; k < kStep; ++k) {
+            d += sums[k * kCh + tid];
+            v += sums[kStep * kCh + k * kCh + tid];
         }
-        const long long row = 2 * part + at.c0 + tid;
+        const long long row = 2 * at.number * p.channels + at.c0 + tid;
         p.part_d[row] = d;
         p.part_d[row + p.channels] = v;
     }
@@ -569,7 +757,8 @@ __global__ void __launch_bounds__(256) scan_bwd_join_kernel(const __grid_constan
         // rows outside every sequence have no sums
         if (p.offsets != nullptr && (row < __ldg(p.offsets) || row >= __ldg(p.offsets + p.batch))) return;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < p.channel_tiles; ++k) {
+#pragma unroll 8
+        for (int k = 0; k < p.sum_tiles; ++k) {
             const float4 v = __ldg(reinterpret_cast<const float4*>(p.part_bc + k * total + e));
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
@@ -597,8 +786,9 @@ __global__ void __launch_bounds__(256) scan_bwd_join_kernel(const __grid_constan
 #pragma unroll
     for (int k = 1; k < 8; ++k) s += sums[k][lane];
     if (is_a) {
-        const long long c = e / states_pad;
-        const int n = static_cast<int>(e - c * states_pad);
+        // [four states][channel][4], see scan_state_at
+        const long long quad = e / (4 * p.channels), c = (e - quad * 4 * p.channels) / 4;
+        const int n = static_cast<int>(quad * 4 + e % 4);
         if (n < p.states) p.dA[c * p.states + n] = s;
     } else if (e < p.channels) {
         if (p.dD) p.dD[e] = s;
@@ -627,10 +817,10 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const __grid_constant__ 
     if (live && slot >= 0) {
         xv = seq_to_float(static_cast<const T*>(p.x)[b * p.ld_x + mine]);
         d = seq_to_float(static_cast<const T*>(p.dt)[b * p.ld_dt + mine]) + (p.dt_bias ? __ldg(p.dt_bias + mine) : 0.0f);
-        if (p.softplus) d = softplus_f(d);
+        if (p.softplus) d = softplus_f<T>(d);
         if (p.z) {
             const float zz = seq_to_float(static_cast<const T*>(p.z)[b * p.ld_z + mine]);
-            gate = zz * sigmoid_f(zz);
+            gate = zz * sigmoid_f<T>(zz);
         }
         y = p.D ? __ldg(p.D + mine) * xv : 0.0f;
     }

@@ -12,7 +12,8 @@ constexpr int64_t kSeqMaxLen = 1 << 30;
 // Programmatic stream serialization: the launch overlaps the tail of the kernel in front of it in the stream; every kernel
 // of this file waits for that kernel's end before it touches global memory.
 template <typename... Params, typename... Given>
-int launch_seq(void (*kernel)(Params...), int64_t grid_x, int64_t grid_y, int threads, size_t smem, cudaStream_t st, const Given&... given) {
+int launch_seq_cluster(void (*kernel)(Params...), int64_t grid_x, int64_t grid_y, int threads, size_t smem, int cluster, cudaStream_t st,
+                       const Given&... given) {
     if (grid_x > INT_MAX || grid_y > 65535) return fail(TDX_ERR_UNSUPPORTED, "problem too large for one launch");
     cudaLaunchConfig_t lc;
     std::memset(&lc, 0, sizeof lc);
@@ -20,14 +21,21 @@ int launch_seq(void (*kernel)(Params...), int64_t grid_x, int64_t grid_y, int th
     lc.blockDim = dim3(static_cast<unsigned>(threads));
     lc.dynamicSmemBytes = smem;
     lc.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     lc.attrs = attr;
-    lc.numAttrs = 1;
+    lc.numAttrs = cluster > 1 ? 2 : 1;
     TDX_CUDA(cudaLaunchKernelEx(&lc, kernel, static_cast<Params>(given)...));
     g_launches.fetch_add(1);
     return TDX_OK;
+}
+template <typename... Params, typename... Given>
+int launch_seq(void (*kernel)(Params...), int64_t grid_x, int64_t grid_y, int threads, size_t smem, cudaStream_t st, const Given&... given) {
+    return launch_seq_cluster(kernel, grid_x, grid_y, threads, smem, 1, st, given...);
 }
 
 bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
@@ -37,6 +45,7 @@ int64_t elem_bytes(int dtype) { return dtype == TDX_F32 ? 4 : 2; }
 int check_tensor(const char* name, const void* p, bool needed, size_t align, int64_t ld = 0, int64_t width = 0) {
     if (p == nullptr) return needed ? fail(TDX_ERR_INVALID_ARG, "%s is NULL", name) : TDX_OK;
     if (misaligned(p, align)) return fail(TDX_ERR_ALIGNMENT, "%s is not aligned to its elements", name);
+    if (ld > (1 << 24)) return fail(TDX_ERR_UNSUPPORTED, "ld_%s = %lld is above 2^24", name, (long long)ld);
     if (ld < width) return fail(TDX_ERR_INVALID_ARG, "ld_%s = %lld is less than the row's %lld elements", name, (long long)ld, (long long)width);
     return TDX_OK;
 }
@@ -178,8 +187,13 @@ int launch_conv1d(ConvPass pass, tdx::Conv1dParams& p, cudaStream_t st) {
     const int64_t piece = tdx::kConvRuns * (pass == kConvForward ? tdx::kConvRows : tdx::kConvBwdRows);
     p.dense = conv_dense_pieces(p.max_len, piece);
     const int64_t grid = tdx::seq_pieces(p.offsets != nullptr, p.batch, p.rows, p.dense, piece) * p.channel_tiles;
-    if (pass == kConvForward) return launch_seq(tdx::conv1d_fwd_kernel<T, VEC, KW>, grid, 1, 128, 0, st, p);
-    return launch_seq(tdx::conv1d_bwd_kernel<T, VEC, KW>, grid, 1, 128, 0, st, p);
+    if constexpr (sizeof(T) == 4 || VEC != 4) {
+        if (pass == kConvForward) return launch_seq(tdx::conv1d_fwd_kernel<T, VEC, KW>, grid, 1, 128, 0, st, p);
+    }
+    if constexpr (sizeof(T) == 4 || VEC != 8) {
+        if (pass == kConvBackward) return launch_seq(tdx::conv1d_bwd_kernel<T, VEC, KW>, grid, 1, 128, 0, st, p);
+    }
+    return fail(TDX_ERR_UNSUPPORTED, "no kernel for this access width");
 }
 template <typename T, int VEC>
 int launch_conv1d_width(ConvPass pass, tdx::Conv1dParams& p, cudaStream_t st) {
@@ -206,10 +220,10 @@ int run_conv1d(const tdx_conv1d_args* a, ConvPass pass, tdx::Conv1dParams& p, cu
 // ------------------------------------------------------------------ selective scan
 enum ScanPass { kScanForwardPass, kScanBackwardPass, kScanStepPass };
 
-int scan_threads_per_channel(int states) {
-    int tpc = 1;
-    while (4 * tpc < states) tpc *= 2;
-    return tpc;
+int scan_padded_states(int states) {
+    int n = 4;
+    while (n < states) n *= 2;
+    return n;
 }
 
 int check_scan(const tdx_scan_args* a, ScanPass pass, tdx::ScanParams* p, bool sizes_only = false) {
@@ -271,18 +285,18 @@ int check_scan(const tdx_scan_args* a, ScanPass pass, tdx::ScanParams* p, bool s
 
 size_t scan_saved_bytes(const tdx::ScanParams& p) {
     const int64_t n = tdx::seq_pieces(p.offsets != nullptr, p.batch, p.rows, ceil_div(p.max_len, tdx::kScanSave), tdx::kScanSave);
-    return static_cast<size_t>(n) * p.channels * 4 * scan_threads_per_channel(p.states) * sizeof(float);
+    return static_cast<size_t>(n) * p.channels * scan_padded_states(p.states) * sizeof(float);
 }
 
-// Cuts sequences into chunks when the channels and sequences alone do not give every SM a block; a cut costs a second
-// look at the inputs and a second exponential per state.
+// How a scan is spread over the SMs: sequences are cut into chunks when channels and sequences alone do not give every SM a
+// block; a cut costs a second look at the inputs and a second exponential per state.
 void plan_scan(tdx::ScanParams* p, int sm_count) {
-    const int tpc = scan_threads_per_channel(p->states), per_block = tdx::kScanThreads / tpc;
-    p->channel_tiles = static_cast<int>(ceil_div(p->group_channels, per_block));
-    const int64_t tiles = std::max<int64_t>(1, static_cast<int64_t>(p->channel_tiles) * p->groups);
+    const int n = scan_padded_states(p->states);
     // sequences that run side by side: packed ones of uneven length count by their rows
     const int64_t longest = std::max<int64_t>(1, std::min(p->max_len, p->rows));
     const int64_t side = p->offsets ? std::max<int64_t>(1, p->rows / longest) : std::max<int64_t>(1, p->batch);
+    p->channel_tiles = static_cast<int>(ceil_div(p->group_channels, tdx::kScanThreads * 4 / n));
+    const int64_t tiles = std::max<int64_t>(1, static_cast<int64_t>(p->channel_tiles) * p->groups);
     p->chunk = ceil_div(longest, 32) * 32;
     if (tiles * side < sm_count) {
         const int64_t want = ceil_div(2 * sm_count, tiles);                // chunks of all sequences together
@@ -294,16 +308,19 @@ void plan_scan(tdx::ScanParams* p, int sm_count) {
 }
 int64_t scan_numbers(const tdx::ScanParams& p) { return tdx::seq_pieces(p.offsets != nullptr, p.batch, p.rows, p.dense, p.chunk); }
 
+int64_t scan_sum_tiles(const tdx::ScanParams& p) { return ceil_div(p.group_channels, 128) * 4; }
+
 struct ScanWorkspace { size_t carry, carry_dt, part_bc, part_a, part_d, total; };
 ScanWorkspace scan_workspace(const tdx::ScanParams& p, bool back) {
     const size_t numbers = static_cast<size_t>(scan_numbers(p)), channels = static_cast<size_t>(p.channels),
-                 pad = 4 * static_cast<size_t>(scan_threads_per_channel(p.states));
+                 pad = static_cast<size_t>(scan_padded_states(p.states));
     ScanWorkspace w;
     size_t at = 0;
     auto take = [&](size_t floats) { const size_t here = at; at += round_256(floats * sizeof(float)); return here; };
     w.carry = take(p.cut ? numbers * channels * pad : 0);
     w.carry_dt = take(p.cut ? numbers * channels : 0);
-    w.part_bc = take(back ? static_cast<size_t>(p.channel_tiles) * p.rows * p.groups * 2 * pad : 0);
+    // blocks of more than 32 channels have sums per 32
+    w.part_bc = take(back ? static_cast<size_t>(std::max<int64_t>(p.channel_tiles, scan_sum_tiles(p))) * p.rows * p.groups * 2 * pad : 0);
     w.part_a = take(back ? numbers * channels * pad : 0);
     w.part_d = take(back ? numbers * channels * 2 : 0);
     w.total = at;
@@ -318,71 +335,109 @@ void place_scan(tdx::ScanParams* p, const ScanWorkspace& w, void* workspace) {
     p->part_d = reinterpret_cast<float*>(base + w.part_d);
 }
 
-template <typename T, int TPC>
-int launch_scan(ScanPass pass, tdx::ScanParams& p, cudaStream_t st) {
+// Neighbouring channels per access: 2 where every row of every activation of the call starts at a multiple of two elements.
+int scan_vector(const tdx_scan_args* a, const tdx::ScanParams& p, bool back) {
+    const int64_t el = elem_bytes(a->dtype);
+    Widest w(2 * el);
+    w.stride(p.group_channels, el);
+    w.ptr(p.x); w.stride(p.ld_x, el);
+    w.ptr(p.dt); w.stride(p.ld_dt, el);
+    if (p.z) { w.ptr(p.z); w.stride(p.ld_z, el); }
+    if (back) {
+        w.ptr(p.dout); w.stride(p.ld_dout, el);
+        w.ptr(p.dx); w.stride(p.ld_dx, el);
+        w.ptr(p.ddt); w.stride(p.ld_ddt, el);
+        if (p.z) { w.ptr(p.dz); w.stride(p.ld_dz, el); }
+    } else {
+        w.ptr(p.out); w.stride(p.ld_out, el);
+    }
+    return w.bytes == 2 * el ? 2 : 1;
+}
+
+template <typename T, int N, int VEC>
+int launch_scan_passes(ScanPass pass, tdx::ScanParams& p, cudaStream_t st) {
+    typedef tdx::ScanShape<N> Shape;
+    const int64_t numbers = scan_numbers(p), grid = numbers * p.channel_tiles * p.groups;
+    constexpr int kThreads = tdx::kScanThreads;
+    if (pass == kScanForwardPass) {
+        if (p.cut) TDX_TRY(launch_seq(tdx::scan_fwd_kernel<T, N, tdx::kScanState, VEC>, grid, 1, kThreads, 0, st, p));
+        return launch_seq(tdx::scan_fwd_kernel<T, N, tdx::kScanFull, VEC>, grid, 1, kThreads, 0, st, p);
+    }
+    p.sum_tiles = p.channel_tiles * (Shape::kChannels > 32 ? Shape::kChannels / 32 : 1);
+    if (p.cut) TDX_TRY(launch_seq(tdx::scan_fwd_kernel<T, N, tdx::kScanAdjoint, VEC>, grid, 1, kThreads, 0, st, p));
+    TDX_TRY(launch_seq(tdx::scan_bwd_kernel<T, N, VEC>, grid, 1, kThreads, 0, st, p));
+    const int64_t bc_blocks = ceil_div(p.rows * p.groups * 2 * N / 4, 256), a_blocks = ceil_div(p.channels * N, 32), d_blocks = ceil_div(2 * p.channels, 32);
+    return launch_seq(tdx::scan_bwd_join_kernel<T>, bc_blocks + a_blocks + d_blocks, 1, 256, 0, st, p, N, static_cast<long long>(bc_blocks),
+                      static_cast<long long>(a_blocks), static_cast<long long>(numbers));
+}
+template <typename T, int N>
+int launch_scan(ScanPass pass, int vec, tdx::ScanParams& p, cudaStream_t st) {
     if (pass == kScanStepPass) {
         p.channel_tiles = static_cast<int>(ceil_div(p.channels, 32));
         const int64_t warps = p.batch * p.channel_tiles;
-        const bool vec4 = p.states == 4 * TPC && !misaligned(p.state_in, 16) && !misaligned(p.state_out, 16) && !misaligned(p.A, 16) &&
-                          p.state_stride % 4 == 0;
-        return vec4 ? launch_seq(tdx::scan_step_kernel<T, TPC, true>, ceil_div(warps, 4), 1, 128, 0, st, p)
-                    : launch_seq(tdx::scan_step_kernel<T, TPC, false>, ceil_div(warps, 4), 1, 128, 0, st, p);
+        const bool vec4 = p.states == N && !misaligned(p.state_in, 16) && !misaligned(p.state_out, 16) && !misaligned(p.A, 16) && p.state_stride % 4 == 0;
+        return vec4 ? launch_seq(tdx::scan_step_kernel<T, N / 4, true>, ceil_div(warps, 4), 1, 128, 0, st, p)
+                    : launch_seq(tdx::scan_step_kernel<T, N / 4, false>, ceil_div(warps, 4), 1, 128, 0, st, p);
     }
-    const int64_t numbers = scan_numbers(p), grid = numbers * p.channel_tiles * p.groups;
-    if (pass == kScanForwardPass) {
-        if (p.cut) TDX_TRY(launch_seq(tdx::scan_fwd_kernel<T, TPC, tdx::kScanState>, grid, 1, tdx::kScanThreads, 0, st, p));
-        return launch_seq(tdx::scan_fwd_kernel<T, TPC, tdx::kScanFull>, grid, 1, tdx::kScanThreads, 0, st, p);
-    }
-    if (p.cut) TDX_TRY(launch_seq(tdx::scan_fwd_kernel<T, TPC, tdx::kScanAdjoint>, grid, 1, tdx::kScanThreads, 0, st, p));
-    constexpr size_t smem = sizeof(tdx::ScanBwdSmem<TPC>);
-    if (smem > 48 * 1024) {
-        // per device; cheap enough next to a backward pass to be set on every call
-        TDX_CUDA(cudaFuncSetAttribute(tdx::scan_bwd_kernel<T, TPC>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    }
-    TDX_TRY(launch_seq(tdx::scan_bwd_kernel<T, TPC>, grid, 1, tdx::kScanThreads, smem, st, p));
-    const int64_t bc_blocks = ceil_div(p.rows * p.groups * 2 * 4 * TPC / 4, 256), a_blocks = ceil_div(p.channels * 4 * TPC, 32),
-                  d_blocks = ceil_div(2 * p.channels, 32);
-    return launch_seq(tdx::scan_bwd_join_kernel<T>, bc_blocks + a_blocks + d_blocks, 1, 256, 0, st, p, 4 * TPC, static_cast<long long>(bc_blocks),
-                      static_cast<long long>(a_blocks), static_cast<long long>(numbers));
+    return vec == 2 ? launch_scan_passes<T, N, 2>(pass, p, st) : launch_scan_passes<T, N, 1>(pass, p, st);
 }
 template <typename T>
-int launch_scan_states(ScanPass pass, tdx::ScanParams& p, cudaStream_t st) {
-    switch (scan_threads_per_channel(p.states)) {
-        case 1: return launch_scan<T, 1>(pass, p, st);
-        case 2: return launch_scan<T, 2>(pass, p, st);
-        case 4: return launch_scan<T, 4>(pass, p, st);
-        case 8: return launch_scan<T, 8>(pass, p, st);
-        case 16: return launch_scan<T, 16>(pass, p, st);
-        default: return launch_scan<T, 32>(pass, p, st);
+int launch_scan_states(ScanPass pass, int vec, tdx::ScanParams& p, cudaStream_t st) {
+    switch (scan_padded_states(p.states)) {
+        case 4: return launch_scan<T, 4>(pass, vec, p, st);
+        case 8: return launch_scan<T, 8>(pass, vec, p, st);
+        case 16: return launch_scan<T, 16>(pass, vec, p, st);
+        case 32: return launch_scan<T, 32>(pass, vec, p, st);
+        case 64: return launch_scan<T, 64>(pass, vec, p, st);
+        default: return launch_scan<T, 128>(pass, vec, p, st);
     }
 }
 int run_scan(const tdx_scan_args* a, ScanPass pass, tdx::ScanParams& p, DeviceCtx* ctx, void* stream) {
     p.status = ctx->status_ptr;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return a->dtype == TDX_F32 ? launch_scan_states<float>(pass, p, st) : launch_scan_states<__nv_bfloat16>(pass, p, st);
+    const int vec = pass == kScanStepPass ? 1 : scan_vector(a, p, pass == kScanBackwardPass);
+    return a->dtype == TDX_F32 ? launch_scan_states<float>(pass, vec, p, st) : launch_scan_states<__nv_bfloat16>(pass, vec, p, st);
 }
 
 // ------------------------------------------------------------------ 4-bit weights
+template <typename T, int WORDS, int BLOCKS>
+int launch_w4_staged(tdx::W4Params p, int warps, cudaStream_t st) {
+    p.per = static_cast<int>(ceil_div(p.steps, warps));
+    const size_t smem = tdx::kW4RingBytes * 32 * warps + tdx::w4_x_bytes<T>(p.steps, p.M) + 8 * static_cast<size_t>(tdx::kW4Rows * BLOCKS) * (p.groups + 1);
+    if (smem > 48 * 1024)
+        TDX_CUDA(cudaFuncSetAttribute(tdx::w4_staged_kernel<T, WORDS, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    return launch_seq(tdx::w4_staged_kernel<T, WORDS, BLOCKS>, ceil_div(p.N, tdx::kW4Rows * BLOCKS), 1, 32 * warps, smem, st, p);
+}
+template <typename T, int WORDS, int TILES>
+int launch_w4_direct(const tdx::W4Params& p, cudaStream_t st) {
+    return launch_seq(tdx::w4_direct_kernel<T, WORDS, TILES>, ceil_div(p.N, 16), ceil_div(p.M, TILES * tdx::W4Columns<T>::kRows), 256, 0, st, p);
+}
 template <typename T, int WORDS>
-int launch_w4_tiles(const tdx::W4Params& p, cudaStream_t st) {
+int launch_w4_tiles(tdx::W4Params p, int sm_count, cudaStream_t st) {
     constexpr int kRows = tdx::W4Columns<T>::kRows;
-    const int64_t blocks = ceil_div(p.N, 16);
-    const int tiles = p.M <= kRows ? 1 : p.M <= 2 * kRows ? 2 : 4;
-    const int64_t y = std::min<int64_t>(ceil_div(p.M, static_cast<int64_t>(tiles) * kRows), 65536);
-    if (tiles == 1) return launch_seq(tdx::w4_mma_kernel<T, WORDS, 1>, blocks, y, 256, 0, st, p);
-    if (tiles == 2) return launch_seq(tdx::w4_mma_kernel<T, WORDS, 2>, blocks, y, 256, 0, st, p);
-    return launch_seq(tdx::w4_mma_kernel<T, WORDS, 4>, blocks, y, 256, 0, st, p);
+    p.steps = static_cast<int>(ceil_div(p.K, tdx::kW4Step));
+    p.groups = static_cast<int>(p.K / p.group);
+    // Sixteen warps a block: eight took 6.7 us instead of 4.7 for one token and 4096 x 4096 weights.  Two sets of 16 rows a block
+    // save a layout of x, but halve the blocks: 13.5 instead of 15.4 us for 8192 x 8192 (512 sets), 7.0 instead of 4.7 for
+    // 4096 x 4096 (256), so they are taken when one set each would need a second wave of two blocks per SM.
+    constexpr int kWarps = 16;
+    if (p.M <= kRows && tdx::w4_x_bytes<T>(p.steps, p.M) <= 64 * 1024)
+        return ceil_div(p.N, tdx::kW4Rows) > 2 * sm_count ? launch_w4_staged<T, WORDS, 2>(p, kWarps, st) : launch_w4_staged<T, WORDS, 1>(p, kWarps, st);
+    if (p.M <= kRows) return launch_w4_direct<T, WORDS, 1>(p, st);
+    if (p.M <= 2 * kRows) return launch_w4_direct<T, WORDS, 2>(p, st);
+    if (p.M <= 3 * kRows) return launch_w4_direct<T, WORDS, 3>(p, st);
+    return launch_w4_direct<T, WORDS, 4>(p, st);
 }
 template <typename T>
-int launch_w4(const tdx::W4Params& p, cudaStream_t st) {
+int launch_w4(const tdx::W4Params& p, int sm_count, cudaStream_t st) {
     // the tensor-core kernel reads 4, 8 or 16 bytes of a weight row and 16 bytes of a row of x at a time
     const bool fast = (p.group == 32 || p.group == 64 || p.group == 128) && p.K % p.group == 0 && !misaligned(p.weight, p.group / 8) &&
                       !misaligned(p.x, 16) && (p.M == 1 || p.ld_x * static_cast<int64_t>(sizeof(T)) % 16 == 0) && p.M <= 65535LL * 8;
     if (!fast) return launch_seq(tdx::w4_generic_kernel<T>, ceil_div(p.N, 4), std::min<int64_t>(ceil_div(p.M, 4), 1024), 128, 0, st, p);
     switch (p.group) {
-        case 32: return launch_w4_tiles<T, 1>(p, st);
-        case 64: return launch_w4_tiles<T, 2>(p, st);
-        default: return launch_w4_tiles<T, 4>(p, st);
+        case 32: return launch_w4_tiles<T, 1>(p, sm_count, st);
+        case 64: return launch_w4_tiles<T, 2>(p, sm_count, st);
+        default: return launch_w4_tiles<T, 4>(p, sm_count, st);
     }
 }
 
@@ -522,7 +577,7 @@ int tdx_gemm_w4(const tdx_w4_args* args, void* stream) {
     p.M = a.M; p.N = a.N; p.K = a.K; p.group = a.group_size;
     p.x = a.x; p.ld_x = a.ld_x; p.weight = a.weight; p.scales = a.scales; p.zeros = a.zeros; p.y = a.y; p.ld_y = a.ld_y;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return a.dtype == TDX_F32 ? launch_w4<float>(p, st) : launch_w4<__nv_bfloat16>(p, st);
+    return a.dtype == TDX_F32 ? launch_w4<float>(p, ctx->sm_count, st) : launch_w4<__nv_bfloat16>(p, ctx->sm_count, st);
 }
 
 int tdx_w4_quantize(int64_t N, int64_t K, int group_size, int dtype, const void* w, int64_t ld_w, uint8_t* weight, void* scales,

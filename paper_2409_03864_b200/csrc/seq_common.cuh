@@ -65,25 +65,30 @@ __device__ __forceinline__ float fast_rcp(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float sigmoid_f(float v) { return fast_rcp(1.0f + expf(-v)); }
-// log(1 + exp(v)) = max(v, 0) + log1p(u), u = exp(-|v|) in (0, 1], and log1p(u) = 2 atanh(s), s = u / (2 + u) <= 1/3:
-// no cancellation for any v, so the result keeps its relative accuracy where it is tiny.  atanh(s) / s is a polynomial of
-// degree 4 in s^2, fitted by least squares in relative error over [0, 1/9] (7.6e-9 with these coefficients).
-__device__ __forceinline__ float log1p_unit(float u) {
-    const float s = u * fast_rcp(2.0f + u), q = s * s;
-    float p = fmaf(q, 0.14080727f, 0.13982172f);
-    p = fmaf(q, p, 0.20012326f);
-    p = fmaf(q, p, 0.3333316f);
+// exp(v).  fp32 activations get expf; behind bf16 ones (2^-9) the rounding of v * log2(e), up to |v| * 2^-24, does not show.
+template <typename T>
+__device__ __forceinline__ float seq_exp(float v) { return sizeof(T) == 4 ? expf(v) : fast_exp2(v * kLog2e); }
+template <typename T>
+__device__ __forceinline__ float sigmoid_f(float v) { return fast_rcp(1.0f + seq_exp<T>(-v)); }
+// log(1 + exp(v)) = max(v, 0) + log1p(u), u = exp(-|v|) in (0, 1], and log1p(u) = 2 atanh(r / 2), r = 2 u / (2 + u) <= 2/3: no
+// cancellation for any v, so the result keeps its relative accuracy where it is tiny.  2 atanh(r / 2) / r is a polynomial of
+// degree 4 in r^2, fitted by least squares in relative error (7.6e-9 with these coefficients).
+__device__ __forceinline__ float softplus_from_exp(float v, float u) {
+    const float r = u * fast_rcp(fmaf(u, 0.5f, 1.0f)), q = r * r;
+    float p = fmaf(q, 0.14080727f / 256.0f, 0.13982172f / 64.0f);
+    p = fmaf(q, p, 0.20012326f / 16.0f);
+    p = fmaf(q, p, 0.3333316f / 4.0f);
     p = fmaf(q, p, 1.0f);
-    return 2.0f * s * p;
+    return fmaf(r, p, fmaxf(v, 0.0f));
 }
-__device__ __forceinline__ float softplus_f(float v) { return fmaxf(v, 0.0f) + log1p_unit(expf(-fabsf(v))); }
-
+template <typename T>
+__device__ __forceinline__ float softplus_f(float v) { return softplus_from_exp(v, seq_exp<T>(-fabsf(v))); }
 // the same with its derivative, the sigmoid of v, from the same exponential
+template <typename T>
 __device__ __forceinline__ float softplus_grad_f(float v, float& grad) {
-    const float u = expf(-fabsf(v));
+    const float u = seq_exp<T>(-fabsf(v));
     grad = (v >= 0.0f ? 1.0f : u) * fast_rcp(1.0f + u);
-    return fmaxf(v, 0.0f) + log1p_unit(u);
+    return softplus_from_exp(v, u);
 }
 // sum of N consecutive floats of shared memory, in ascending order (16-byte loads where N allows)
 template <int N>
