@@ -31,12 +31,15 @@ struct Conv1dParams {
     float* partial;          // [pieces][channels][width + 1]
     long long dense;         // pieces per sequence of a dense batch
     int channel_tiles;
+    int weight_aligned;      // to 16 bytes
     int* status;
 };
 
-constexpr int kConvRows = 16;        // rows of a run in the forward kernel
-constexpr int kConvBwdRows = 32;     // rows of a run in the backward kernel
+constexpr int kConvRows = 32;        // rows of a run in the forward kernel
+constexpr int kConvBwdRows = 64;     // rows of a run in the backward kernel
 constexpr int kConvRuns = 4;         // runs (warps) of a block, one after the other in time
+constexpr int kConvChunk = 16;       // rows that a thread loads at a time, forward
+constexpr int kConvBwdChunk = 4;     // and backward (of x and dy)
 
 template <typename T, int VEC>
 __device__ __forceinline__ void conv_zero(float (&f)[VEC]) {
@@ -74,8 +77,13 @@ __device__ __forceinline__ void conv_load_weights(const Conv1dParams& p, long lo
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
         const float* wp = p.weight + (c + i) * p.width - (KW - p.width);
+        if (KW == 4 && p.weight_aligned) {
+            const float4 v = __ldg(reinterpret_cast<const float4*>(wp));
+            w[0][i] = v.x; w[1][i] = v.y; w[KW - 2][i] = v.z; w[KW - 1][i] = v.w;
+        } else {
 #pragma unroll
-        for (int k = 0; k < KW; ++k) w[k][i] = conv_tap<KW>(k, p.width) ? __ldg(wp + k) : 0.0f;
+            for (int k = 0; k < KW; ++k) w[k][i] = conv_tap<KW>(k, p.width) ? __ldg(wp + k) : 0.0f;
+        }
         bias[i] = p.bias ? __ldg(p.bias + c + i) : 0.0f;
     }
 }
@@ -85,7 +93,7 @@ __device__ __forceinline__ void conv_load_weights(const Conv1dParams& p, long lo
 // The thread that reads the state (run 0) is also the one that writes the state after the sequence, so state_out may be
 // state_in.
 template <typename T, int VEC, int KW>
-__global__ void __launch_bounds__(128) conv1d_fwd_kernel(const __grid_constant__ Conv1dParams p) {
+__global__ void __launch_bounds__(128, KW <= 4 ? 5 : 2) conv1d_fwd_kernel(const __grid_constant__ Conv1dParams p) {
     seq_grid_wait();
     const long long bid = blockIdx.x;
     const int ct = static_cast<int>(bid % p.channel_tiles);
@@ -112,15 +120,15 @@ __global__ void __launch_bounds__(128) conv1d_fwd_kernel(const __grid_constant__
     const int rows = min(kConvRows, seq.len - t0);
     T* y = static_cast<T*>(p.y) + (seq.first + t0) * p.ld_y + c;
     const T* xr = x + t0 * p.ld_x;
+    // A chunk of rows: all its loads, then its sums, so that the loads are in flight together.  Whole chunks go without checks.
+    auto chunk = [&](auto checked, auto silu, int r0) {
+        SeqVec<T, VEC> raw[kConvChunk];
 #pragma unroll
-    for (int half = 0; half < kConvRows; half += 8) {
-        SeqVec<T, VEC> raw[8];
+        for (int r = 0; r < kConvChunk; ++r)
+            if (!decltype(checked)::value || r0 + r < rows) raw[r] = seq_load<T, VEC>(xr + (r0 + r) * p.ld_x);
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
-            if (half + r < rows) raw[r] = seq_load<T, VEC>(xr + (half + r) * p.ld_x);
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            if (half + r < rows) {
+        for (int r = 0; r < kConvChunk; ++r) {
+            if (!decltype(checked)::value || r0 + r < rows) {
                 float now[VEC], out[VEC];
                 seq_unpack<T, VEC>(raw[r], now);
 #pragma unroll
@@ -130,15 +138,22 @@ __global__ void __launch_bounds__(128) conv1d_fwd_kernel(const __grid_constant__
                     for (int k = 0; k < KW - 1; ++k)
                         if (conv_tap<KW>(k, p.width)) acc = fmaf(w[k][i], win[k][i], acc);
                     acc = fmaf(w[KW - 1][i], now[i], acc);
-                    out[i] = p.silu ? acc * sigmoid_f<T>(acc) : acc;
+                    out[i] = decltype(silu)::value ? acc * sigmoid_f<T>(acc) : acc;
 #pragma unroll
                     for (int k = 0; k + 1 < KW - 1; ++k) win[k][i] = win[k + 1][i];
                     win[KW - 2][i] = now[i];
                 }
-                seq_store<T, VEC>(y + (half + r) * p.ld_y, out);
+                seq_store<T, VEC>(y + (r0 + r) * p.ld_y, out);
             }
         }
-    }
+    };
+    auto run_rows = [&](auto silu) {
+        int r0 = 0;
+        for (; r0 + kConvChunk <= rows; r0 += kConvChunk) chunk(SeqNo(), silu, r0);
+        if (r0 < rows) chunk(SeqYes(), silu, r0);
+    };
+    if (p.silu) run_rows(SeqYes());
+    else run_rows(SeqNo());
     if (first && p.state_out && slot >= 0) {
         // the state after the sequence is e[len .. len + W - 2]; ascending, so that in place a row is read before it is written
         T* out = static_cast<T*>(p.state_out) + slot * p.state_stride + c;
@@ -150,20 +165,13 @@ __global__ void __launch_bounds__(128) conv1d_fwd_kernel(const __grid_constant__
     }
 }
 
-template <typename T>
-__device__ __forceinline__ float conv_act_grad(float pre, int silu) {
-    if (!silu) return 1.0f;
-    const float s = sigmoid_f<T>(pre);
-    return s * fmaf(pre, 1.0f - s, 1.0f);
-}
-
 // Backward.  With g[t] = dy[t] * act'(pre[t]):
 //   de[j] = sum_k weight[k] g[j - k]  (+ dstate_out behind the sequence),  dweight[k] = sum_t g[t] e[t + k],  dbias = sum_t g[t].
 // One pass over x and dy: a thread walks a run of rows with the last KW rows of x and of g in registers; row t of g completes
 // de of the row KW - 1 before it.  A run re-reads KW - 1 rows on either side (from L2).  dweight and dbias are summed over the
 // run in registers, over a block's runs in shared memory and over blocks by conv1d_dweight_kernel, always in the same order.
 template <typename T, int VEC, int KW>
-__global__ void __launch_bounds__(128) conv1d_bwd_kernel(const __grid_constant__ Conv1dParams p) {
+__global__ void __launch_bounds__(128, KW <= 4 ? 4 : 2) conv1d_bwd_kernel(const __grid_constant__ Conv1dParams p) {
     constexpr int kSums = VEC * (KW + 1);
     __shared__ float sums[kConvRuns][32][kSums + 1];
     seq_grid_wait();
@@ -201,43 +209,48 @@ __global__ void __launch_bounds__(128) conv1d_bwd_kernel(const __grid_constant__
         for (int k = 0; k < KW - 1; ++k) conv_ext_row<T, VEC>(x, p.ld_x, state, p.channels, w1, t0 + k - (KW - p.width), len, win[k]);
 #pragma unroll
         for (int m = 0; m < KW; ++m) conv_zero<T, VEC>(gw[m]);
-        const int stop = min(kConvBwdRows, max(len - t0, 0)) + KW - 1;   // the last row of dx of this run is emitted at stop - 1
-        for (int i0 = 0; i0 < stop; i0 += 8) {
-            SeqVec<T, VEC> rx[8], rg[8];
+        const int own_rows = min(kConvBwdRows, max(len - t0, 0)), stop = own_rows + KW - 1;   // the last row of dx of this run is emitted at stop - 1
+        const T* xr = x + t0 * p.ld_x;
+        const T* dyr = dy + t0 * p.ld_dy;
+        T* dxr = dx + (t0 - (KW - 1)) * p.ld_dx;               // the row of x that is complete when row 0 of the run is reached
+        auto chunk = [&](auto checked, auto silu, int i0) {
+            constexpr bool kChecked = decltype(checked)::value;
+            SeqVec<T, VEC> rx[kConvBwdChunk], rg[kConvBwdChunk];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const int t = t0 + i0 + r;
-                if (i0 + r < stop && t < len) {
-                    rx[r] = seq_load<T, VEC>(x + t * p.ld_x);
-                    rg[r] = seq_load<T, VEC>(dy + t * p.ld_dy);
+            for (int r = 0; r < kConvBwdChunk; ++r) {
+                if (!kChecked || (i0 + r < stop && t0 + i0 + r < len)) {
+                    rx[r] = seq_load<T, VEC>(xr + (i0 + r) * p.ld_x);
+                    rg[r] = seq_load<T, VEC>(dyr + (i0 + r) * p.ld_dy);
                 }
             }
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
+            for (int r = 0; r < kConvBwdChunk; ++r) {
                 const int i = i0 + r, t = t0 + i;
-                if (i < stop) {
+                if (!kChecked || i < stop) {
                     float now[VEC], g[VEC], de[VEC];
-                    conv_zero<T, VEC>(now);
-                    conv_zero<T, VEC>(g);
-                    if (t < len) {
+                    const bool there = !kChecked || t < len, own = !kChecked || (i < kConvBwdRows && there);
+                    if (there) {
                         seq_unpack<T, VEC>(rx[r], now);
                         seq_unpack<T, VEC>(rg[r], g);
+                    } else {
+                        conv_zero<T, VEC>(now);
+                        conv_zero<T, VEC>(g);
                     }
-                    const bool own = i < kConvBwdRows && t < len;
                     const int j = t - (KW - 1);                          // the row of x completed by g[t]
-                    const bool emit_x = i >= KW - 1 && j < len, emit_s = first && dsi != nullptr && j < 0 && j + w1 >= 0;
-                    const bool from_state = dso != nullptr && j + w1 >= len && (emit_x || emit_s);
+                    const bool emit_x = !kChecked || (i >= KW - 1 && j < len), emit_s = kChecked && first && dsi != nullptr && j < 0 && j + w1 >= 0;
+                    const bool from_state = kChecked && dso != nullptr && j + w1 >= len && (emit_x || emit_s);
                     if (from_state) conv_state_row<T, VEC>(dso + (j + w1 - len) * p.channels, de);
                     else conv_zero<T, VEC>(de);
 #pragma unroll
                     for (int v = 0; v < VEC; ++v) {
-                        if (t < len) {
+                        if (there && decltype(silu)::value) {
                             float pre = bias[v];
 #pragma unroll
                             for (int k = 0; k < KW - 1; ++k)
                                 if (conv_tap<KW>(k, p.width)) pre = fmaf(w[k][v], win[k][v], pre);
                             pre = fmaf(w[KW - 1][v], now[v], pre);
-                            g[v] *= conv_act_grad<T>(pre, p.silu);
+                            const float s = sigmoid_f<T>(pre);
+                            g[v] *= s * fmaf(pre, 1.0f - s, 1.0f);       // silu'(pre)
                         }
                         if (own) {
 #pragma unroll
@@ -257,11 +270,19 @@ __global__ void __launch_bounds__(128) conv1d_bwd_kernel(const __grid_constant__
                         for (int k = 0; k < KW; ++k)
                             if (conv_tap<KW>(k, p.width)) de[v] = fmaf(w[k][v], gw[k][v], de[v]);
                     }
-                    if (emit_x) seq_store<T, VEC>(dx + j * p.ld_dx, de);
+                    if (emit_x) seq_store<T, VEC>(dxr + i * p.ld_dx, de);
                     if (emit_s) seq_store<T, VEC>(dsi + (j + w1) * p.channels, de);
                 }
             }
-        }
+        };
+        auto run_rows = [&](auto silu) {
+            int i0 = 0;
+            for (; i0 < KW - 1; i0 += kConvBwdChunk) chunk(SeqYes(), silu, i0);      // no row is complete before row KW - 1
+            for (; i0 + kConvBwdChunk <= own_rows; i0 += kConvBwdChunk) chunk(SeqNo(), silu, i0);
+            for (; i0 < stop; i0 += kConvBwdChunk) chunk(SeqYes(), silu, i0);
+        };
+        if (p.silu) run_rows(SeqYes());
+        else run_rows(SeqNo());
     }
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {

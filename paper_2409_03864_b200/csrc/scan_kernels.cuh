@@ -152,9 +152,6 @@ __device__ __forceinline__ void scan_sum(const float* p, float (&s)[VEC]) {
     }
 }
 
-struct ScanYes { static constexpr bool value = true; };
-struct ScanNo { static constexpr bool value = false; };
-
 enum ScanMode { kScanFull = 0, kScanState = 1, kScanAdjoint = 2 };
 
 // kScanFull: the forward pass over a chunk, from the state before it.
@@ -270,11 +267,11 @@ __global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(const __grid_con
     auto fetch = [&](int row0) {
         const int left = min(t1 - row0, kRows);
         if (whole && left == kRows) {
-            if (gated) fetch_as(ScanYes(), ScanNo(), left);
-            else fetch_as(ScanNo(), ScanNo(), left);
+            if (gated) fetch_as(SeqYes(), SeqNo(), left);
+            else fetch_as(SeqNo(), SeqNo(), left);
         } else {
-            if (gated) fetch_as(ScanYes(), ScanYes(), left);
-            else fetch_as(ScanNo(), ScanYes(), left);
+            if (gated) fetch_as(SeqYes(), SeqYes(), left);
+            else fetch_as(SeqNo(), SeqYes(), left);
         }
         const long long move = kBack ? -kRows : kRows;
         px += move * ld_x;
@@ -349,11 +346,11 @@ __global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(const __grid_con
     for (int tile = 0; tile < tiles; ++tile) {
         const int row0 = kBack ? first_row - tile * kRows : first_row + tile * kRows, left = min(t1 - row0, kRows);
         if (p.softplus) {
-            if (gated) elementwise_as(ScanYes(), ScanYes(), left);
-            else elementwise_as(ScanNo(), ScanYes(), left);
+            if (gated) elementwise_as(SeqYes(), SeqYes(), left);
+            else elementwise_as(SeqNo(), SeqYes(), left);
         } else {
-            if (gated) elementwise_as(ScanYes(), ScanNo(), left);
-            else elementwise_as(ScanNo(), ScanNo(), left);
+            if (gated) elementwise_as(SeqYes(), SeqNo(), left);
+            else elementwise_as(SeqNo(), SeqNo(), left);
         }
 #pragma unroll
         for (int i = 0; i < kBc; ++i) {

@@ -38,6 +38,19 @@ int launch_seq(void (*kernel)(Params...), int64_t grid_x, int64_t grid_y, int th
     return launch_seq_cluster(kernel, grid_x, grid_y, threads, smem, 1, st, given...);
 }
 
+// Lets a kernel have more than 48 KB of shared memory: as much as there is, remembered per device, so that later calls skip it.
+template <typename Kernel>
+int allow_smem(Kernel kernel, std::atomic<bool> (&known)[64], size_t bytes) {
+    if (bytes <= 48 * 1024) return TDX_OK;
+    int dev = 0;
+    TDX_CUDA(cudaGetDevice(&dev));
+    const bool listed = dev >= 0 && dev < 64;
+    if (listed && known[dev].load(std::memory_order_acquire)) return TDX_OK;
+    TDX_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimitDefault));
+    if (listed) known[dev].store(true, std::memory_order_release);
+    return TDX_OK;
+}
+
 bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
 int64_t elem_bytes(int dtype) { return dtype == TDX_F32 ? 4 : 2; }
 
@@ -134,6 +147,7 @@ int check_conv1d(const tdx_conv1d_args* a, ConvPass pass, tdx::Conv1dParams* p) 
     p->batch = a->batch; p->max_len = a->max_len; p->rows = a->rows; p->channels = a->channels;
     p->width = a->width; p->silu = a->silu;
     p->x = a->x; p->ld_x = a->ld_x; p->weight = a->weight; p->bias = a->bias; p->y = a->y; p->ld_y = a->ld_y;
+    p->weight_aligned = !misaligned(a->weight, 16);
     p->offsets = a->seq_offsets; p->slots = a->slots; p->n_slots = a->n_slots; p->state_stride = stride;
     p->state_in = stateful ? a->state_in : nullptr;
     p->state_out = stateful ? a->state_out : nullptr;
@@ -187,13 +201,8 @@ int launch_conv1d(ConvPass pass, tdx::Conv1dParams& p, cudaStream_t st) {
     const int64_t piece = tdx::kConvRuns * (pass == kConvForward ? tdx::kConvRows : tdx::kConvBwdRows);
     p.dense = conv_dense_pieces(p.max_len, piece);
     const int64_t grid = tdx::seq_pieces(p.offsets != nullptr, p.batch, p.rows, p.dense, piece) * p.channel_tiles;
-    if constexpr (sizeof(T) == 4 || VEC != 4) {
-        if (pass == kConvForward) return launch_seq(tdx::conv1d_fwd_kernel<T, VEC, KW>, grid, 1, 128, 0, st, p);
-    }
-    if constexpr (sizeof(T) == 4 || VEC != 8) {
-        if (pass == kConvBackward) return launch_seq(tdx::conv1d_bwd_kernel<T, VEC, KW>, grid, 1, 128, 0, st, p);
-    }
-    return fail(TDX_ERR_UNSUPPORTED, "no kernel for this access width");
+    if (pass == kConvForward) return launch_seq(tdx::conv1d_fwd_kernel<T, VEC, KW>, grid, 1, 128, 0, st, p);
+    return launch_seq(tdx::conv1d_bwd_kernel<T, VEC, KW>, grid, 1, 128, 0, st, p);
 }
 template <typename T, int VEC>
 int launch_conv1d_width(ConvPass pass, tdx::Conv1dParams& p, cudaStream_t st) {
@@ -209,12 +218,10 @@ int run_conv1d(const tdx_conv1d_args* a, ConvPass pass, tdx::Conv1dParams& p, cu
     if (a->dtype == TDX_F32) {
         return conv_vector(a, p, 16, back) == 4 ? launch_conv1d_width<float, 4>(pass, p, st) : launch_conv1d_width<float, 1>(pass, p, st);
     }
-    // the backward kernel keeps four rows of sums per channel: eight channels a thread would not fit its registers
-    const int vec = conv_vector(a, p, back ? 8 : 16, back);
-    if (back) return vec == 4 ? launch_conv1d_width<__nv_bfloat16, 4>(pass, p, st)
-                     : vec >= 2 ? launch_conv1d_width<__nv_bfloat16, 2>(pass, p, st) : launch_conv1d_width<__nv_bfloat16, 1>(pass, p, st);
-    return vec == 8 ? launch_conv1d_width<__nv_bfloat16, 8>(pass, p, st)
-           : vec >= 2 ? launch_conv1d_width<__nv_bfloat16, 2>(pass, p, st) : launch_conv1d_width<__nv_bfloat16, 1>(pass, p, st);
+    // windows, weights and sums of eight channels a thread would leave too few warps
+    const int vec = conv_vector(a, p, 8, back);
+    return vec == 4 ? launch_conv1d_width<__nv_bfloat16, 4>(pass, p, st)
+           : vec == 2 ? launch_conv1d_width<__nv_bfloat16, 2>(pass, p, st) : launch_conv1d_width<__nv_bfloat16, 1>(pass, p, st);
 }
 
 // ------------------------------------------------------------------ selective scan
@@ -404,8 +411,8 @@ template <typename T, int WORDS, int BLOCKS>
 int launch_w4_staged(tdx::W4Params p, int warps, cudaStream_t st) {
     p.per = static_cast<int>(ceil_div(p.steps, warps));
     const size_t smem = tdx::kW4RingBytes * 32 * warps + tdx::w4_x_bytes<T>(p.steps, p.M) + 8 * static_cast<size_t>(tdx::kW4Rows * BLOCKS) * (p.groups + 1);
-    if (smem > 48 * 1024)
-        TDX_CUDA(cudaFuncSetAttribute(tdx::w4_staged_kernel<T, WORDS, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    static std::atomic<bool> known[64];
+    TDX_TRY(allow_smem(tdx::w4_staged_kernel<T, WORDS, BLOCKS>, known, smem));
     return launch_seq(tdx::w4_staged_kernel<T, WORDS, BLOCKS>, ceil_div(p.N, tdx::kW4Rows * BLOCKS), 1, 32 * warps, smem, st, p);
 }
 template <typename T, int WORDS, int TILES>

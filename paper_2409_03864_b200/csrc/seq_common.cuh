@@ -11,6 +11,10 @@ namespace tdx {
 // lies outside the caller's tensors; that sequence or state is skipped
 enum : int { kStatusSequence = 9 };
 
+// compile-time answers for generic lambdas
+struct SeqYes { static constexpr bool value = true; };
+struct SeqNo { static constexpr bool value = false; };
+
 // ---------------------------------------------------------------- elements
 __device__ __forceinline__ float seq_to_float(float v) { return v; }
 __device__ __forceinline__ float seq_to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
