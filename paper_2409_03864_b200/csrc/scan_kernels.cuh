@@ -794,82 +794,125 @@ __global__ void __launch_bounds__(256) scan_bwd_join_kernel(const __grid_constan
     }
 }
 
-// One new row for each of a batch of sequences.  A warp takes 32 channels of one batch row: a lane does the elementwise work
-// of one channel, then the warp goes through the states in TPC rounds of 32 / TPC channels, four states (16 bytes) a lane.
-// Bound by reading and writing the states.  A thread writes only the states that it read, so state_out may be state_in.  A
-// batch row without a slot is padding: out = 0.
-template <typename T, int TPC, bool VEC4>
+// One new row for each of a batch of sequences.  A warp takes 32 channels of batch rows in turn (blockIdx.y, + gridDim.y, ...), with A
+// in registers: a lane does the elementwise work of one channel, then the warp goes through the states in PER rounds of 32 / PER
+// channels, four states (16 bytes) a lane.  Bound by reading and writing the states.  A thread writes only the states that it
+// read, so state_out may be state_in.  A batch row without a slot is padding: out = 0.
+template <typename T, int PER, bool VEC4>
 __global__ void __launch_bounds__(128) scan_step_kernel(const __grid_constant__ ScanParams p) {
-    constexpr int kPer = 32 / TPC;                         // channels of a round
+    constexpr int kCh = 32 / PER;                          // channels of a round
+    constexpr int kHeld = PER <= 8 ? PER : 1;              // rounds whose A is held
     seq_launch_dependents();
-    seq_grid_wait();
-    const int lane = threadIdx.x & 31;
-    const long long warp = blockIdx.x * 4LL + (threadIdx.x >> 5);
-    const long long b = warp / p.channel_tiles;
-    if (b >= p.batch) return;
-    const long long c0 = (warp - b * p.channel_tiles) * 32, mine = c0 + lane;
+    const int lane = threadIdx.x & 31, sub = lane / PER, n0 = (lane % PER) * 4;
+    const long long tile = blockIdx.x * 4LL + (threadIdx.x >> 5), c0 = tile * 32, mine = c0 + lane;
+    if (tile >= p.channel_tiles) return;
     const bool live = mine < p.channels;
-    const long long slot = state_slot(p.slots, b, p.n_slots, p.status);
-    float xv = 0.0f, d = 0.0f, gate = 1.0f, y = 0.0f;
-    if (live && slot >= 0) {
-        xv = seq_to_float(static_cast<const T*>(p.x)[b * p.ld_x + mine]);
-        d = seq_to_float(static_cast<const T*>(p.dt)[b * p.ld_dt + mine]) + (p.dt_bias ? __ldg(p.dt_bias + mine) : 0.0f);
-        if (p.softplus) d = softplus_f<T>(d);
-        if (p.z) {
-            const float zz = seq_to_float(static_cast<const T*>(p.z)[b * p.ld_z + mine]);
-            gate = zz * sigmoid_f<T>(zz);
+    const int group0 = static_cast<int>(c0 / p.group_channels);
+    const bool one_group = min(c0 + 31, p.channels - 1) / p.group_channels == group0;
+    seq_grid_wait();
+    float a[kHeld][4];
+    auto load_a = [&](long long c, float (&v)[4]) {
+        if (VEC4) {
+            const float4 q = c < p.channels ? __ldg(reinterpret_cast<const float4*>(p.A + c * p.states + n0)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            v[0] = q.x * kLog2e; v[1] = q.y * kLog2e; v[2] = q.z * kLog2e; v[3] = q.w * kLog2e;
+        } else {
+            scan_load_a(p, c, n0, c < p.channels, v);
         }
-        y = p.D ? __ldg(p.D + mine) * xv : 0.0f;
+    };
+    if (PER <= 8) {
+#pragma unroll
+        for (int round = 0; round < kHeld; ++round) load_a(c0 + round * kCh + sub, a[round]);
     }
-    if (slot >= 0) {
+    const float bias = p.dt_bias && live ? __ldg(p.dt_bias + mine) : 0.0f, skip = p.D && live ? __ldg(p.D + mine) : 0.0f;
+    for (long long b = blockIdx.y; b < p.batch; b += gridDim.y) {
+        const long long slot = state_slot(p.slots, b, p.n_slots, p.status);
+        T* out = static_cast<T*>(p.out) + b * p.ld_out + mine;
+        if (slot < 0) {
+            if (live) *out = seq_from_float<T>(0.0f);
+            continue;
+        }
+        float xv = 0.0f, d = 0.0f, gate = 1.0f;
+        if (live) {
+            xv = seq_to_float(static_cast<const T*>(p.x)[b * p.ld_x + mine]);
+            d = seq_to_float(static_cast<const T*>(p.dt)[b * p.ld_dt + mine]) + bias;
+            if (p.z) gate = seq_to_float(static_cast<const T*>(p.z)[b * p.ld_z + mine]);
+        }
+        // B and C of a lane's states: the same in every round, unless the warp's channels lie in several groups
+        float bv[4] = {0.f, 0.f, 0.f, 0.f}, cv[4] = {0.f, 0.f, 0.f, 0.f};
+        auto load_bc = [&](long long group) {
+            const T* B = static_cast<const T*>(p.B) + b * p.ld_b + group * p.states + n0;
+            const T* C = static_cast<const T*>(p.C) + b * p.ld_c + group * p.states + n0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (VEC4 || n0 + i < p.states) {
+                    bv[i] = seq_to_float(__ldg(B + i));
+                    cv[i] = seq_to_float(__ldg(C + i));
+                }
+            }
+        };
+        load_bc(group0);
+        const float* from = p.state_in + slot * p.state_stride + n0;
+        float* to = p.state_out + slot * p.state_stride + n0;
+        auto load_h = [&](long long c, float (&h)[4]) {
+            if (c >= p.channels) return;
+            if (VEC4) {
+                const float4 q = *reinterpret_cast<const float4*>(from + c * p.states);
+                h[0] = q.x; h[1] = q.y; h[2] = q.z; h[3] = q.w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (n0 + i < p.states) h[i] = from[c * p.states + i];
+            }
+        };
+        float held[kHeld][4];
+        if (PER <= 8) {                                     // all states are in flight before the first is used
+#pragma unroll
+            for (int round = 0; round < kHeld; ++round) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) held[round][i] = 0.0f;
+                load_h(c0 + round * kCh + sub, held[round]);
+            }
+        }
+        if (p.softplus) d = softplus_f<T>(d);
+        if (p.z) gate *= sigmoid_f<T>(gate);
         const float u = d * xv;
-        const int sub = lane / TPC, n0 = (lane % TPC) * 4;
+        float y = skip * xv;
 #pragma unroll
-        for (int round = 0; round < TPC; ++round) {
-            const int from = round * kPer + sub;
-            const long long c = c0 + from;
-            const float dd = __shfl_sync(0xffffffffu, d, from), uu = __shfl_sync(0xffffffffu, u, from);
+        for (int round = 0; round < PER; ++round) {
+            const int src = round * kCh + sub;
+            const long long c = c0 + src;
+            float (&h)[4] = held[PER <= 8 ? round : 0];
+            float (&aa)[4] = a[PER <= 8 ? round : 0];
+            if (PER > 8) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) h[i] = 0.0f;
+                load_h(c, h);
+                load_a(c, aa);
+            }
+            const float dd = __shfl_sync(0xffffffffu, d, src), uu = __shfl_sync(0xffffffffu, u, src);
+            if (!one_group && c < p.channels) load_bc(c / p.group_channels);
             float part = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                h[i] = fmaf(fast_exp2(dd * aa[i]), h[i], uu * bv[i]);
+                part = fmaf(h[i], cv[i], part);
+            }
             if (c < p.channels) {
-                const long long at = slot * p.state_stride + c * p.states + n0;
-                const long long group = c / p.group_channels;
-                const T* B = static_cast<const T*>(p.B) + b * p.ld_b + group * p.states + n0;
-                const T* C = static_cast<const T*>(p.C) + b * p.ld_c + group * p.states + n0;
-                float h[4], av[4];
                 if (VEC4) {
-                    const float4 hv = *reinterpret_cast<const float4*>(p.state_in + at);
-                    const float4 aa = __ldg(reinterpret_cast<const float4*>(p.A + c * p.states + n0));
-                    h[0] = hv.x; h[1] = hv.y; h[2] = hv.z; h[3] = hv.w;
-                    av[0] = aa.x; av[1] = aa.y; av[2] = aa.z; av[3] = aa.w;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        h[i] = n0 + i < p.states ? p.state_in[at + i] : 0.0f;
-                        av[i] = n0 + i < p.states ? __ldg(p.A + c * p.states + n0 + i) : 0.0f;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (VEC4 || n0 + i < p.states) {
-                        h[i] = fmaf(fast_exp2(dd * (av[i] * kLog2e)), h[i], uu * seq_to_float(B[i]));
-                        part = fmaf(h[i], seq_to_float(C[i]), part);
-                    }
-                }
-                if (VEC4) {
-                    *reinterpret_cast<float4*>(p.state_out + at) = make_float4(h[0], h[1], h[2], h[3]);
+                    *reinterpret_cast<float4*>(to + c * p.states) = make_float4(h[0], h[1], h[2], h[3]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (n0 + i < p.states) p.state_out[at + i] = h[i];
+                        if (n0 + i < p.states) to[c * p.states + i] = h[i];
                 }
             }
 #pragma unroll
-            for (int m = 1; m < TPC; m *= 2) part += __shfl_xor_sync(0xffffffffu, part, m);
-            const float got = __shfl_sync(0xffffffffu, part, (lane % kPer) * TPC);
-            if (lane / kPer == round) y += got;
+            for (int m = 1; m < PER; m *= 2) part += __shfl_xor_sync(0xffffffffu, part, m);
+            const float got = __shfl_sync(0xffffffffu, part, (lane % kCh) * PER);
+            if (lane / kCh == round) y += got;
         }
+        if (live) *out = seq_from_float<T>(y * gate);
     }
-    if (live) static_cast<T*>(p.out)[b * p.ld_out + mine] = seq_from_float<T>(slot >= 0 ? y * gate : 0.0f);
 }
 
 }  // namespace tdx

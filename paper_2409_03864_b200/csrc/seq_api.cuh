@@ -297,7 +297,7 @@ size_t scan_saved_bytes(const tdx::ScanParams& p) {
 
 // How a scan is spread over the SMs: sequences are cut into chunks when channels and sequences alone do not give every SM a
 // block; a cut costs a second look at the inputs and a second exponential per state.
-void plan_scan(tdx::ScanParams* p, int sm_count) {
+void plan_scan(tdx::ScanParams* p, int sm_count, bool back) {
     const int n = scan_padded_states(p->states);
     // sequences that run side by side: packed ones of uneven length count by their rows
     const int64_t longest = std::max<int64_t>(1, std::min(p->max_len, p->rows));
@@ -305,8 +305,8 @@ void plan_scan(tdx::ScanParams* p, int sm_count) {
     p->channel_tiles = static_cast<int>(ceil_div(p->group_channels, tdx::kScanThreads * 4 / n));
     const int64_t tiles = std::max<int64_t>(1, static_cast<int64_t>(p->channel_tiles) * p->groups);
     p->chunk = ceil_div(longest, 32) * 32;
-    if (tiles * side < sm_count) {
-        const int64_t want = ceil_div(2 * sm_count, tiles);                // chunks of all sequences together
+        if (tiles * side < sm_count) {
+        const int64_t want = ceil_div((back ? 2 : 3) * sm_count, tiles);                // chunks of all sequences together
         const int64_t chunk = std::max<int64_t>(64, ceil_div(ceil_div(p->offsets ? p->rows : longest * side, want), 32) * 32);
         if (chunk < p->chunk) p->chunk = chunk;
     }
@@ -378,32 +378,33 @@ int launch_scan_passes(ScanPass pass, tdx::ScanParams& p, cudaStream_t st) {
                       static_cast<long long>(a_blocks), static_cast<long long>(numbers));
 }
 template <typename T, int N>
-int launch_scan(ScanPass pass, int vec, tdx::ScanParams& p, cudaStream_t st) {
+int launch_scan(ScanPass pass, int vec, tdx::ScanParams& p, int sm_count, cudaStream_t st) {
     if (pass == kScanStepPass) {
         p.channel_tiles = static_cast<int>(ceil_div(p.channels, 32));
-        const int64_t warps = p.batch * p.channel_tiles;
         const bool vec4 = p.states == N && !misaligned(p.state_in, 16) && !misaligned(p.state_out, 16) && !misaligned(p.A, 16) && p.state_stride % 4 == 0;
-        return vec4 ? launch_seq(tdx::scan_step_kernel<T, N / 4, true>, ceil_div(warps, 4), 1, 128, 0, st, p)
-                    : launch_seq(tdx::scan_step_kernel<T, N / 4, false>, ceil_div(warps, 4), 1, 128, 0, st, p);
+        // several batch rows a warp, as long as every SM has 32 warps
+        const int64_t blocks = ceil_div(p.channel_tiles, 4), rows = std::min<int64_t>(std::min<int64_t>(65535, p.batch), ceil_div(8 * sm_count, blocks));
+        return vec4 ? launch_seq(tdx::scan_step_kernel<T, N / 4, true>, blocks, rows, 128, 0, st, p)
+                    : launch_seq(tdx::scan_step_kernel<T, N / 4, false>, blocks, rows, 128, 0, st, p);
     }
     return vec == 2 ? launch_scan_passes<T, N, 2>(pass, p, st) : launch_scan_passes<T, N, 1>(pass, p, st);
 }
 template <typename T>
-int launch_scan_states(ScanPass pass, int vec, tdx::ScanParams& p, cudaStream_t st) {
+int launch_scan_states(ScanPass pass, int vec, tdx::ScanParams& p, int sm_count, cudaStream_t st) {
     switch (scan_padded_states(p.states)) {
-        case 4: return launch_scan<T, 4>(pass, vec, p, st);
-        case 8: return launch_scan<T, 8>(pass, vec, p, st);
-        case 16: return launch_scan<T, 16>(pass, vec, p, st);
-        case 32: return launch_scan<T, 32>(pass, vec, p, st);
-        case 64: return launch_scan<T, 64>(pass, vec, p, st);
-        default: return launch_scan<T, 128>(pass, vec, p, st);
+        case 4: return launch_scan<T, 4>(pass, vec, p, sm_count, st);
+        case 8: return launch_scan<T, 8>(pass, vec, p, sm_count, st);
+        case 16: return launch_scan<T, 16>(pass, vec, p, sm_count, st);
+        case 32: return launch_scan<T, 32>(pass, vec, p, sm_count, st);
+        case 64: return launch_scan<T, 64>(pass, vec, p, sm_count, st);
+        default: return launch_scan<T, 128>(pass, vec, p, sm_count, st);
     }
 }
 int run_scan(const tdx_scan_args* a, ScanPass pass, tdx::ScanParams& p, DeviceCtx* ctx, void* stream) {
     p.status = ctx->status_ptr;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int vec = pass == kScanStepPass ? 1 : scan_vector(a, p, pass == kScanBackwardPass);
-    return a->dtype == TDX_F32 ? launch_scan_states<float>(pass, vec, p, st) : launch_scan_states<__nv_bfloat16>(pass, vec, p, st);
+    return a->dtype == TDX_F32 ? launch_scan_states<float>(pass, vec, p, ctx->sm_count, st) : launch_scan_states<__nv_bfloat16>(pass, vec, p, ctx->sm_count, st);
 }
 
 // ------------------------------------------------------------------ 4-bit weights
@@ -510,7 +511,7 @@ int tdx_selective_scan(const tdx_scan_args* args, void* stream) {
     }
     DeviceCtx* ctx;
     TDX_TRY(get_ctx(&ctx));
-    plan_scan(&p, ctx->sm_count);
+    plan_scan(&p, ctx->sm_count, false);
     const ScanWorkspace w = scan_workspace(p, false);
     TDX_TRY(check_workspace(args->workspace, args->workspace_bytes, w.total));
     place_scan(&p, w, args->workspace);
@@ -531,7 +532,7 @@ int tdx_selective_scan_bwd(const tdx_scan_args* args, void* stream) {
         if (p.ddt_bias) TDX_CUDA(cudaMemsetAsync(p.ddt_bias, 0, p.channels * sizeof(float), st));
         return TDX_OK;
     }
-    plan_scan(&p, ctx->sm_count);
+    plan_scan(&p, ctx->sm_count, true);
     const ScanWorkspace w = scan_workspace(p, true);
     TDX_TRY(check_workspace(args->workspace, args->workspace_bytes, w.total));
     place_scan(&p, w, args->workspace);
@@ -559,8 +560,13 @@ int tdx_selective_scan_workspace_size(const tdx_scan_args* args, size_t* bytes) 
     if (bytes == nullptr) return fail(TDX_ERR_INVALID_ARG, "bytes is NULL");
     tdx::ScanParams p;
     TDX_TRY(check_scan(args, kScanForwardPass, &p, true));
-    plan_scan(&p, sm_count_or_default());
-    *bytes = scan_workspace(p, args->saved != nullptr).total;
+    const int sm_count = sm_count_or_default();
+    plan_scan(&p, sm_count, false);
+    *bytes = scan_workspace(p, false).total;
+    if (args->saved != nullptr) {
+        plan_scan(&p, sm_count, true);
+        *bytes = std::max(*bytes, scan_workspace(p, true).total);
+    }
     return TDX_OK;
 }
 
