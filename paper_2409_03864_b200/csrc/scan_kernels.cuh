@@ -478,20 +478,11 @@ __global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(const __grid_con
     constexpr int kEl = (kRows + kStep - 1) / kStep;
     constexpr int kBcStep = N >= kScanThreads ? 1 : kScanThreads / N, kBc = (kRows + kBcStep - 1) / kBcStep;
     constexpr int kSubs = kCh > 32 ? kCh / 32 : 1;         // warps that share their states
-    // dt', dt' x and g, each twice, so that they load as pairs (once where there would be too much of it: N = 4)
-    constexpr bool kTwice = kCh <= 64;
-    __shared__ float4 s_dt[kRows][kTwice ? kCh : kCh / 2];
-    __shared__ float2 s_g[kRows][kTwice ? kCh : kCh / 2];
-    auto dt_at = [&](int r, int c) {
-        if (kTwice) return *reinterpret_cast<const ulonglong2*>(&s_dt[r][c]);
-        const float2 v = reinterpret_cast<const float2*>(&s_dt[r][0])[c];
-        return make_ulonglong2(pack2(v.x, v.x), pack2(v.y, v.y));
-    };
-    auto g_at = [&](int r, int c) {
-        if (kTwice) return *reinterpret_cast<const f32x2*>(&s_g[r][c]);
-        const float v = reinterpret_cast<const float*>(&s_g[r][0])[c];
-        return pack2(v, v);
-    };
+    // (each once: twice, as in the forward kernel, saves moves, but shared memory is busier here; 781 instead of 766 us for the
+    // training step of 8192 rows x 2048 channels x 16 states)
+    __shared__ float2 s_dt[kRows][kCh];                    // dt', dt' x
+    __shared__ float s_g[kRows][kCh];
+    auto dt_at = [&](int r, int c) { return make_ulonglong2(pack2(s_dt[r][c].x, s_dt[r][c].x), pack2(s_dt[r][c].y, s_dt[r][c].y)); };
     __shared__ __align__(16) float s_b[kRows][N];
     __shared__ __align__(16) float s_c[kRows][N];
     __shared__ float4 s_list[kScanThreads / 32][8][kScanSumPitch];      // see scan_sum_lanes
@@ -610,13 +601,8 @@ __global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(const __grid_con
                     eg[i][v] = z ? eo[i][v] * (ez[i][v] * ezs[i][v]) : eo[i][v];
                     float w = ed[i][v] * ex[i][v];
                     if (!there) ed[i][v] = w = eg[i][v] = 0.0f;
-                    if (kTwice) {
-                        s_dt[r][cc + v] = make_float4(ed[i][v], ed[i][v], w, w);
-                        s_g[r][cc + v] = make_float2(eg[i][v], eg[i][v]);
-                    } else {
-                        reinterpret_cast<float2*>(&s_dt[r][0])[cc + v] = make_float2(ed[i][v], w);
-                        reinterpret_cast<float*>(&s_g[r][0])[cc + v] = eg[i][v];
-                    }
+                    s_dt[r][cc + v] = make_float2(ed[i][v], w);
+                    s_g[r][cc + v] = eg[i][v];
                 }
             }
         }
@@ -651,7 +637,7 @@ __global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(const __grid_con
 #pragma unroll
         for (int r = kRows - 1; r >= 0; --r) {
             const ulonglong2 dv = dt_at(r, ch);
-            const f32x2 g2 = g_at(r, ch);
+            const f32x2 g2 = pack2(s_g[r][ch], s_g[r][ch]);
             f32x2 b[P], cv[P], db[P], dc[P], y, du, dl;
             scan_load_pairs(&s_b[r][n0], b);
             scan_load_pairs(&s_c[r][n0], cv);
