@@ -9,7 +9,7 @@ namespace tdx {
 
 // recorded in the device status word (see kStatusBounds in simt_kernels.cuh): a sequence offset or a state slot that
 // lies outside the caller's tensors; that sequence or state is skipped
-enum : int { kStatusSequence = 9 };
+enum : int { kStatusSequence = 16 };
 
 // compile-time answers for generic lambdas
 struct SeqYes { static constexpr bool value = true; };

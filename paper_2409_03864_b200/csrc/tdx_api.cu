@@ -1701,6 +1701,10 @@ int tdx_tune_clear(void) {
     return TDX_OK;
 }
 
+// the status word holds one code, and what is reported goes by its value
+constexpr int kSequenceCode = tdx::kStatusSequence;
+static_assert(kSequenceCode != tdx::kStatusBounds && kSequenceCode != tdx::kTimeoutProducer && kSequenceCode != tdx::kTimeoutMma &&
+              kSequenceCode != tdx::kTimeoutEpilogue && kSequenceCode != tdx::kTimeoutSelfTest, "status codes must differ");
 int tdx_check_device_status(void* stream) {
     DeviceCtx* ctx;
     int rc = get_ctx(&ctx);
