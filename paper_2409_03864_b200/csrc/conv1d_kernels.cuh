@@ -89,7 +89,10 @@ __device__ __forceinline__ void conv_load_weights(const Conv1dParams& p, long lo
 }
 
 // Forward.  A warp takes 32 * VEC neighbouring channels of a run of kConvRows rows; a thread keeps the last KW - 1 rows of
-// its VEC channels in registers, so each row is read once (plus KW - 1 rows in front of a run).  Bound by memory.
+// its VEC channels in registers, so each row is read once (plus KW - 1 rows in front of a run).
+// 22.0 us for 4470 packed rows of 4096 channels in bf16 (3.3 TB/s, half of the copy rate; the whole call): the loads of a chunk wait for
+// memory at five blocks per SM, and SiLU takes two special functions a value.  The next chunk's rows in registers ahead of time cost more
+// in moves and checks than they hid (32 us against 24.9 in the form of that time).
 // The thread that reads the state (run 0) is also the one that writes the state after the sequence, so state_out may be
 // state_in.
 template <typename T, int VEC, int KW>
