@@ -491,6 +491,7 @@ int tdx_causal_conv1d_bwd(const tdx_conv1d_args* args, void* stream) {
     if (p.channels == 0) return TDX_OK;
     const int64_t numbers = conv_bwd_numbers(p), elems = p.channels * (p.width + 1);
     TDX_TRY(check_workspace(args->workspace, args->workspace_bytes, static_cast<size_t>(numbers) * elems * sizeof(float)));
+    if (numbers == 0 && p.dweight == nullptr && p.dbias == nullptr) return TDX_OK;
     DeviceCtx* ctx;
     TDX_TRY(get_ctx(&ctx));
     p.status = ctx->status_ptr;

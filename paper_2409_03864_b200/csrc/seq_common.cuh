@@ -165,11 +165,11 @@ __device__ __forceinline__ SeqRange seq_range(const int* __restrict__ offsets, l
 // Sequences are cut into pieces of `piece` rows, each worked on by a block (or a few).  A dense batch has `dense` pieces per
 // sequence.  Packed ones share rows / piece + batch numbers: sequence b starts at number offsets[b] / piece + b, which leaves
 // room for ceil(len / piece) of them and at least one, whatever the lengths are; the few numbers left over are pieces with no
-// rows.  Number i belongs to the last sequence that starts at or before i.
+// rows.  Number i belongs to the last sequence that starts at or before i.  No sequences have no pieces: there is no offset behind the first.
 constexpr int kNoPiece = 1 << 29;
 struct SeqPiece { long long b; int index; };
 __host__ __device__ __forceinline__ long long seq_pieces(bool packed, long long batch, long long rows, long long dense, long long piece) {
-    return packed ? rows / piece + batch : batch * dense;
+    return !packed ? batch * dense : batch > 0 ? rows / piece + batch : 0;
 }
 __device__ __forceinline__ SeqPiece seq_piece(const int* __restrict__ offsets, long long batch, long long dense, long long piece, long long i) {
     SeqPiece r;

@@ -295,3 +295,16 @@ def test_empty_problems():
     p.backward()
     p.check_backward()
     assert (p.dweight == 0).all() and (p.dbias == 0).all()
+
+
+def test_backward_of_a_packed_batch_of_no_sequences():
+    """The parameters' gradients are zero, and rows that belong to no sequence stay what they are."""
+    d, rows = 32, 1000
+    x, dy, dx = Rows(np.full((rows, d), np.nan), "f32"), Rows(np.full((rows, d), np.nan), "f32"), Rows(np.full((rows, d), 9.0), "f32")
+    w, offsets, dweight, dbias = f32(np.ones((d, 4))), i32([0]), f32(np.full((d, 4), np.nan)), f32(np.full(d, np.nan))
+    a = tdx.tdx_conv1d_args(batch=0, max_len=500, rows=rows, channels=d, width=4, dtype=tdx.TDX_F32, silu=1, x=x.ptr, ld_x=d, weight=w, seq_offsets=offsets,
+                            dy=dy.ptr, ld_dy=d, dx=dx.ptr, ld_dx=d, dweight=dweight, dbias=dbias)
+    assert tdx.tdx_causal_conv1d_workspace_size(a) == (tdx.TDX_OK, 0)
+    tdx.check(tdx.tdx_causal_conv1d_bwd(a))
+    assert tdx.tdx_check_device_status() == 0
+    assert (dweight == 0).all() and (dbias == 0).all() and (dx.host() == 9).all() and dx.guards_intact()

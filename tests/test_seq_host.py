@@ -163,3 +163,13 @@ def test_block_layouts_match_the_header():
         size = {"ptr": 8, "int64_t": 8, "size_t": 8, "int": 4}
         assert names == [n for n, _ in cls._fields_]
         assert [size[t] for t in types] == [ctypes.sizeof(t) for _, t in cls._fields_]
+
+
+def test_a_packed_batch_of_no_sequences_has_no_work():
+    """Rows that belong to no sequence make no pieces: nothing may be launched for them, as the offsets have one value only."""
+    empty = dict(batch=0, max_len=500, rows=1000, seq_offsets=P)
+    assert tdx.tdx_causal_conv1d_workspace_size(conv(**empty)) == (tdx.TDX_OK, 0)
+    assert tdx.tdx_selective_scan_saved_size(scan(**empty)) == (tdx.TDX_OK, 0)
+    assert tdx.tdx_causal_conv1d(conv(**empty)) == tdx.TDX_OK
+    assert tdx.tdx_causal_conv1d_bwd(conv(**empty, dweight=None, dbias=None)) == tdx.TDX_OK
+    assert tdx.tdx_selective_scan(scan(**empty)) == tdx.TDX_OK
