@@ -409,44 +409,53 @@ int run_scan(const tdx_scan_args* a, ScanPass pass, tdx::ScanParams& p, DeviceCt
 }
 
 // ------------------------------------------------------------------ 4-bit weights
+constexpr int kW4Warps = 16;         // of a staged block (see launch_w4_tiles)
+// What a block of w4_staged_kernel keeps in shared memory: the ring of weights, x, and `sets` times 16 rows of scales.
+template <typename T>
+size_t w4_staged_smem(const tdx::W4Params& p, int sets) {
+    return tdx::kW4RingBytes * 32 * kW4Warps + tdx::w4_x_bytes<T>(p.steps, p.M) + sizeof(float2) * static_cast<size_t>(tdx::kW4Rows * sets) * (p.groups + 1);
+}
 template <typename T, int WORDS, int BLOCKS>
-int launch_w4_staged(tdx::W4Params p, int warps, cudaStream_t st) {
-    p.per = static_cast<int>(ceil_div(p.steps, warps));
-    const size_t smem = tdx::kW4RingBytes * 32 * warps + tdx::w4_x_bytes<T>(p.steps, p.M) + 8 * static_cast<size_t>(tdx::kW4Rows * BLOCKS) * (p.groups + 1);
+int launch_w4_staged(tdx::W4Params p, cudaStream_t st) {
+    p.per = static_cast<int>(ceil_div(p.steps, kW4Warps));
+    const size_t smem = w4_staged_smem<T>(p, BLOCKS);
     static std::atomic<bool> known[64];
     TDX_TRY(allow_smem(tdx::w4_staged_kernel<T, WORDS, BLOCKS>, known, smem));
-    return launch_seq(tdx::w4_staged_kernel<T, WORDS, BLOCKS>, ceil_div(p.N, tdx::kW4Rows * BLOCKS), 1, 32 * warps, smem, st, p);
+    return launch_seq(tdx::w4_staged_kernel<T, WORDS, BLOCKS>, ceil_div(p.N, tdx::kW4Rows * BLOCKS), 1, 32 * kW4Warps, smem, st, p);
 }
 template <typename T, int WORDS, int TILES>
 int launch_w4_direct(const tdx::W4Params& p, cudaStream_t st) {
     return launch_seq(tdx::w4_direct_kernel<T, WORDS, TILES>, ceil_div(p.N, 16), ceil_div(p.M, TILES * tdx::W4Columns<T>::kRows), 256, 0, st, p);
 }
 template <typename T, int WORDS>
-int launch_w4_tiles(tdx::W4Params p, int sm_count, cudaStream_t st) {
+int launch_w4_tiles(tdx::W4Params p, const DeviceCtx& ctx, cudaStream_t st) {
     constexpr int kRows = tdx::W4Columns<T>::kRows;
     p.steps = static_cast<int>(ceil_div(p.K, tdx::kW4Step));
     p.groups = static_cast<int>(p.K / p.group);
     // Sixteen warps a block: eight took 6.7 us instead of 4.7 for one token and 4096 x 4096 weights.  Two sets of 16 rows a block
     // save a layout of x, but halve the blocks: 13.5 instead of 15.4 us for 8192 x 8192 (512 sets), 7.0 instead of 4.7 for
-    // 4096 x 4096 (256), so they are taken when one set each would need a second wave of two blocks per SM.
-    constexpr int kWarps = 16;
-    if (p.M <= kRows && tdx::w4_x_bytes<T>(p.steps, p.M) <= 64 * 1024)
-        return ceil_div(p.N, tdx::kW4Rows) > 2 * sm_count ? launch_w4_staged<T, WORDS, 2>(p, kWarps, st) : launch_w4_staged<T, WORDS, 1>(p, kWarps, st);
+    // 4096 x 4096 (256), so they are taken when one set each would need a second wave of two blocks per SM.  Scales grow with K /
+    // group: where they and x leave no room for two sets a block has one, and where not even for one the direct kernel runs.
+    if (p.M <= kRows && tdx::w4_x_bytes<T>(p.steps, p.M) <= 64 * 1024) {
+        const size_t most = static_cast<size_t>(ctx.smem_optin);
+        if (ceil_div(p.N, tdx::kW4Rows) > 2 * ctx.sm_count && w4_staged_smem<T>(p, 2) <= most) return launch_w4_staged<T, WORDS, 2>(p, st);
+        if (w4_staged_smem<T>(p, 1) <= most) return launch_w4_staged<T, WORDS, 1>(p, st);
+    }
     if (p.M <= kRows) return launch_w4_direct<T, WORDS, 1>(p, st);
     if (p.M <= 2 * kRows) return launch_w4_direct<T, WORDS, 2>(p, st);
     if (p.M <= 3 * kRows) return launch_w4_direct<T, WORDS, 3>(p, st);
     return launch_w4_direct<T, WORDS, 4>(p, st);
 }
 template <typename T>
-int launch_w4(const tdx::W4Params& p, int sm_count, cudaStream_t st) {
+int launch_w4(const tdx::W4Params& p, const DeviceCtx& ctx, cudaStream_t st) {
     // the tensor-core kernel reads 4, 8 or 16 bytes of a weight row and 16 bytes of a row of x at a time
     const bool fast = (p.group == 32 || p.group == 64 || p.group == 128) && p.K % p.group == 0 && !misaligned(p.weight, p.group / 8) &&
                       !misaligned(p.x, 16) && (p.M == 1 || p.ld_x * static_cast<int64_t>(sizeof(T)) % 16 == 0) && p.M <= 65535LL * 8;
     if (!fast) return launch_seq(tdx::w4_generic_kernel<T>, ceil_div(p.N, 4), std::min<int64_t>(ceil_div(p.M, 4), 1024), 128, 0, st, p);
     switch (p.group) {
-        case 32: return launch_w4_tiles<T, 1>(p, sm_count, st);
-        case 64: return launch_w4_tiles<T, 2>(p, sm_count, st);
-        default: return launch_w4_tiles<T, 4>(p, sm_count, st);
+        case 32: return launch_w4_tiles<T, 1>(p, ctx, st);
+        case 64: return launch_w4_tiles<T, 2>(p, ctx, st);
+        default: return launch_w4_tiles<T, 4>(p, ctx, st);
     }
 }
 
@@ -592,7 +601,7 @@ int tdx_gemm_w4(const tdx_w4_args* args, void* stream) {
     p.M = a.M; p.N = a.N; p.K = a.K; p.group = a.group_size;
     p.x = a.x; p.ld_x = a.ld_x; p.weight = a.weight; p.scales = a.scales; p.zeros = a.zeros; p.y = a.y; p.ld_y = a.ld_y;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return a.dtype == TDX_F32 ? launch_w4<float>(p, ctx->sm_count, st) : launch_w4<__nv_bfloat16>(p, ctx->sm_count, st);
+    return a.dtype == TDX_F32 ? launch_w4<float>(p, *ctx, st) : launch_w4<__nv_bfloat16>(p, *ctx, st);
 }
 
 int tdx_w4_quantize(int64_t N, int64_t K, int group_size, int dtype, const void* w, int64_t ld_w, uint8_t* weight, void* scales,

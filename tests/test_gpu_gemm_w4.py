@@ -149,3 +149,18 @@ def test_same_bits_on_another_stream():
         again = run("bf16", 3, 64, 1024, 128, True).view.clone()
     side.synchronize()
     assert torch.equal(first, again)
+
+
+@pytest.mark.parametrize("shape", [
+    # m, n, k, group: where x, the scales and the ring of weights together pass the shared memory of a block ...
+    (1, 4740, 28672, 64), (2, 4740, 14336, 32), (1, 40, 32768, 32), (1, 4740, 17408, 32), (4, 33, 8192, 32),
+    # ... and where they just fit, for both numbers of row sets
+    (1, 4768, 16384, 32), (1, 40, 16384, 32), (2, 4740, 8192, 32), (4, 4737, 8192, 64),
+])
+def test_long_rows_and_small_groups(shape):
+    run("bf16", *shape, True)
+
+
+def test_long_rows_and_small_groups_fp32():
+    run("f32", 1, 4750, 10880, 32, True)
+    run("f32", 1, 300, 10912, 32, False)
