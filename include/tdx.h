@@ -302,7 +302,8 @@ int tdx_causal_conv1d(const tdx_conv1d_args* args, void* stream);
 /* dx, dweight, dbias, dstate_in from x, weight, bias, state_in, dy and dstate_out; pre is computed again.  Needs a workspace. */
 int tdx_causal_conv1d_bwd(const tdx_conv1d_args* args, void* stream);
 /* One token for each of `batch` rows of x and y: seq_offsets, max_len and rows are not used, state_in and state_out are
- * needed (width > 1), and a row without a slot is padding whose y is zero. */
+ * needed (width > 1), and a row without a slot is padding whose y is zero.  (With width 1 there are no states, n_slots is not
+ * used, and slots, where given, only tell by their sign which rows are padding.) */
 int tdx_causal_conv1d_step(const tdx_conv1d_args* args, void* stream);
 /* Workspace of tdx_causal_conv1d_bwd (host only). */
 int tdx_causal_conv1d_workspace_size(const tdx_conv1d_args* args, size_t* bytes);

@@ -126,6 +126,7 @@ int check_conv1d(const tdx_conv1d_args* a, ConvPass pass, tdx::Conv1dParams* p) 
     int64_t stride = a->state_stride;
     TDX_TRY(check_states(stateful && (a->state_in || a->state_out || (back && (a->dstate_in || a->dstate_out))), a->batch, per_slot, &stride,
                          a->slots, a->n_slots));
+    if (step && misaligned(a->slots, 4)) return fail(TDX_ERR_ALIGNMENT, "slots is not aligned to its elements");
     const size_t el = elem_bytes(a->dtype);
     const bool any = a->channels > 0 && a->batch > 0, rows = any && (step || a->rows > 0);
     TDX_TRY(check_tensor("x", a->x, rows, el, a->ld_x, a->channels));
@@ -148,7 +149,8 @@ int check_conv1d(const tdx_conv1d_args* a, ConvPass pass, tdx::Conv1dParams* p) 
     p->width = a->width; p->silu = a->silu;
     p->x = a->x; p->ld_x = a->ld_x; p->weight = a->weight; p->bias = a->bias; p->y = a->y; p->ld_y = a->ld_y;
     p->weight_aligned = !misaligned(a->weight, 16);
-    p->offsets = a->seq_offsets; p->slots = a->slots; p->n_slots = a->n_slots; p->state_stride = stride;
+    // without states there are no slots to stay below: a step's slots then only tell which rows are padding
+    p->offsets = a->seq_offsets; p->slots = a->slots; p->n_slots = stateful ? a->n_slots : INT64_MAX; p->state_stride = stride;
     p->state_in = stateful ? a->state_in : nullptr;
     p->state_out = stateful ? a->state_out : nullptr;
     if (back) {

@@ -308,3 +308,24 @@ def test_backward_of_a_packed_batch_of_no_sequences():
     tdx.check(tdx.tdx_causal_conv1d_bwd(a))
     assert tdx.tdx_check_device_status() == 0
     assert (dweight == 0).all() and (dbias == 0).all() and (dx.host() == 9).all() and dx.guards_intact()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_single_tokens_of_width_one_need_neither_states_nor_slots(dtype):
+    rng = np.random.default_rng(8)
+    batch, d = 5, 24
+    v, w, bias = seeded(rng, (batch, d), dtype), seeded(rng, (d, 1), "f32"), seeded(rng, (d,), "f32")
+    x, y, dev_w, dev_b = Rows(v, dtype), Rows(np.zeros((batch, d)), dtype, fill=float("nan")), f32(w), f32(bias)
+    a = tdx.tdx_conv1d_args(batch=batch, channels=d, width=1, dtype=DT[dtype], silu=1, x=x.ptr, ld_x=d, weight=dev_w, bias=dev_b, y=y.ptr, ld_y=d)
+    tdx.check(tdx.tdx_causal_conv1d_step(a))
+    assert tdx.tdx_check_device_status() == 0
+    seqs, none = [(i, 1) for i in range(batch)], np.zeros((batch, 0, d))
+    o, m = ref.conv1d(v, w, bias, 1, seqs, none), ref.conv1d(v, w, bias, 1, seqs, none, magnitude=True)
+    assert_close("y", y.host(), o["y"], m["y"], forward_factor(1), dtype)
+    # slots only tell which rows are padding
+    slots = i32([7, -1, 0, 900, -3])
+    a.set(slots=slots)
+    tdx.check(tdx.tdx_causal_conv1d_step(a))
+    assert tdx.tdx_check_device_status() == 0
+    there = np.array([1, 0, 1, 1, 0])[:, None]
+    assert_close("y", y.host(), o["y"] * there, m["y"] * there, forward_factor(1), dtype)

@@ -173,3 +173,7 @@ def test_a_packed_batch_of_no_sequences_has_no_work():
     assert tdx.tdx_causal_conv1d(conv(**empty)) == tdx.TDX_OK
     assert tdx.tdx_causal_conv1d_bwd(conv(**empty, dweight=None, dbias=None)) == tdx.TDX_OK
     assert tdx.tdx_selective_scan(scan(**empty)) == tdx.TDX_OK
+
+
+def test_slots_of_a_step_without_states_are_checked_too():
+    assert tdx.tdx_causal_conv1d_step(conv(width=1, slots=P + 2, n_slots=0)) == ALIGNMENT
