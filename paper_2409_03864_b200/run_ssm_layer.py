@@ -7,8 +7,9 @@ causal convolution with SiLU, a projection of its result to the low-rank step, B
 selective scan, and an output projection.  Prompts of different lengths run packed, with tdx_gemm for the projections; their
 states go to slots of a cache, from which single tokens go on, with tdx_gemm_w4 for the projections.  The same tokens appended
 to the prompts and run as prompts must give the same outputs (up to the rounding of 4-bit against bf16 weights, which is why the
-prompts of the comparison run with the 4-bit weights too).  All work is on one stream, and every buffer and workspace is made
-before the first call.
+prompts of the comparison run with the 4-bit weights too).  All work goes to the caller's current stream, the library's calls as well
+as torch's.  Prompts and gradients make their buffers per call; single tokens work in buffers that are made once, so that a token
+step can be captured in a CUDA graph (after one step outside of it).
 """
 from __future__ import annotations
 
@@ -21,6 +22,11 @@ from . import binding as tdx
 BF16 = torch.bfloat16
 
 
+def _call(function, *args):
+    """A call of the library on the current stream, so that it comes after torch's work there and before what follows."""
+    tdx.check(function(*args, stream=torch.cuda.current_stream()))
+
+
 class Linear:
     """y = x W^T with bf16 weights for many rows and the same weights in 4 bits for few."""
 
@@ -30,18 +36,18 @@ class Linear:
         self.packed = torch.empty(n, k // 2, dtype=torch.uint8, device="cuda")
         self.scales = torch.empty(n, k // group, dtype=BF16, device="cuda")
         self.zeros = torch.empty(n, k // group, dtype=torch.uint8, device="cuda")
-        tdx.check(tdx.tdx_w4_quantize(n, k, group, tdx.TDX_BF16, w, k, self.packed, self.scales, self.zeros))
+        _call(tdx.tdx_w4_quantize, n, k, group, tdx.TDX_BF16, w, k, self.packed, self.scales, self.zeros)
         # the weights that the 4 bits stand for, so that prompts and single tokens run the same layer
         q = torch.stack([self.packed & 15, self.packed >> 4], dim=2).view(n, k // group, group).float()
         self.weight = ((q - self.zeros.float()[:, :, None]) * self.scales.float()[:, :, None]).view(n, k).to(BF16)
 
     def many(self, x, y):
-        tdx.check(tdx.tdx_gemm(x.shape[0], self.n, self.k, 0, 1, 1.0, tdx.TDX_BF16, x, self.weight, y))
+        _call(tdx.tdx_gemm, x.shape[0], self.n, self.k, 0, 1, 1.0, tdx.TDX_BF16, x, self.weight, y)
 
     def few(self, x, y):
-        tdx.check(tdx.tdx_gemm_w4(tdx.tdx_w4_args(
+        _call(tdx.tdx_gemm_w4, tdx.tdx_w4_args(
             M=x.shape[0], N=self.n, K=self.k, group_size=self.group, dtype=tdx.TDX_BF16, x=x, ld_x=x.stride(0), weight=self.packed,
-            scales=self.scales, zeros=self.zeros, y=y, ld_y=y.stride(0))))
+            scales=self.scales, zeros=self.zeros, y=y, ld_y=y.stride(0)))
 
 
 class Layer:
@@ -80,11 +86,11 @@ class Layer:
 
     def _run(self, u, b, apply, conv, scan):
         apply(self.proj_in, u, b["xz"])
-        tdx.check(conv())
+        _call(*conv)
         apply(self.proj_x, b["conv"], b["proj"])
         b["low"].copy_(b["proj"][:, :self.R])
         apply(self.proj_dt, b["low"], b["dt"])
-        tdx.check(scan())
+        _call(*scan)
         apply(self.proj_out, b["y"], b["out"])
         return b["out"]
 
@@ -104,7 +110,7 @@ class Layer:
         tdx.check(status)
         workspace = torch.empty(size, dtype=torch.uint8, device="cuda")
         scan.set(workspace=workspace, workspace_bytes=size)
-        out = self._run(u, b, Linear.many, lambda: tdx.tdx_causal_conv1d(conv), lambda: tdx.tdx_selective_scan(scan))
+        out = self._run(u, b, Linear.many, (tdx.tdx_causal_conv1d, conv), (tdx.tdx_selective_scan, scan))
         if keep is not None:
             keep.update(b=b, conv=conv, scan=scan, workspace=workspace, offsets=offsets, slots=slots)
         return out
@@ -114,7 +120,7 @@ class Layer:
         common = dict(batch=u.shape[0], slots=slots, n_slots=cache[0].shape[0])
         conv = self.conv_args(b, state_in=cache[0], state_out=cache[0], **common)
         scan = self.scan_args(b, state_in=cache[1], state_out=cache[1], **common)
-        return self._run(u, b, Linear.few, lambda: tdx.tdx_causal_conv1d_step(conv), lambda: tdx.tdx_selective_scan_step(scan))
+        return self._run(u, b, Linear.few, (tdx.tdx_causal_conv1d_step, conv), (tdx.tdx_selective_scan_step, scan))
 
     def between_gradients(self, keep, dy):
         """Gradients of what stands between the projections for a gradient dy of the scan's output: d conv input, d dt, d B, d C, d z and
@@ -125,16 +131,15 @@ class Layer:
         g = {"dx": e(self.D), "ddt": e(self.D), "dB": e(self.N), "dC": e(self.N), "dz": e(self.D)}
         p = {"dA": torch.empty_like(self.A), "dD": torch.empty_like(self.skip), "ddt_bias": torch.empty_like(self.dt_bias)}
         scan.set(dout=dy, ld_dout=dy.stride(0), **g, **{"ld_" + k: v.stride(0) for k, v in g.items()}, **p, state_out=None)
-        tdx.check(tdx.tdx_selective_scan_bwd(scan))
+        _call(tdx.tdx_selective_scan_bwd, scan)
         g["dconv_in"], p["dconv_w"], p["dconv_b"] = e(self.D), torch.empty_like(self.conv_w), torch.empty_like(self.conv_b)
         conv.set(dy=g["dx"], ld_dy=self.D, dx=g["dconv_in"], ld_dx=self.D, dweight=p["dconv_w"], dbias=p["dconv_b"], state_out=None)
         status, size = tdx.tdx_causal_conv1d_workspace_size(conv)
         tdx.check(status)
         workspace = torch.empty(size, dtype=torch.uint8, device="cuda")
         conv.set(workspace=workspace, workspace_bytes=size)
-        tdx.check(tdx.tdx_causal_conv1d_bwd(conv))
+        _call(tdx.tdx_causal_conv1d_bwd, conv)
         assert b["y"].shape == dy.shape
-        torch.cuda.synchronize()                            # `workspace` is let go
         return g | p
 
 
@@ -173,7 +178,7 @@ def main(argv=None):
     u = torch.randn(sum(lengths), layer.E, device="cuda").to(BF16)
     layer.prompts(u, lengths, layer.cache(len(lengths)), list(range(len(lengths))), keep)
     grads = layer.between_gradients(keep, torch.randn(sum(lengths), layer.D, device="cuda").to(BF16))
-    tdx.check(tdx.tdx_check_device_status())
+    _call(tdx.tdx_check_device_status)
     print("gradients:", ", ".join(f"{k} {v.float().norm():.3g}" for k, v in grads.items()))
 
 

@@ -44,3 +44,57 @@ def test_gradients_between_the_projections():
 def test_the_command(capsys):
     main(["--width", "128", "--lengths", "9,0,17", "--tokens", "2"])
     assert "gradients" in capsys.readouterr().out
+
+
+def test_on_another_stream():
+    """Inputs that the side stream makes late, and states and buffers that it alone touches: the bits of the default stream."""
+    layer, lengths = Layer(128), [30, 1, 7]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    u, one = (torch.randn(n, layer.E, generator=g, device="cuda").to(torch.bfloat16) for n in (38, 3))
+
+    def both():
+        cache, b, slots = layer.cache(3), layer.buffers(3), torch.tensor([2, 0, 1], dtype=torch.int32, device="cuda")
+        outs = [layer.prompts(u * 1.0, lengths, cache, [2, 0, 1]).clone()]
+        for _ in range(3):
+            outs.append(layer.tokens(one * 1.0, cache, slots, b).clone())
+        return outs + list(cache)
+
+    want = both()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)                        # about 10 ms: what runs elsewhere runs before it
+        got = both()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert tdx.tdx_check_device_status() == 0
+
+
+def test_single_tokens_in_a_graph():
+    """A captured token step, replayed, gives the bits of the calls one by one."""
+    layer, slots = Layer(128), torch.tensor([1, -1, 0, 3], dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    rows = torch.randn(5, 4, layer.E, generator=g, device="cuda").to(torch.bfloat16)
+    u = torch.zeros_like(rows[0])
+
+    def five(step, cache):
+        outs = []
+        for r in rows:
+            u.copy_(r)
+            outs.append(step().clone())
+        return outs + [c.clone() for c in cache]
+
+    cache, b = layer.cache(4), layer.buffers(4)
+    want = five(lambda: layer.tokens(u, cache, slots, b), cache)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = layer.tokens(u, cache, slots, b)
+    for c in cache:
+        c.zero_()
+    got = five(lambda: graph.replay() or out, cache)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert (want[0][1] == 0).all() and tdx.tdx_check_device_status() == 0
