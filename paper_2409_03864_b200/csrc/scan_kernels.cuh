@@ -742,8 +742,8 @@ __global__ void __launch_bounds__(256) scan_bwd_join_kernel(const __grid_constan
         const long long e = (blockIdx.x * 256LL + threadIdx.x) * 4, total = p.rows * per_row;
         if (e >= total) return;
         const long long row = e / per_row;
-        // rows outside every sequence have no sums
-        if (p.offsets != nullptr && (row < __ldg(p.offsets) || row >= __ldg(p.offsets + p.batch))) return;
+        // rows outside every sequence, and those of a sequence that was skipped, have no sums
+        if (p.offsets != nullptr && !seq_has_row(p.offsets, p.batch, p.max_len, p.rows, row)) return;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
         for (int k = 0; k < p.sum_tiles; ++k) {

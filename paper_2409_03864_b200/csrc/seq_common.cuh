@@ -144,6 +144,9 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
 // Sequence b occupies rows [first, first + len).  Without offsets the batch is dense.  Offsets live on the device, so the
 // kernels check them: a sequence that leaves [0, rows) or is longer than max_len is reported and treated as empty.
 struct SeqRange { long long first; int len; };
+__device__ __forceinline__ bool seq_accepted(int lo, int hi, long long max_len, long long rows) {
+    return lo >= 0 && hi >= lo && hi <= rows && hi - lo <= max_len;
+}
 __device__ __forceinline__ SeqRange seq_range(const int* __restrict__ offsets, long long b, long long max_len, long long rows, int* status) {
     SeqRange r;
     if (offsets == nullptr) {
@@ -152,7 +155,7 @@ __device__ __forceinline__ SeqRange seq_range(const int* __restrict__ offsets, l
         return r;
     }
     const int lo = __ldg(offsets + b), hi = __ldg(offsets + b + 1);
-    if (lo < 0 || hi < lo || hi > rows || hi - lo > max_len) {
+    if (!seq_accepted(lo, hi, max_len, rows)) {
         atomicCAS(status, 0, kStatusSequence);
         r.first = 0;
         r.len = 0;
@@ -188,6 +191,17 @@ __device__ __forceinline__ SeqPiece seq_piece(const int* __restrict__ offsets, l
     const long long index = i - (__ldg(offsets + lo) / piece + lo);
     r.index = index < 0 || index > kNoPiece ? kNoPiece : static_cast<int>(index);   // in front of the first sequence: no rows
     return r;
+}
+// Whether a row belongs to a sequence that was worked on: the last one that starts at or before it.
+__device__ __forceinline__ bool seq_has_row(const int* __restrict__ offsets, long long batch, long long max_len, long long rows, long long row) {
+    long long lo = 0, hi = batch - 1;
+    while (lo < hi) {
+        const long long mid = (lo + hi + 1) / 2;
+        if (__ldg(offsets + mid) <= row) lo = mid;
+        else hi = mid - 1;
+    }
+    const int from = __ldg(offsets + lo), to = __ldg(offsets + lo + 1);
+    return from <= row && row < to && seq_accepted(from, to, max_len, rows);
 }
 // Slot of sequence (or batch row) b in the state tensors; negative: it has no state.
 __device__ __forceinline__ long long state_slot(const int* __restrict__ slots, long long b, long long n_slots, int* status) {

@@ -372,3 +372,24 @@ def test_empty_problems():
     p.backward()
     p.check_backward()
     assert all((t == 0).all() for t in p.p.values())
+
+
+@pytest.mark.parametrize("groups", [1, 2])
+def test_rows_of_a_rejected_sequence_get_no_gradients(groups):
+    """A sequence in the middle is longer than max_len: everything else is as if it were not there, and its rows stay what they are."""
+    lengths, d, n = [40, 300, 50], 40, 16
+    p = Problem("f32", n, d, lengths, True, groups, with_states=False)
+    p.args.set(max_len=100)
+    p.v["seqs"] = [p.v["seqs"][0], (40, 0), p.v["seqs"][2]]
+    p.forward(save=True)
+    assert tdx.tdx_check_device_status() == tdx.TDX_ERR_BOUNDS
+    p.backward(with_state=False)
+    assert tdx.tdx_check_device_status() == tdx.TDX_ERR_BOUNDS
+    o, m = ref.scan(**p.v, dout=p.dout), ref.scan(**p.v, dout=p.dout, magnitude=True)
+    inside = np.r_[0:40, 340:390]
+    for k, t in {"out": p.out, **p.g}.items():
+        factor = p.f["out" if k == "out" else "over_channels" if k in ("dB", "dC") else "grad"]
+        assert_close(k, t.host()[inside], o[k][inside], m[k][inside], factor)
+        assert np.isnan(t.host()[40:340]).all(), k
+    for k, t in p.p.items():
+        assert_close(k, t.double().cpu().numpy(), o[k], m[k], p.f["over_rows"])
