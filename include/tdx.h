@@ -255,7 +255,9 @@ int tdx_conv2d_bias_relu_ex(int64_t N, int64_t H, int64_t W, int64_t Cin, int64_
  *  - Sequences: seq_offsets = NULL is a dense batch of `batch` sequences of max_len rows each (rows = batch * max_len).
  *    Otherwise sequence b has the rows seq_offsets[b] .. seq_offsets[b + 1] - 1 (device memory, batch + 1 values, ascending),
  *    none longer than max_len; empty ones are allowed, and rows outside every sequence are neither read nor written.  A
- *    sequence that leaves [0, rows) or exceeds max_len is skipped and reported by tdx_check_device_status (TDX_ERR_BOUNDS).
+ *    sequence that leaves [0, rows) or exceeds max_len is treated as an empty one (its rows are neither read nor written) and
+ *    reported by tdx_check_device_status (TDX_ERR_BOUNDS).  Offsets that do not ascend are reported too, but which of the
+ *    call's other sequences are then computed is not specified; nothing outside the tensors is touched.
  *  - States: the state of sequence b is in slot slots[b] (device memory; NULL: slot b) of a tensor of n_slots slots that are
  *    state_stride elements apart (0: dense).  A negative slot means that the sequence has no state: nothing is read (zeros
  *    are taken) or written.  A slot >= n_slots is treated like a negative one and reported as above.  No two sequences

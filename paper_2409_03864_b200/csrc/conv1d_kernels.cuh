@@ -100,7 +100,9 @@ __global__ void __launch_bounds__(128, KW <= 4 ? 5 : 2) conv1d_fwd_kernel(const 
     seq_grid_wait();
     const long long bid = blockIdx.x;
     const int ct = static_cast<int>(bid % p.channel_tiles);
-    const SeqPiece at = seq_piece(p.offsets, p.batch, p.dense, kConvRuns * kConvRows, bid / p.channel_tiles);
+    const long long number = bid / p.channel_tiles;
+    const SeqPiece at = seq_piece(p.offsets, p.batch, p.dense, kConvRuns * kConvRows, number);
+    if (ct == 0) seq_check(p.offsets, number, p.batch, p.max_len, p.rows, p.status);
     const long long b = at.b;
     const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
     const long long c = (static_cast<long long>(ct) * 32 + lane) * VEC;
@@ -182,6 +184,7 @@ __global__ void __launch_bounds__(128, KW <= 4 ? 4 : 2) conv1d_bwd_kernel(const 
     const int ct = static_cast<int>(bid % p.channel_tiles);
     const long long number = bid / p.channel_tiles;
     const SeqPiece at = seq_piece(p.offsets, p.batch, p.dense, kConvRuns * kConvBwdRows, number);
+    if (ct == 0) seq_check(p.offsets, number, p.batch, p.max_len, p.rows, p.status);
     const long long b = at.b;
     const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
     const long long c = (static_cast<long long>(ct) * 32 + lane) * VEC;

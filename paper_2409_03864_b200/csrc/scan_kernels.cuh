@@ -108,6 +108,7 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanParams& p) {
     r.number = bid / per_chunk;
     const int ct = static_cast<int>(bid - r.number * per_chunk);
     const SeqPiece piece = seq_piece(p.offsets, p.batch, p.dense, p.chunk, r.number);
+    if (ct == 0) seq_check(p.offsets, r.number, p.batch, p.max_len, p.rows, p.status);
     r.b = piece.b;
     r.chunk = piece.index;
     r.group = ct / p.channel_tiles;

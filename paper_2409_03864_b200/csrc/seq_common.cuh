@@ -192,6 +192,11 @@ __device__ __forceinline__ SeqPiece seq_piece(const int* __restrict__ offsets, l
     r.index = index < 0 || index > kNoPiece ? kNoPiece : static_cast<int>(index);   // in front of the first sequence: no rows
     return r;
 }
+// seq_piece relies on ascending offsets: where they do not ascend, some sequences are found by no piece.  So that they are reported
+// all the same, one thread of the pieces 0 .. batch - 1 (there are at least as many) looks at the sequence of the piece's number.
+__device__ __forceinline__ void seq_check(const int* __restrict__ offsets, long long number, long long batch, long long max_len, long long rows, int* status) {
+    if (offsets != nullptr && threadIdx.x == 0 && number < batch) seq_range(offsets, number, max_len, rows, status);
+}
 // Whether a row belongs to a sequence that was worked on: the last one that starts at or before it.
 __device__ __forceinline__ bool seq_has_row(const int* __restrict__ offsets, long long batch, long long max_len, long long rows, long long row) {
     long long lo = 0, hi = batch - 1;

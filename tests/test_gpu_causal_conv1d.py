@@ -329,3 +329,20 @@ def test_single_tokens_of_width_one_need_neither_states_nor_slots(dtype):
     assert tdx.tdx_check_device_status() == 0
     there = np.array([1, 0, 1, 1, 0])[:, None]
     assert_close("y", y.host(), o["y"] * there, m["y"] * there, forward_factor(1), dtype)
+
+
+@pytest.mark.parametrize("offsets", [[0, 1000, 500, 2000], [0, 5000, 100, 2000], [0, 2000, -7, 1500], [1990, 3, 1000, 900]])
+def test_offsets_that_do_not_ascend_are_reported(offsets):
+    """Each call reports them, wherever they stand, and writes only into its tensors."""
+    d, rows = 32, 2000
+    x, y, dx = Rows(np.ones((rows, d)), "f32"), Rows(np.zeros((rows, d)), "f32", 3), Rows(np.zeros((rows, d)), "f32", 3)
+    w, off, dweight = f32(np.ones((d, 4))), i32(offsets), f32(np.zeros((d, 4)))
+    a = tdx.tdx_conv1d_args(batch=3, max_len=rows, rows=rows, channels=d, width=4, dtype=tdx.TDX_F32, silu=1, x=x.ptr, ld_x=x.ld, weight=w, y=y.ptr, ld_y=y.ld,
+                            seq_offsets=off, dy=x.ptr, ld_dy=x.ld, dx=dx.ptr, ld_dx=dx.ld, dweight=dweight)
+    ws = workspace(tdx.tdx_causal_conv1d_workspace_size(a))
+    a.set(workspace=ws, workspace_bytes=ws.numel())
+    tdx.check(tdx.tdx_causal_conv1d(a))
+    assert tdx.tdx_check_device_status() == tdx.TDX_ERR_BOUNDS
+    tdx.check(tdx.tdx_causal_conv1d_bwd(a))
+    assert tdx.tdx_check_device_status() == tdx.TDX_ERR_BOUNDS
+    assert x.guards_intact() and y.guards_intact() and dx.guards_intact()

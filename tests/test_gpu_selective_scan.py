@@ -393,3 +393,24 @@ def test_rows_of_a_rejected_sequence_get_no_gradients(groups):
         assert np.isnan(t.host()[40:340]).all(), k
     for k, t in p.p.items():
         assert_close(k, t.double().cpu().numpy(), o[k], m[k], p.f["over_rows"])
+
+
+@pytest.mark.parametrize("channels", [32, 4800])            # cut into chunks, and one chunk a sequence
+@pytest.mark.parametrize("offsets", [[0, 1000, 500, 2000], [0, 5000, 100, 2000], [0, 2000, -7, 1500], [1990, 3, 1000, 900]])
+def test_offsets_that_do_not_ascend_are_reported(offsets, channels):
+    """Each call reports them, wherever they stand, and writes only into its tensors."""
+    rows, n = 2000, 4
+    dev = {k: Rows(np.full((rows, w), 0.5), "f32") for k, w in (("x", channels), ("dt", channels), ("B", n), ("C", n), ("dout", channels))}
+    outs = {k: Rows(np.zeros((rows, w)), "f32", 4) for k, w in (("out", channels), ("dx", channels), ("ddt", channels), ("dB", n), ("dC", n))}
+    off, A, dA = i32(offsets), f32(-np.ones((channels, n))), f32(np.zeros((channels, n)))
+    a = tdx.tdx_scan_args(batch=3, max_len=rows, rows=rows, channels=channels, states=n, groups=1, dtype=tdx.TDX_F32, dt_softplus=1, A=A, dA=dA, seq_offsets=off,
+                          **{k: t.ptr for k, t in {**dev, **outs}.items()}, **{"ld_" + k: t.ld for k, t in {**dev, **outs}.items()})
+    saved = workspace(tdx.tdx_selective_scan_saved_size(a))
+    a.set(saved=saved, saved_bytes=saved.numel())
+    ws = workspace(tdx.tdx_selective_scan_workspace_size(a))
+    a.set(workspace=ws, workspace_bytes=ws.numel())
+    tdx.check(tdx.tdx_selective_scan(a))
+    assert tdx.tdx_check_device_status() == tdx.TDX_ERR_BOUNDS
+    tdx.check(tdx.tdx_selective_scan_bwd(a))
+    assert tdx.tdx_check_device_status() == tdx.TDX_ERR_BOUNDS
+    assert all(t.guards_intact() for t in {**dev, **outs}.values())
