@@ -160,6 +160,54 @@ __device__ __forceinline__ void scan_sum(const float* p, float (&s)[VEC]) {
 
 enum ScanMode { kScanFull = 0, kScanState = 1, kScanAdjoint = 2 };
 
+// States and channels that only fill up a thread or a block have a, B and C of zero and add nothing, as long as all is finite: an
+// infinity (or an overflow) times their zeros is not a number, which stays in their states and spoils the sums.  Their states are
+// zero by right, so that a look at them behind each tile shows it, and the tile is then gone through again with them kept at zero,
+// by a function of its own that takes nothing from the kernel's loops.  (4096 x 4096 x 16 forward and 8192 x 2048 x 16 training: a
+// look at every element in front of the tile cost 3.6 and 3.2 percent, the second walk as a part of the kernel 0.9 and 1.3, this form nothing;
+// with states or channels to fill up it costs up to 5 percent.)
+// States n and n + 1 of v:
+__device__ __forceinline__ f32x2 scan_keep(f32x2 v, int n, int states) {
+    const f32x2 low = n < states ? 0xffffffffull : 0ull, high = n + 1 < states ? 0xffffffff00000000ull : 0ull;
+    return v & (low | high);
+}
+__device__ __forceinline__ bool scan_spoilt(const f32x2 (&v)[2], int n0, int states) {
+    return v[0] != scan_keep(v[0], n0, states) || v[1] != scan_keep(v[1], n0 + 2, states);
+}
+struct ScanStates { f32x2 v[2]; };
+// A tile of the forward kernel again, from the states `h` in front of it; dt, b, c and y: the tile in shared memory, y from this
+// thread's first place on.
+template <int N, int MODE>
+__device__ __noinline__ ScanStates scan_again(ScanStates h, ScanStates a, const float4* dt, const float* b, const float* c, float* y, int ch, int n0,
+                                              int states, float* saved, long long save_step, int left) {
+    constexpr int kRows = ScanShape<N>::kRows, kCh = ScanShape<N>::kChannels;
+    constexpr bool kBack = MODE == kScanAdjoint;
+#pragma unroll 1
+    for (int r = 0; r < kRows; ++r) {
+        if (MODE == kScanFull && r % kScanSave == 0 && saved) {
+            if (r < left) scan_store_states(saved, h.v);
+            saved += save_step;
+        }
+        const int row = kBack ? kRows - 1 - r : r;
+        const ulonglong2 d = *reinterpret_cast<const ulonglong2*>(dt + row * kCh + ch);
+        f32x2 bv[2], cv[2], sum = 0;
+        scan_load_pairs(b + row * N + n0, bv);
+        if (MODE == kScanFull) scan_load_pairs(c + row * N + n0, cv);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const f32x2 w = exp2_pair(mul2(d.x, a.v[i])), u = mul2(d.y, bv[i]);
+            h.v[i] = scan_keep(kBack ? mul2(w, add2(u, h.v[i])) : fma2(w, h.v[i], u), n0 + 2 * i, states);
+            if (MODE == kScanFull) sum = i == 0 ? mul2(h.v[i], cv[i]) : fma2(h.v[i], cv[i], sum);
+        }
+        if (MODE == kScanFull) {
+            float lo, hi;
+            unpack2(sum, lo, hi);
+            y[r * kCh] = lo + hi;
+        }
+    }
+    return h;
+}
+
 // kScanFull: the forward pass over a chunk, from the state before it.
 // kScanState: only the state that a chunk adds to what comes before it, h from h = 0, and the sum of dt'.  (The chunk's
 //   effect on an incoming state is then exp(A * sum dt').)  Run first when a sequence is cut into chunks, for all chunks but
@@ -169,8 +217,12 @@ enum ScanMode { kScanFull = 0, kScanState = 1, kScanAdjoint = 2 };
 // VEC neighbouring channels (2 where the rows' alignment allows) are one element of the elementwise work, which is as long as the
 // recurrence itself unless its addresses and checks are kept cheap: a thread's offsets in a tile are computed once, and a full
 // tile is read without checks.
+// Blocks per SM that the register bound asks for; 0: no bound.  Three where they fit without spills and the compiler would take more (8
+// states in bf16, two channels an access: 81 us instead of 107 for 2 x 2048 rows of 2048 channels); one with 32 states, where its
+// own choice is less than two blocks may have (146 us instead of 158).
+constexpr int scan_fwd_blocks(int n, int vec, int elem_bytes) { return n == 64 || (n == 8 && vec == 2 && elem_bytes == 2) ? 3 : n == 32 ? 1 : 0; }
 template <typename T, int N, int MODE, int VEC>
-__global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(const __grid_constant__ ScanParams p) {
+__global__ void __launch_bounds__(kScanThreads, scan_fwd_blocks(N, VEC, sizeof(T))) scan_fwd_kernel(const __grid_constant__ ScanParams p) {
     typedef ScanShape<N> Shape;
     typedef SeqVec<T, VEC> raw_t;
     constexpr int kRows = Shape::kRows, kCh = Shape::kChannels, kPer = Shape::kPer, S = kScanStates, P = S / 2;
@@ -226,7 +278,7 @@ __global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(const __grid_con
     f32x2 h[P], a[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        h[i] = pack2(hv[2 * i], hv[2 * i + 1]);
+        h[i] = scan_keep(pack2(hv[2 * i], hv[2 * i + 1]), n0 + 2 * i, p.states);
         a[i] = pack2(av[2 * i], av[2 * i + 1]);
     }
 
@@ -348,6 +400,7 @@ __global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(const __grid_con
             s_y[per][r][ch] = lo + hi;
         }
     };
+    const bool padded = p.states < N;                    // see scan_again
     if (tiles > 0) fetch(first_row);
     for (int tile = 0; tile < tiles; ++tile) {
         const int row0 = kBack ? first_row - tile * kRows : first_row + tile * kRows, left = min(t1 - row0, kRows);
@@ -369,6 +422,8 @@ __global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(const __grid_con
         }
         __syncthreads();
         if (tile + 1 < tiles) fetch(kBack ? row0 - kRows : row0 + kRows);
+        const ScanStates before = {{h[0], h[1]}};
+        float* saved_before = saved;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) load_row(k, dv[0][k], bv[0][k]);
 #pragma unroll
@@ -389,6 +444,12 @@ __global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(const __grid_con
                 if (g + 1 < kGroups) decay_row((g + 1) * kAhead + k, dv[next][k], bv[next][k], w[next][k], u[next][k], cv[next][k]);
                 walk_row(g * kAhead + k, w[now][k], u[now][k], cv[now][k]);
             }
+        }
+        if (padded && scan_spoilt(h, n0, p.states)) {
+            const ScanStates again = scan_again<N, MODE>(before, {{a[0], a[1]}}, &s_dt[0][0], &s_b[0][0], &s_c[0][0], &s_y[MODE == kScanFull ? per : 0][0][ch], ch,
+                                                         n0, p.states, saved_before, save_step, left);
+            h[0] = again.v[0];
+            h[1] = again.v[1];
         }
         __syncthreads();
         if (MODE == kScanFull) {
@@ -467,6 +528,67 @@ __device__ __forceinline__ void scan_sum_lanes(const float4* list, int lane, flo
     if (there) out[2 * odd + second] = mine;
 }
 
+// A tile of the backward kernel again, with the states that only fill up kept at zero, and the sum of dA over the tile's own rows only
+// (dlog dt' is zero behind them only while dlog is finite).  h: states in front of the tile; q: gradient behind it; sum: this thread's
+// place for row 0 in s_sum.
+struct ScanBwdStates { ScanStates q, ta; };
+template <int N>
+__device__ __noinline__ ScanBwdStates scan_bwd_again(ScanStates h, ScanStates q, ScanStates a, const float2* dt, const float* g, const float* b, const float* c,
+                                                     float* sum, float4* list, int ch, int n0, int states, int left, float* part_bc, long long bc_step) {
+    constexpr int kRows = kScanSave, kCh = ScanShape<N>::kChannels, kSum = ScanShape<N>::kPer * kRows * kCh;
+    const int lane = threadIdx.x & 31;
+    f32x2 hs[kRows + 1][2], w[kRows][2];
+    ScanBwdStates r = {q, {{0, 0}}};
+    hs[0][0] = h.v[0];
+    hs[0][1] = h.v[1];
+#pragma unroll 1
+    for (int t = 0; t < kRows; ++t) {
+        const float2 d = dt[t * kCh + ch];
+        f32x2 bv[2];
+        scan_load_pairs(b + t * N + n0, bv);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            w[t][i] = scan_keep(exp2_pair(mul2(pack2(d.x, d.x), a.v[i])), n0 + 2 * i, states);
+            hs[t + 1][i] = scan_keep(fma2(w[t][i], hs[t][i], mul2(pack2(d.y, d.y), bv[i])), n0 + 2 * i, states);
+        }
+    }
+#pragma unroll 1
+    for (int t = kRows - 1; t >= 0; --t) {
+        const float2 d = dt[t * kCh + ch];
+        const float gv = g[t * kCh + ch];
+        f32x2 bv[2], cv[2], db[2], dc[2], y = 0, du = 0, dl = 0;
+        scan_load_pairs(b + t * N + n0, bv);
+        scan_load_pairs(c + t * N + n0, cv);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const f32x2 dh = scan_keep(fma2(pack2(gv, gv), cv[i], r.q.v[i]), n0 + 2 * i, states);
+            r.q.v[i] = mul2(w[t][i], dh);
+            const f32x2 dlog = mul2(r.q.v[i], hs[t][i]);
+            if (t < left) r.ta.v[i] = fma2(dlog, pack2(d.x, d.x), r.ta.v[i]);
+            y = i == 0 ? mul2(hs[t + 1][i], cv[i]) : fma2(hs[t + 1][i], cv[i], y);
+            du = i == 0 ? mul2(dh, bv[i]) : fma2(dh, bv[i], du);
+            dl = i == 0 ? mul2(dlog, a.v[i]) : fma2(dlog, a.v[i], dl);
+            db[i] = mul2(dh, pack2(d.y, d.y));
+            dc[i] = mul2(hs[t + 1][i], pack2(gv, gv));
+        }
+        float lo, hi;
+        unpack2(y, lo, hi);
+        sum[t * kCh] = lo + hi;
+        unpack2(dl, lo, hi);
+        sum[kSum + t * kCh] = lo + hi;
+        unpack2(du, lo, hi);
+        sum[2 * kSum + t * kCh] = lo + hi;
+        *reinterpret_cast<ulonglong2*>(&list[(t % 4 * 2) * kScanSumPitch + lane]) = make_ulonglong2(db[0], db[1]);
+        *reinterpret_cast<ulonglong2*>(&list[(t % 4 * 2 + 1) * kScanSumPitch + lane]) = make_ulonglong2(dc[0], dc[1]);
+        if (t % 4 == 0) {
+            __syncwarp();
+            scan_sum_lanes<kCh>(list, lane, part_bc + t * bc_step, bc_step, N, left - t);
+            __syncwarp();
+        }
+    }
+    return r;
+}
+
 // Backward.  With g = dout * silu(z) (or dout), for one channel and state
 //   dh[t] = C[t] g[t] + a[t + 1] dh[t + 1],   a[t] = exp(dt'[t] A)
 //   dC[t] = sum_d g h,   dB[t] = sum_d dh dt' x,   dlog = dh a h[t - 1],   dA = sum_t dlog dt'
@@ -519,10 +641,11 @@ __global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(const __grid_con
             for (int i = 0; i < S; ++i) qv[i] = fmaf(qv[i], fast_exp2(av[i] * sum), add[i]);
         }
     }
+    const int live_states = live ? p.states : 0;
     f32x2 q[P], a[P], da[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        q[i] = pack2(qv[2 * i], qv[2 * i + 1]);
+        q[i] = scan_keep(pack2(qv[2 * i], qv[2 * i + 1]), n0 + 2 * i, p.states);
         a[i] = pack2(av[2 * i], av[2 * i + 1]);
         da[i] = pack2(0.f, 0.f);
     }
@@ -586,6 +709,7 @@ __global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(const __grid_con
     if (tiles > 0) fetch(t0 + (tiles - 1) * kRows);
     for (int tile = tiles - 1; tile >= 0; --tile) {
         const int row0 = t0 + tile * kRows, left = min(t1 - row0, kRows);
+        const bool padded = at.live < kCh || p.states < N || left < kRows;       // see scan_bwd_again
         // x, dt', d dt' / d dt, z, sigmoid(z), dout, g
         float ex[kEl][VEC], ed[kEl][VEC], eds[kEl][VEC], ez[kEl][VEC], ezs[kEl][VEC], eo[kEl][VEC], eg[kEl][VEC];
 #pragma unroll
@@ -626,6 +750,7 @@ __global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(const __grid_con
         for (int i = 0; i < P; ++i) hs[0][i] = pack2(rh[2 * i], rh[2 * i + 1]);
         __syncthreads();
         if (tile > 0) fetch(row0 - kRows);
+        const ScanStates behind = {{q[0], q[1]}};
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
             const ulonglong2 dv = dt_at(r, ch);
@@ -637,6 +762,7 @@ __global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(const __grid_con
                 hs[r + 1][i] = fma2(w[r][i], hs[r][i], mul2(dv.y, b[i]));
             }
         }
+        bool spoilt = padded && scan_spoilt(hs[kRows], n0, live_states);
         f32x2 ta[P];
 #pragma unroll
         for (int i = 0; i < P; ++i) ta[i] = pack2(0.f, 0.f);
@@ -672,6 +798,23 @@ __global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(const __grid_con
                 __syncwarp();
                 scan_sum_lanes<kCh>(list, lane, part_bc + (row0 + r) * bc_step, bc_step, N, left - r);
                 __syncwarp();
+            }
+        }
+        if (padded) {
+            spoilt |= scan_spoilt(q, n0, live_states);
+            if (left < kRows) {
+                float lo, hi;
+                unpack2(add2(ta[0], ta[1]), lo, hi);
+                spoilt |= lo + hi != lo + hi;
+            }
+            if (__any_sync(0xffffffffu, spoilt)) {         // lanes share the sums of dB and dC
+                const ScanBwdStates again = scan_bwd_again<N>({{hs[0][0], hs[0][1]}}, behind, {{a[0], a[1]}}, &s_dt[0][0], &s_g[0][0], &s_b[0][0], &s_c[0][0],
+                                                              &s_sum[0][per][0][ch], list, ch, n0, live_states, left, part_bc + row0 * bc_step, bc_step);
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    q[i] = again.q.v[i];
+                    ta[i] = again.ta.v[i];
+                }
             }
         }
 #pragma unroll
@@ -887,7 +1030,7 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const __grid_constant__ 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 h[i] = fmaf(fast_exp2(dd * aa[i]), h[i], uu * bv[i]);
-                part = fmaf(h[i], cv[i], part);
+                if (VEC4 || n0 + i < p.states) part = fmaf(h[i], cv[i], part);      // 0 * infinity is not a number
             }
             if (c < p.channels) {
                 if (VEC4) {

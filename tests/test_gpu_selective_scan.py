@@ -5,7 +5,7 @@ import torch
 
 import paper_2409_03864_b200 as tdx
 import seq_reference as ref
-from seq_util import DT, EPS, Rows, assert_close, f32, i32, offsets_of, seeded, workspace
+from seq_util import DT, EPS, TORCH, Rows, assert_close, f32, i32, offsets_of, seeded, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -414,3 +414,58 @@ def test_offsets_that_do_not_ascend_are_reported(offsets, channels):
     tdx.check(tdx.tdx_selective_scan_bwd(a))
     assert tdx.tdx_check_device_status() == tdx.TDX_ERR_BOUNDS
     assert all(t.guards_intact() for t in {**dev, **outs}.values())
+
+
+def assert_close_but_infinities(name, got, want, magnitude, factor, dtype="f32"):
+    """What is infinite or undefined is so on both sides; the rest is close."""
+    there = np.isfinite(want)
+    wrong = np.argwhere(~((got == want) | (np.isnan(got) & np.isnan(want))) & ~there)
+    assert not len(wrong), (name, wrong[0], got[tuple(wrong[0])], want[tuple(wrong[0])])
+    assert_close(name, got[there], want[there], magnitude[there], factor, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("where", ["x", "B", "C", "dt", "dout"])
+@pytest.mark.parametrize("n,d,length", [(3, 10, 21), (16, 10, 21), (20, 16, 24), (16, 64, 37), (3, 10, 150), (16, 33, 150)])
+def test_infinities_reach_what_depends_on_them_and_nothing_else(n, d, length, where, dtype):
+    """One infinity among positive inputs, so that sums over states and channels have a definite sign.  States and channels that fill
+    up a thread or a block, and rows behind the last of a tile, must add nothing."""
+    p = Problem(dtype, n, d, [length], False, with_states=False)
+    for k in ("x", "B", "C", "z", "D"):
+        p.v[k] = np.abs(p.v[k]) + 2.0 ** -4
+    p.v = {k: (torch.from_numpy(v).to(TORCH[dtype]).double().numpy() if k in ("x", "B", "C", "z") else v) for k, v in p.v.items()}
+    p.dout = np.abs(p.dout)
+    (p.dout if where == "dout" else p.v[where])[4, 1] = np.inf
+    for k, t in p.dev.items():
+        t.view[:] = torch.from_numpy(p.v[k]).cuda().to(TORCH[dtype])
+    p.par["D"].copy_(torch.from_numpy(p.v["D"]))
+    with np.errstate(all="ignore"):
+        o, m = ref.scan(**p.v, dout=p.dout), ref.scan(**p.v, dout=p.dout, magnitude=True)
+        p.forward(save=True)
+        p.backward(with_state=False)
+        got = {"out": p.out.host(), "state": p.new_state.host()[:1], **{k: t.host() for k, t in p.g.items()},
+               **{k: t.double().cpu().numpy() for k, t in p.p.items()}}
+        kind = {"out": "out", "state": "state", "dB": "over_channels", "dC": "over_channels", "dA": "over_rows", "dD": "over_rows", "ddt_bias": "over_rows"}
+        for k, v in got.items():
+            assert_close_but_infinities(k, v, o[k], m[k], p.f[kind.get(k, "grad")], dtype if k in ("out", "dx", "ddt", "dz", "dB", "dC") else "f32")
+    assert tdx.tdx_check_device_status() == 0
+
+
+@pytest.mark.parametrize("where", ["x", "B", "C", "dt"])
+@pytest.mark.parametrize("n,d", [(3, 10), (16, 40), (20, 33), (100, 5)])
+def test_infinities_in_single_tokens(n, d, where):
+    batch = 3
+    p = Problem("f32", n, d, [1] * batch, False)
+    for k in ("x", "B", "C", "z", "D", "state"):
+        p.v[k] = np.abs(p.v[k])
+    p.v[where][1, 1] = np.inf
+    for k, t in p.dev.items():
+        t.view[:] = torch.from_numpy(p.v[k]).cuda().float()
+    p.par["D"].copy_(torch.from_numpy(p.v["D"]))
+    state, out = Rows(p.v["state"], "f32"), Rows(np.zeros((batch, d)), "f32", fill=float("nan"))
+    p.args.set(out=out.ptr, ld_out=out.ld, state_in=state.ptr, state_out=state.ptr, n_slots=batch)
+    with np.errstate(all="ignore"):
+        o, m = ref.scan(**p.v), ref.scan(**p.v, magnitude=True)
+        tdx.check(tdx.tdx_selective_scan_step(p.args))
+        assert_close_but_infinities("out", out.host(), o["out"], m["out"], p.f["out"])
+        assert_close_but_infinities("state", state.host(), o["state"], m["state"], p.f["state"])
