@@ -71,6 +71,14 @@ def assert_close(name, got, want, magnitude, factor, dtype="f32"):
         raise AssertionError(f"{name}: {bad.sum()} of {bad.size} values off, first at {i}: {got[i]} instead of {want[i]}, tolerance {tol[i]:.3g}")
 
 
+def assert_close_but_infinities(name, got, want, magnitude, factor, dtype="f32"):
+    """What is infinite or undefined is so on both sides; the rest is close."""
+    there = np.isfinite(want)
+    wrong = np.argwhere(~((got == want) | (np.isnan(got) & np.isnan(want))) & ~there)
+    assert not len(wrong), (name, wrong[0], got[tuple(wrong[0])], want[tuple(wrong[0])])
+    assert_close(name, got[there], want[there], magnitude[there], factor, dtype)
+
+
 def workspace(answer):
     status, size = answer
     tdx.check(status)

@@ -5,7 +5,7 @@ import torch
 
 import paper_2409_03864_b200 as tdx
 import seq_reference as ref
-from seq_util import DT, EPS, Rows, assert_close, f32, i32, offsets_of, seeded, workspace
+from seq_util import DT, EPS, TORCH, Rows, assert_close, assert_close_but_infinities, f32, i32, offsets_of, seeded, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -346,3 +346,30 @@ def test_offsets_that_do_not_ascend_are_reported(offsets):
     tdx.check(tdx.tdx_causal_conv1d_bwd(a))
     assert tdx.tdx_check_device_status() == tdx.TDX_ERR_BOUNDS
     assert x.guards_intact() and y.guards_intact() and dx.guards_intact()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("width", [2, 4, 6])
+@pytest.mark.parametrize("where,value", [("x", np.inf), ("x", -np.inf), ("x", np.nan), ("dy", np.inf), ("state", np.inf)])
+@pytest.mark.parametrize("silu", [0, 1])
+def test_infinities_reach_the_rows_of_their_filter_only(silu, where, value, width, dtype):
+    p = Problem(dtype, width, 36, [70, 9], True, silu=silu)
+    {"x": p.x, "dy": p.dy, "state": p.state.reshape(-1, 36)}[where][1 if where == "state" and width > 2 else 0 if where == "state" else 33, 3] = value
+    p.dev_x.view[:] = torch.from_numpy(p.x).cuda().to(TORCH[dtype])
+    p.all_states[:2] = p.state
+    p.dev_state.view[:] = torch.from_numpy(p.all_states.reshape(p.n_slots, -1)).cuda().to(TORCH[dtype])
+    with np.errstate(all="ignore"):
+        a = (p.x, p.weight, p.bias, silu, p.seqs, p.state)
+        o, m = ref.conv1d(*a, p.dy, p.dstate), ref.conv1d(*a, p.dy, p.dstate, magnitude=True)
+        if not silu:                                     # dx, dbias and dstate do not depend on x then, but the helper's sizes have 0 * |pre|
+            clean = [np.where(np.isfinite(v), v, 0.0) for v in (p.x, p.state)]
+            sizes = ref.conv1d(clean[0], p.weight, p.bias, silu, p.seqs, clean[1], p.dy, p.dstate, magnitude=True)
+            m |= {k: sizes[k] for k in ("dx", "dbias", "dstate")} | {"dweight": np.where(np.isnan(m["dweight"]), sizes["dweight"], m["dweight"])}
+        p.forward()
+        p.backward()
+        got = {"y": p.y.host(), "dx": p.dx.host(), "dweight": p.dweight.double().cpu().numpy(), "dbias": p.dbias.double().cpu().numpy(),
+               "state": p.new_state.host()[:2], "dstate": p.dstate_in.host()[:2]}
+        for k, v in got.items():
+            factor = forward_factor(width) if k == "y" else backward_factor(width, p.rows if k in ("dweight", "dbias") else 0)
+            assert_close_but_infinities(k, v, o[k], m[k], factor, "f32" if k in ("dweight", "dbias") else dtype)
+    assert tdx.tdx_check_device_status() == 0

@@ -164,3 +164,31 @@ def test_long_rows_and_small_groups(shape):
 def test_long_rows_and_small_groups_fp32():
     run("f32", 1, 4750, 10880, 32, True)
     run("f32", 1, 300, 10912, 32, False)
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("dtype,shape", [
+    # more than two sets of 16 rows per SM, a ragged last set, and more steps of K than a warp has in flight
+    ("bf16", (1, 4801, 10368, 128)), ("bf16", (8, 4740, 8192, 128)), ("bf16", (3, 4737, 10304, 64)), ("bf16", (5, 4752, 2112, 32)),
+    ("f32", (2, 4740, 5376, 128)), ("f32", (1, 4801, 10816, 64)),
+    # the same with one set a block
+    ("bf16", (1, 100, 16512, 128)), ("bf16", (2, 33, 16384, 64)), ("f32", (1, 50, 10880, 32)),
+])
+def test_many_rows_of_weights_and_long_sums(dtype, shape, zeros):
+    run(dtype, *shape, zeros)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,group", [(2, 64), (20, 128), (3, 48)])
+def test_zeros_of_a_whole_byte(m, group, dtype):
+    """A zero may be any byte; q - zero is then up to 255 in size."""
+    rng = np.random.default_rng(6)
+    n, k = 40, 384
+    x, weight = seeded(rng, (m, k), dtype), rng.integers(0, 256, (n, k // 2), dtype=np.uint8)
+    scales, z = seeded(rng, (n, k // group), dtype, lo=0.01, hi=0.1), rng.integers(0, 256, (n, k // group), dtype=np.uint8)
+    dx, y, dw, dz = Rows(x, dtype), Rows(np.zeros((m, n)), dtype), torch.from_numpy(weight).cuda(), torch.from_numpy(z).cuda()
+    ds = torch.from_numpy(scales).cuda().to(TORCH[dtype])
+    a = tdx.tdx_w4_args(M=m, N=n, K=k, group_size=group, dtype=DT[dtype], x=dx.ptr, ld_x=k, weight=dw, scales=ds, zeros=dz, y=y.ptr, ld_y=n)
+    tdx.check(tdx.tdx_gemm_w4(a))
+    w = ref.unpack_w4(weight, scales, z, k, group)
+    assert_close("y", y.host(), x @ w.T, np.abs(x) @ np.abs(w).T, (k + 8) * EPS, dtype)

@@ -5,7 +5,7 @@ import torch
 
 import paper_2409_03864_b200 as tdx
 import seq_reference as ref
-from seq_util import DT, EPS, TORCH, Rows, assert_close, f32, i32, offsets_of, seeded, workspace
+from seq_util import DT, EPS, TORCH, Rows, assert_close, assert_close_but_infinities, f32, i32, offsets_of, seeded, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -416,14 +416,6 @@ def test_offsets_that_do_not_ascend_are_reported(offsets, channels):
     assert all(t.guards_intact() for t in {**dev, **outs}.values())
 
 
-def assert_close_but_infinities(name, got, want, magnitude, factor, dtype="f32"):
-    """What is infinite or undefined is so on both sides; the rest is close."""
-    there = np.isfinite(want)
-    wrong = np.argwhere(~((got == want) | (np.isnan(got) & np.isnan(want))) & ~there)
-    assert not len(wrong), (name, wrong[0], got[tuple(wrong[0])], want[tuple(wrong[0])])
-    assert_close(name, got[there], want[there], magnitude[there], factor, dtype)
-
-
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("where", ["x", "B", "C", "dt", "dout"])
 @pytest.mark.parametrize("n,d,length", [(3, 10, 21), (16, 10, 21), (20, 16, 24), (16, 64, 37), (3, 10, 150), (16, 33, 150)])
@@ -469,3 +461,59 @@ def test_infinities_in_single_tokens(n, d, where):
         tdx.check(tdx.tdx_selective_scan_step(p.args))
         assert_close_but_infinities("out", out.host(), o["out"], m["out"], p.f["out"])
         assert_close_but_infinities("state", state.host(), o["state"], m["state"], p.f["state"])
+
+
+LONGER = [
+    # states, channels, lengths: every block goes through three tiles of rows or more
+    (16, 1600, [100] * 3),           # one chunk a sequence: tiles of 32 rows
+    (32, 800, [100] * 3),
+    (8, 3200, [60] * 3),             # 16 rows
+    (64, 400, [60] * 3),
+    (4, 6400, [40] * 3),             # 8 rows
+    (128, 200, [40] * 3),
+    (12, 1600, [100] * 3),           # states that do not fill up the last thread
+    (16, 3200, [500]),               # chunks of 128 rows
+    (32, 1600, [500]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", LONGER)
+def test_many_tiles_a_block(shape, dtype):
+    n, d, lengths = shape
+    p = Problem(dtype, n, d, lengths, False)
+    p.forward(save=True)
+    p.check_forward()
+    p.backward()
+    # Among so many values some lie next to the root of silu'(z) = s (1 + z (1 - s)), whose rounding goes by the size of the terms
+    # of the sum, not by the sum: dz is compared with that size, and taken out of the common check.
+    extra = {"dout": p.dout, "dstate": p.dstate}
+    o, m = ref.scan(**p.v, **extra), ref.scan(**p.v, **extra, magnitude=True)
+    z, s = p.v["z"], ref.sigmoid(p.v["z"])
+    y = m["out"] / np.abs(z * s)
+    assert_close("dz", p.g["dz"].host(), o["dz"], np.abs(p.dout) * y * s * (1 + np.abs(z) * (1 - s)), p.f["grad"], dtype)
+    assert p.g.pop("dz").guards_intact()
+    p.check_backward()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d,batch", [(16, 4096, 100), (12, 4095, 100), (64, 4096, 40), (4, 9000, 50)])
+def test_single_tokens_of_many_rows(n, d, batch, dtype):
+    """More rows than the grid has: a warp goes through several of them, some without a slot."""
+    slots = [(5 * b) % (batch + 1) for b in range(batch)]
+    slots[batch // 2::9] = [-1] * len(slots[batch // 2::9])
+    p = Problem(dtype, n, d, [1] * batch, False, order=slots)
+    state, out = Rows(p.all_states, "f32"), Rows(np.zeros((batch, d)), dtype, 1, fill=float("nan"))
+    p.args.set(out=out.ptr, ld_out=out.ld, state_in=state.ptr, state_out=state.ptr)
+    tdx.check(tdx.tdx_selective_scan_step(p.args))
+    assert tdx.tdx_check_device_status() == 0
+    o, m = ref.scan(**p.v), ref.scan(**p.v, magnitude=True)
+    there = (np.array(slots) >= 0)[:, None]
+    assert_close("out", out.host(), o["out"] * there, m["out"] * there, p.f["out"], dtype)
+    got = state.host()
+    for b, s in enumerate(slots):
+        if s >= 0:
+            assert_close("state", got[s], o["state"][b], m["state"][b], p.f["state"])
+    for s in set(range(p.n_slots)) - set(slots):
+        assert np.array_equal(got[s], p.all_states[s])
+    assert out.guards_intact() and state.guards_intact()
