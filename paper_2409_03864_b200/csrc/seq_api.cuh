@@ -12,8 +12,7 @@ constexpr int64_t kSeqMaxLen = 1 << 30;
 // Programmatic stream serialization: the launch overlaps the tail of the kernel in front of it in the stream; every kernel
 // of this file waits for that kernel's end before it touches global memory.
 template <typename... Params, typename... Given>
-int launch_seq_cluster(void (*kernel)(Params...), int64_t grid_x, int64_t grid_y, int threads, size_t smem, int cluster, cudaStream_t st,
-                       const Given&... given) {
+int launch_seq(void (*kernel)(Params...), int64_t grid_x, int64_t grid_y, int threads, size_t smem, cudaStream_t st, const Given&... given) {
     if (grid_x > INT_MAX || grid_y > 65535) return fail(TDX_ERR_UNSUPPORTED, "problem too large for one launch");
     cudaLaunchConfig_t lc;
     std::memset(&lc, 0, sizeof lc);
@@ -21,21 +20,14 @@ int launch_seq_cluster(void (*kernel)(Params...), int64_t grid_x, int64_t grid_y
     lc.blockDim = dim3(static_cast<unsigned>(threads));
     lc.dynamicSmemBytes = smem;
     lc.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    lc.attrs = attr;
-    lc.numAttrs = cluster > 1 ? 2 : 1;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = &attr;
+    lc.numAttrs = 1;
     TDX_CUDA(cudaLaunchKernelEx(&lc, kernel, static_cast<Params>(given)...));
     g_launches.fetch_add(1);
     return TDX_OK;
-}
-template <typename... Params, typename... Given>
-int launch_seq(void (*kernel)(Params...), int64_t grid_x, int64_t grid_y, int threads, size_t smem, cudaStream_t st, const Given&... given) {
-    return launch_seq_cluster(kernel, grid_x, grid_y, threads, smem, 1, st, given...);
 }
 
 // Lets a kernel have more than 48 KB of shared memory: as much as there is, remembered per device, so that later calls skip it.
@@ -308,7 +300,7 @@ void plan_scan(tdx::ScanParams* p, int sm_count, bool back) {
     p->channel_tiles = static_cast<int>(ceil_div(p->group_channels, tdx::kScanThreads * 4 / n));
     const int64_t tiles = std::max<int64_t>(1, static_cast<int64_t>(p->channel_tiles) * p->groups);
     p->chunk = ceil_div(longest, 32) * 32;
-        if (tiles * side < sm_count) {
+    if (tiles * side < sm_count) {
         const int64_t want = ceil_div((back ? 2 : 3) * sm_count, tiles);                // chunks of all sequences together
         const int64_t chunk = std::max<int64_t>(64, ceil_div(ceil_div(p->offsets ? p->rows : longest * side, want), 32) * 32);
         if (chunk < p->chunk) p->chunk = chunk;
@@ -415,7 +407,7 @@ constexpr int kW4Warps = 16;         // of a staged block (see launch_w4_tiles)
 // What a block of w4_staged_kernel keeps in shared memory: the ring of weights, x, and `sets` times 16 rows of scales.
 template <typename T>
 size_t w4_staged_smem(const tdx::W4Params& p, int sets) {
-    return tdx::kW4RingBytes * 32 * kW4Warps + tdx::w4_x_bytes<T>(p.steps, p.M) + sizeof(float2) * static_cast<size_t>(tdx::kW4Rows * sets) * (p.groups + 1);
+    return tdx::kW4RingBytes * 32 * kW4Warps + tdx::w4_x_bytes<T>(p.steps, p.M) + sizeof(float2) * static_cast<size_t>(tdx::kW4Rows * sets) * tdx::w4_scale_pitch(p.groups);
 }
 template <typename T, int WORDS, int BLOCKS>
 int launch_w4_staged(tdx::W4Params p, cudaStream_t st) {

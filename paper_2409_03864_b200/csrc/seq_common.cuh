@@ -94,27 +94,6 @@ __device__ __forceinline__ float softplus_grad_f(float v, float& grad) {
     grad = (v >= 0.0f ? 1.0f : u) * fast_rcp(1.0f + u);
     return softplus_from_exp(v, u);
 }
-// sum of N consecutive floats of shared memory, in ascending order (16-byte loads where N allows)
-template <int N>
-__device__ __forceinline__ float sum_row(const float* p, float s) {
-    if (N % 4 == 0) {
-#pragma unroll
-        for (int i = 0; i < N; i += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(p + i);
-            s += (v.x + v.y) + (v.z + v.w);
-        }
-    } else if (N % 2 == 0) {
-#pragma unroll
-        for (int i = 0; i < N; i += 2) {
-            const float2 v = *reinterpret_cast<const float2*>(p + i);
-            s += v.x + v.y;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) s += p[i];
-    }
-    return s;
-}
 
 // ---------------------------------------------------------------- pairs of fp32 (one instruction for two values)
 typedef unsigned long long f32x2;

@@ -162,6 +162,8 @@ template <typename T>
 __host__ __device__ inline size_t w4_x_bytes(long long steps, long long rows_of_x) {
     return static_cast<size_t>(steps) * rows_of_x * W4Columns<T>::kPieces * kW4Step * 2;
 }
+// pairs (scale, offset) between two rows of W: an odd number, so that eight rows start in different banks
+__host__ __device__ constexpr int w4_scale_pitch(int groups) { return groups | 1; }
 constexpr size_t kW4RingBytes = 4 * 2 * 16;      // of a thread (kW4Depth steps); a warp's sums are never longer than its part
 
 // 16 bytes of x in shared memory: eight neighbouring k (an octet) of a row of x (of one piece of it) as pairs (j, j + 4).  Octet o of
@@ -338,7 +340,7 @@ __global__ void __launch_bounds__(512) w4_staged_kernel(const __grid_constant__ 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, threads = blockDim.x, g = lane >> 2, t = lane & 3;
     const long long n0 = blockIdx.x * static_cast<long long>(kW4Rows * BLOCKS);
     const int rows_of_x = static_cast<int>(p.M), first = min(p.steps, warp * p.per), count = min(p.steps, first + p.per) - first;
-    const int word_x = rows_of_x * kP * 4, pitch = p.groups + 1;       // an odd number of pairs: rows in different banks
+    const int word_x = rows_of_x * kP * 4, pitch = w4_scale_pitch(p.groups);
     uint4* ring = reinterpret_cast<uint4*>(w4_smem);
     uint4* xs = ring + kW4Depth * 2 * threads;
     float2* scales = reinterpret_cast<float2*>(xs + p.steps * 4 * word_x);
