@@ -305,7 +305,7 @@ void plan_scan(tdx::ScanParams* p, int sm_count, bool back) {
         const int64_t chunk = std::max<int64_t>(64, ceil_div(ceil_div(p->offsets ? p->rows : longest * side, want), 32) * 32);
         if (chunk < p->chunk) p->chunk = chunk;
     }
-    p->cut = p->max_len > p->chunk;
+    p->cut = longest > p->chunk;
     p->dense = std::max<int64_t>(1, ceil_div(p->max_len, p->chunk));
 }
 int64_t scan_numbers(const tdx::ScanParams& p) { return tdx::seq_pieces(p.offsets != nullptr, p.batch, p.rows, p.dense, p.chunk); }

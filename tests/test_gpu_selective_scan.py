@@ -517,3 +517,13 @@ def test_single_tokens_of_many_rows(n, d, batch, dtype):
     for s in set(range(p.n_slots)) - set(slots):
         assert np.array_equal(got[s], p.all_states[s])
     assert out.guards_intact() and state.guards_intact()
+
+
+@pytest.mark.parametrize("lengths", [[20, 0, 33, 1], [150, 0, 90, 3]])
+def test_a_generous_max_len_changes_nothing(lengths):
+    p = Problem("f32", 16, 40, lengths, True, order=[2, 0, 3, 1])
+    p.args.set(max_len=32768)
+    p.forward(save=True)
+    p.check_forward()
+    p.backward()
+    p.check_backward()

@@ -177,3 +177,9 @@ def test_a_packed_batch_of_no_sequences_has_no_work():
 
 def test_slots_of_a_step_without_states_are_checked_too():
     assert tdx.tdx_causal_conv1d_step(conv(width=1, slots=P + 2, n_slots=0)) == ALIGNMENT
+
+
+def test_a_generous_max_len_does_not_cut_short_sequences():
+    """No sequence is longer than all rows together, so a scan of few rows needs no workspace whatever max_len allows."""
+    st, n = tdx.tdx_selective_scan_workspace_size(scan(seq_offsets=P, rows=60, max_len=32768, saved=None))
+    assert (st, n) == (tdx.TDX_OK, 0)
