@@ -89,9 +89,10 @@ __device__ __forceinline__ void scan_load_pairs(const float* p, f32x2 (&v)[2]) {
     const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(p);
     v[0] = q.x; v[1] = q.y;
 }
-__device__ __forceinline__ f32x2 exp2_pair(f32x2 e) {
+constexpr float kDecayAddend = 2.4e-8f;
+__device__ __forceinline__ f32x2 scan_decay(f32x2 dt, f32x2 a) {
     float lo, hi;
-    unpack2(e, lo, hi);
+    unpack2(fma2(dt, a, pack2(kDecayAddend, kDecayAddend)), lo, hi);
     return pack2(fast_exp2(lo), fast_exp2(hi));
 }
 
@@ -195,7 +196,7 @@ __device__ __noinline__ ScanStates scan_again(ScanStates h, ScanStates a, const 
         if (MODE == kScanFull) scan_load_pairs(c + row * N + n0, cv);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const f32x2 w = exp2_pair(mul2(d.x, a.v[i])), u = mul2(d.y, bv[i]);
+            const f32x2 w = scan_decay(d.x, a.v[i]), u = mul2(d.y, bv[i]);
             h.v[i] = scan_keep(kBack ? mul2(w, add2(u, h.v[i])) : fma2(w, h.v[i], u), n0 + 2 * i, states);
             if (MODE == kScanFull) sum = i == 0 ? mul2(h.v[i], cv[i]) : fma2(h.v[i], cv[i], sum);
         }
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(kScanThreads, scan_fwd_blocks(N, VEC, sizeof(T
         else sum_dt += __uint_as_float(static_cast<uint32_t>(d.x));
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            ww[i] = exp2_pair(mul2(d.x, a[i]));
+            ww[i] = scan_decay(d.x, a[i]);
             uu[i] = mul2(d.y, b[i]);
         }
     };
@@ -548,7 +549,7 @@ __device__ __noinline__ ScanBwdStates scan_bwd_again(ScanStates h, ScanStates q,
         scan_load_pairs(b + t * N + n0, bv);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            w[t][i] = scan_keep(exp2_pair(mul2(pack2(d.x, d.x), a.v[i])), n0 + 2 * i, states);
+            w[t][i] = scan_keep(scan_decay(pack2(d.x, d.x), a.v[i]), n0 + 2 * i, states);
             hs[t + 1][i] = scan_keep(fma2(w[t][i], hs[t][i], mul2(pack2(d.y, d.y), bv[i])), n0 + 2 * i, states);
         }
     }
@@ -758,7 +759,7 @@ __global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(const __grid_con
             scan_load_pairs(&s_b[r][n0], b);
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                w[r][i] = exp2_pair(mul2(dv.x, a[i]));
+                w[r][i] = scan_decay(dv.x, a[i]);
                 hs[r + 1][i] = fma2(w[r][i], hs[r][i], mul2(dv.y, b[i]));
             }
         }
@@ -1029,7 +1030,7 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const __grid_constant__ 
             float part = 0.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                h[i] = fmaf(fast_exp2(dd * aa[i]), h[i], uu * bv[i]);
+                h[i] = fmaf(fast_exp2(fmaf(dd, aa[i], kDecayAddend)), h[i], uu * bv[i]);
                 if (VEC4 || n0 + i < p.states) part = fmaf(h[i], cv[i], part);      // 0 * infinity is not a number
             }
             if (c < p.channels) {

@@ -527,3 +527,36 @@ def test_a_generous_max_len_changes_nothing(lengths):
     p.check_forward()
     p.backward()
     p.check_backward()
+
+
+def kept_states(L, e, d, n, step_by_step):
+    """States of ones behind L rows whose inputs are zero and whose steps are e, all with A = -1."""
+    A, state = f32(-np.ones((d, n))), torch.ones(1, d, n, device="cuda")
+    zero, bc, dt, out = (torch.zeros(L, w, device="cuda") for w in (d, n, d, d))
+    dt[:] = torch.from_numpy(e).cuda().float()
+    a = tdx.tdx_scan_args(batch=1, max_len=L, rows=L, channels=d, states=n, groups=1, dtype=tdx.TDX_F32, dt_softplus=0, x=zero, ld_x=d, dt=dt, ld_dt=d, A=A, B=bc,
+                          ld_B=n, C=bc, ld_C=n, out=out, ld_out=d, state_in=state, state_out=state, n_slots=1)
+    ws = workspace(tdx.tdx_selective_scan_workspace_size(a))
+    a.set(workspace=ws, workspace_bytes=ws.numel())
+    for _ in range(L if step_by_step else 1):
+        tdx.check((tdx.tdx_selective_scan_step if step_by_step else tdx.tdx_selective_scan)(a))
+    torch.cuda.synchronize()
+    return state[0].double().cpu().numpy()
+
+
+@pytest.mark.parametrize("step_by_step", [False, True])
+@pytest.mark.parametrize("lo,hi", [(0.002, 0.006), (0.006, 0.02), (0.02, 0.1)])
+def test_decays_are_right_on_average(lo, hi, step_by_step):
+    """A state takes in the error of one decay per row.  Over 8192 different decays the mean error of a row has to be well below what
+    the rounding of a single one may be (2^-25): below half of it."""
+    L, d, n = 64, 8192, 4
+    e = np.random.default_rng(0).uniform(lo, hi, d).astype(np.float32).astype(np.float64)
+    got = kept_states(L, e, d, n, step_by_step)
+    want = np.exp(-L * e)[:, None]
+    assert abs(((got - want) / want).mean()) / L < 2.0 ** -26
+
+
+@pytest.mark.parametrize("step_by_step", [False, True])
+@pytest.mark.parametrize("d,n", [(64, 16), (40, 3), (9, 100)])
+def test_a_step_of_zero_keeps_the_state(d, n, step_by_step):
+    assert (kept_states(45, np.zeros(d), d, n, step_by_step) == 1).all()
