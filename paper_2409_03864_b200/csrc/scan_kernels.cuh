@@ -11,10 +11,10 @@
 // and so do the sums over a channel's threads.  Neighbouring lanes hold neighbouring channels of the same states, so B and C
 // are read once per warp.
 //
-// Bound by issue and latency, not by memory: a block of 128 threads per 512 / N channels leaves about seven warps on an SM, and a warp
-// nearly alone takes about three cycles an instruction.  In bf16 with 16 states, whole calls: 4096 x 4096 forward 239 us (one exponential per
-// state takes 58 at 16 a cycle and SM); 8192 x 2048 training 762 us (forward 170, backward 570, joining the sums 20); 128 single
-// tokens of 4096 channels 17.5 us, state traffic at 4.1 TB/s, 63 % of the copy rate.
+// Bound by issue and latency, not by memory: registers allow two blocks of four warps on an SM in the main kernels (N = 16), which issue
+// in less than half of their cycles and wait for shared memory and for results.  In bf16 with 16 states, whole calls: 4096 x 4096
+// forward 239 us (one exponential per state takes 58 at 16 a cycle and SM); 8192 x 2048 training 755 us (forward 158, backward 580, joining
+// the sums 20); 128 single tokens of 4096 channels 17.5 us, state traffic at 4.1 TB/s, 63 % of the copy rate.
 #pragma once
 #include "seq_common.cuh"
 

@@ -290,8 +290,8 @@ size_t scan_saved_bytes(const tdx::ScanParams& p) {
 }
 
 // How a scan is spread over the SMs: sequences are cut into chunks when channels and sequences alone do not give every SM a
-// block; a cut costs a second look at the inputs and a second exponential per state.  Blocks per SM for 4096 x 4096 with 16
-// states forward: two 255 us, three 240; the backward kernel holds so many registers that only two are resident.
+// block; a cut costs a second look at the inputs and a second exponential per state.  Blocks per SM asked for, 4096 x 4096 with 16
+// states forward: two 255 us, three 240, although only two are resident (208 registers); backward two, as many as are resident.
 void plan_scan(tdx::ScanParams* p, int sm_count, bool back) {
     const int n = scan_padded_states(p->states);
     // sequences that run side by side: packed ones of uneven length count by their rows

@@ -213,7 +213,7 @@ __device__ __forceinline__ void w4_lay_out(uint4* step_x, int o, int row, int ro
 // A thread's weights of a step (two rows, 16 bytes each) travel through shared memory by asynchronous copies, kW4Depth steps
 // ahead, into a place that only this thread uses: a loop that prefetched into registers waited for its newest loads (about
 // twice the time for 8192 x 8192 weights in the form of that time), and a ring costs no registers and little code.
-// Whole calls in bf16: 6.7 us for one token and 4096 x 4096 weights (4.7 on the device; the host's part bounds it), 13.4 us for
+// Whole calls in bf16: 7.0 us for one token and 4096 x 4096 weights (4.6 in a graph; the host's part bounds it), 13.4 us for
 // 8192 x 8192 (2.6 TB/s; start-up, layout of x and the join are about half of it).
 constexpr int kW4Depth = 4;
 __device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
