@@ -384,7 +384,7 @@ typedef struct {
 
 int tdx_gemm_w4(const tdx_w4_args* args, void* stream);
 /*
- * Weights for it from w (N x K, rows ld_w elements apart, in the type `dtype`, which the scales get too).  zeros = NULL: scale =
+ * Weights for it from w (N x K, rows ld_w elements apart, finite, in the type `dtype`, which the scales get too).  zeros = NULL: scale =
  * max |w| / 7 of the group and q = round(w / scale) + 8; else scale = (max(w, 0) - min(w, 0)) / 15, zero = round(-min / scale), q =
  * round(w / scale) + zero, limited to 0 .. 15.  Halves round to even; an all-zero group gets the scale 1.  group_size is even or
  * at least K.

@@ -77,7 +77,8 @@ __global__ void __launch_bounds__(128) w4_quantize_kernel(long long N, long long
         lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, m));
         hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, m));
     }
-    const T stored = seq_from_float<T>(zeros ? (hi - lo) / 15.0f : fmaxf(hi, -lo) / 7.0f);
+    const float range = hi - lo, fifteenth = isinf(range) ? hi / 15.0f - lo / 15.0f : range / 15.0f;      // the range may overflow
+    const T stored = seq_from_float<T>(zeros ? fifteenth : fmaxf(hi, -lo) / 7.0f);
     float scale = seq_to_float(stored);
     if (!(scale > 0.0f)) scale = 1.0f;
     const float zero = zeros ? fminf(fmaxf(rintf(-lo / scale), 0.0f), 15.0f) : 8.0f, least = zeros ? 0.0f : 1.0f;

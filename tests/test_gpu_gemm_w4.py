@@ -192,3 +192,17 @@ def test_zeros_of_a_whole_byte(m, group, dtype):
     tdx.check(tdx.tdx_gemm_w4(a))
     w = ref.unpack_w4(weight, scales, z, k, group)
     assert_close("y", y.host(), x @ w.T, np.abs(x) @ np.abs(w).T, (k + 8) * EPS, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantisation_of_the_widest_range(dtype):
+    """max - min passes the largest number of the type, the scale does not."""
+    w = torch.tensor([[3e38, -3e38, 1e38, 0.0], [3.3e38, 0.0, -1e38, 1.0]]).to(TORCH[dtype]).cuda()
+    q, s, z = torch.zeros(2, 2, dtype=torch.uint8, device="cuda"), torch.zeros(2, 1, dtype=TORCH[dtype], device="cuda"), torch.zeros(2, 1, dtype=torch.uint8, device="cuda")
+    tdx.check(tdx.tdx_w4_quantize(2, 4, 4, DT[dtype], w, 4, q, s, z))
+    torch.cuda.synchronize()
+    scales, values = s.double().cpu().numpy(), w.double().cpu().numpy()
+    want = (values.max(1) - np.minimum(values.min(1), 0)) / 15
+    assert np.all(np.abs(scales[:, 0] - want) <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -22) * want)
+    back = ref.unpack_w4(q.cpu().numpy(), scales, z.cpu().numpy(), 4, 4)
+    assert np.all(np.abs(back - values) <= (1.0 + 15 * 2.0 ** -8) * scales)
