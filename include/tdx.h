@@ -393,6 +393,54 @@ int tdx_w4_quantize(int64_t N, int64_t K, int group_size, int dtype, const void*
                     uint8_t* zeros, void* stream);
 
 /*
+ * Operators of a block with linear attention and experts.  They go by the conventions of the state-space operators above (blocks of
+ * arguments, rows `ld_*` elements apart, sequences, slots, fixed order of sums, the caller's workspace), and stand between the same
+ * projections.
+ *
+ * Norms before and after a block, with its gate and residual scale, in one pass.  For every row of x:
+ *
+ *   u = x * rstd(x) * weight_in with norm_in = 1, else x         rstd(v) = 1 / sqrt(mean(v^2) + eps), over groups of `group` channels
+ *   a = u * gate * sigmoid(gate) with a gate, else u
+ *   s = residual + scale * a   (no residual: scale * a)           sum = s
+ *   y = s * rstd(s) * weight_out                                  over the whole row, from s before it is rounded
+ *
+ * sum and y are both optional, but one is needed.  Missing weights and scales are ones.  sum may be residual (in place).  The heads'
+ * norm and gate behind an attention is norm_in = 1 with group = a head's channels and only `sum`; the norm in front of a block is
+ * norm_in = 0 with only `y`; the stream's sum behind a block with the next block's norm has all of it.
+ * Backward: all gradients from x, gate, residual, dsum and dy (either may be NULL: zeros; dy stands for y); s is computed again.
+ * dresidual may be dsum.  channels up to 2^20; rows of up to 8192 channels are read once, wider ones several times.
+ */
+typedef struct {
+    int64_t rows, channels;
+    int64_t group;                /* channels per norm of x, a divisor of channels; 0: all of them */
+    int dtype;                    /* tdx_dtype of the activations                                */
+    int norm_in;                  /* 0 or 1                                                      */
+    float eps;                    /* >= 0                                                        */
+    const void* x; int64_t ld_x;          /* rows x channels                                     */
+    const float* weight_in;               /* channels, or NULL                                   */
+    const void* gate; int64_t ld_gate;    /* rows x channels, or NULL                            */
+    const float* scale;                   /* channels, or NULL                                   */
+    const void* residual; int64_t ld_residual;   /* rows x channels, or NULL                     */
+    void* sum; int64_t ld_sum;            /* rows x channels, or NULL                            */
+    const float* weight_out;              /* channels, or NULL                                   */
+    void* y; int64_t ld_y;                /* rows x channels, or NULL                            */
+    const void* dsum; int64_t ld_dsum;    /* gradients: rows x channels, or NULL                 */
+    const void* dy; int64_t ld_dy;
+    void* dx; int64_t ld_dx;
+    void* dgate; int64_t ld_dgate;               /* needed with a gate                           */
+    void* dresidual; int64_t ld_dresidual;       /* needed with a residual                       */
+    float* dweight_in;                    /* channels, overwritten; NULL: not wanted             */
+    float* dscale;                        /* channels, overwritten; NULL: not wanted             */
+    float* dweight_out;                   /* channels, overwritten; NULL: not wanted             */
+    void* workspace; size_t workspace_bytes;
+} tdx_norm_args;
+
+int tdx_block_norm(const tdx_norm_args* args, void* stream);
+int tdx_block_norm_bwd(const tdx_norm_args* args, void* stream);
+/* Workspace of tdx_block_norm_bwd (host only; depends on the current device's SM count, or on a B200's where there is no device). */
+int tdx_block_norm_workspace_size(const tdx_norm_args* args, size_t* bytes);
+
+/*
  * Host-buffer variants: A, B, C (x, w, bias, y) are HOST pointers (pinned memory gives the best
  * copy rate).  The call copies the inputs to device staging buffers owned by the library, runs the
  * same kernels as above, copies the result back and returns after the stream has drained.

@@ -69,7 +69,7 @@ class _Args(ctypes.Structure):
 
 def _fields(text):
     """'i64 a b; int c; ptr d' -> the fields of a ctypes structure, in order."""
-    types = {"i64": ctypes.c_int64, "int": ctypes.c_int, "ptr": ctypes.c_void_p, "size": ctypes.c_size_t}
+    types = {"i64": ctypes.c_int64, "int": ctypes.c_int, "f32": ctypes.c_float, "ptr": ctypes.c_void_p, "size": ctypes.c_size_t}
     return [(name, types[group.split()[0]]) for group in text.split(";") for name in group.split()[1:]]
 
 
@@ -91,7 +91,14 @@ class tdx_w4_args(_Args):
     _fields_ = _fields("i64 M N K; int group_size dtype; ptr x; i64 ld_x; ptr weight scales zeros y; i64 ld_y")
 
 
-for _cls in (tdx_conv1d_args, tdx_scan_args, tdx_w4_args):
+class tdx_norm_args(_Args):
+    _fields_ = _fields("i64 rows channels group; int dtype norm_in; f32 eps; ptr x; i64 ld_x; ptr weight_in gate; i64 ld_gate; ptr scale residual;"
+                       "i64 ld_residual; ptr sum; i64 ld_sum; ptr weight_out y; i64 ld_y; ptr dsum; i64 ld_dsum; ptr dy; i64 ld_dy; ptr dx;"
+                       "i64 ld_dx; ptr dgate; i64 ld_dgate; ptr dresidual; i64 ld_dresidual; ptr dweight_in dscale dweight_out workspace;"
+                       "size workspace_bytes")
+
+
+for _cls in (tdx_conv1d_args, tdx_scan_args, tdx_w4_args, tdx_norm_args):
     _cls._names = frozenset(n for n, _ in _cls._fields_)
     _cls._pointers = frozenset(n for n, t in _cls._fields_ if t is ctypes.c_void_p)
 
@@ -146,9 +153,10 @@ def lib() -> ctypes.CDLL:
         L.tdx_gemm_k_balanced_plan.argtypes = [i64, i64, i64, ci, ci, ci, ip, ci, ip, ip, ip]
         L.tdx_gemm_splitk_static.argtypes = [i64, i64, i64, ci, ci, cf, vp, vp, vp, ci, ci, vp]
         for op in ("causal_conv1d", "causal_conv1d_bwd", "causal_conv1d_step", "selective_scan", "selective_scan_bwd",
-                   "selective_scan_step", "gemm_w4"):
+                   "selective_scan_step", "gemm_w4", "block_norm", "block_norm_bwd"):
             getattr(L, "tdx_" + op).argtypes = [vp, vp]
-        for op in ("causal_conv1d_workspace_size", "selective_scan_workspace_size", "selective_scan_saved_size"):
+        for op in ("causal_conv1d_workspace_size", "selective_scan_workspace_size", "selective_scan_saved_size",
+                   "block_norm_workspace_size"):
             getattr(L, "tdx_" + op).argtypes = [vp, ctypes.POINTER(sz)]
         L.tdx_w4_quantize.argtypes = [i64, i64, ci, ci, vp, i64, vp, vp, vp, vp]
         L.tdx_check_device_status.argtypes = [vp]
@@ -181,6 +189,7 @@ EXPORTS = (
     "tdx_causal_conv1d", "tdx_causal_conv1d_bwd", "tdx_causal_conv1d_step", "tdx_causal_conv1d_workspace_size",
     "tdx_selective_scan", "tdx_selective_scan_bwd", "tdx_selective_scan_step", "tdx_selective_scan_saved_size",
     "tdx_selective_scan_workspace_size", "tdx_gemm_w4", "tdx_w4_quantize",
+    "tdx_block_norm", "tdx_block_norm_bwd", "tdx_block_norm_workspace_size",
 )
 
 
@@ -513,6 +522,20 @@ def tdx_gemm_w4(args: tdx_w4_args, stream=None) -> int:
 def tdx_w4_quantize(N, K, group_size, dtype, w, ld_w, weight, scales, zeros=None, stream=None) -> int:
     """4-bit weights, scales and (unless None) zeros from an N x K matrix."""
     return lib().tdx_w4_quantize(N, K, group_size, dtype, _ptr(w), ld_w, _ptr(weight), _ptr(scales), _ptr(zeros), _stream(stream))
+
+
+def tdx_block_norm(args: tdx_norm_args, stream=None) -> int:
+    """Norm of a block's output, gate, scaled residual sum and the next block's norm in one pass: sum and y."""
+    return lib().tdx_block_norm(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_block_norm_bwd(args: tdx_norm_args, stream=None) -> int:
+    return lib().tdx_block_norm_bwd(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_block_norm_workspace_size(args: tdx_norm_args):
+    """Returns (status, bytes)."""
+    return _args_size(lib().tdx_block_norm_workspace_size, args)
 
 
 def tdx_check_device_status(stream=None) -> int:

@@ -4,6 +4,7 @@
 // tile plans), host_launch.cuh (launches).
 #include "host_launch.cuh"
 #include "host_space.cuh"
+#include "layer_bridge.h"
 #include "seq_common.cuh"
 
 #include <array>
@@ -1896,4 +1897,29 @@ const char* tdx_version(void) { return "tdx 0.1.0 (sm_100a)"; }
 
 }  // extern "C"
 
+namespace {
+void count_launch() { g_launches.fetch_add(1); }
+}  // namespace
 #include "seq_api.cuh"
+
+// What the other translation units of the library use of this one (layer_host.cuh).
+namespace tdx_host {
+int fail_text(int status, const char* text) {
+    g_err = text;
+    return status;
+}
+void count_launch() { g_launches.fetch_add(1); }
+int get_device(Device* out) {
+    DeviceCtx* ctx;
+    TDX_TRY(get_ctx(&ctx));
+    out->sm_count = ctx->sm_count;
+    out->smem_optin = ctx->smem_optin;
+    out->status = ctx->status_ptr;
+    return TDX_OK;
+}
+int bf16_map(const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides_bytes, const uint32_t* box, CUtensorMap* out) {
+    DeviceCtx* ctx;
+    TDX_TRY(get_ctx(&ctx));
+    return get_tensor_map(ctx, ptr, rank, dims, strides_bytes, box, out);
+}
+}  // namespace tdx_host

@@ -1,0 +1,50 @@
+"""Argument checks of the block operators: refusals come before any device work, and sizes need no device."""
+import pytest
+
+import paper_2409_03864_b200 as tdx
+from paper_2409_03864_b200 import build as tdx_build
+
+P = 1 << 20        # an aligned address that is never used
+INVALID, UNSUPPORTED, ALIGNMENT, WORKSPACE = tdx.TDX_ERR_INVALID_ARG, tdx.TDX_ERR_UNSUPPORTED, tdx.TDX_ERR_ALIGNMENT, tdx.TDX_ERR_WORKSPACE
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    tdx_build.build()
+
+
+def norm(**change):
+    a = dict(rows=4, channels=8, group=4, dtype=tdx.TDX_BF16, norm_in=1, eps=1e-5, weight_in=P, scale=P, weight_out=P, dweight_in=P, dscale=P, dweight_out=P)
+    for n in ("x", "gate", "residual", "sum", "y", "dsum", "dy", "dx", "dgate", "dresidual"):
+        a.update({n: P, "ld_" + n: 8})
+    return tdx.tdx_norm_args(**{**a, **change})
+
+
+NORM_BAD = [
+    (dict(rows=-1), INVALID), (dict(channels=-1), INVALID), (dict(group=-4), INVALID), (dict(group=3), INVALID), (dict(dtype=2), INVALID),
+    (dict(norm_in=2), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID), (dict(x=None), INVALID), (dict(ld_x=7), INVALID),
+    (dict(ld_gate=7), INVALID), (dict(ld_residual=7), INVALID), (dict(x=P + 1), ALIGNMENT), (dict(gate=P + 1), ALIGNMENT), (dict(scale=P + 2), ALIGNMENT),
+    (dict(weight_in=P + 2), ALIGNMENT), (dict(weight_out=P + 1), ALIGNMENT), (dict(channels=(1 << 20) + 1, group=0), UNSUPPORTED),
+    (dict(channels=10000, group=2), UNSUPPORTED), (dict(ld_x=(1 << 24) + 1), UNSUPPORTED),
+]
+
+
+@pytest.mark.parametrize("change,status", NORM_BAD + [(dict(sum=None, y=None), INVALID), (dict(ld_sum=7), INVALID), (dict(ld_y=7), INVALID), (dict(y=P + 1), ALIGNMENT)])
+def test_block_norm_refusals(change, status):
+    assert tdx.tdx_block_norm(norm(**change)) == status, tdx.tdx_last_error()
+    assert tdx.tdx_last_error()
+
+
+@pytest.mark.parametrize("change,status", NORM_BAD + [
+    (dict(dsum=None, dy=None), INVALID), (dict(dx=None), INVALID), (dict(dgate=None), INVALID), (dict(dresidual=None), INVALID), (dict(ld_dx=7), INVALID),
+    (dict(ld_dy=7), INVALID), (dict(norm_in=0), INVALID), (dict(dweight_in=P + 2), ALIGNMENT), (dict(dscale=P + 1), ALIGNMENT)])
+def test_block_norm_bwd_refusals(change, status):
+    assert tdx.tdx_block_norm_bwd(norm(**change)) == status, tdx.tdx_last_error()
+
+
+def test_block_norm_sizes_and_empty_calls():
+    status, size = tdx.tdx_block_norm_workspace_size(norm())
+    assert status == 0 and size > 0
+    assert tdx.tdx_block_norm(norm(rows=0, x=None, sum=None, y=None)) == 0
+    assert tdx.tdx_block_norm(norm(channels=0, group=0)) == 0
+    assert tdx.lib().tdx_block_norm(None, None) == INVALID and tdx.lib().tdx_block_norm_bwd(None, None) == INVALID
