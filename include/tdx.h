@@ -441,6 +441,38 @@ int tdx_block_norm_bwd(const tdx_norm_args* args, void* stream);
 int tdx_block_norm_workspace_size(const tdx_norm_args* args, size_t* bytes);
 
 /*
+ * Matrix products grouped by expert: with the rows offsets[e] .. offsets[e + 1] - 1 belonging to expert e,
+ *
+ *   y[t, n] = sum_k x[t, k] * weight[e, n, k]                     tdx_gemm_grouped
+ *   dx[t, k] = sum_n dy[t, n] * weight[e, n, k]                   tdx_gemm_grouped_dx
+ *   dweight[e, n, k] = sum_t dy[t, n] * x[t, k]                   tdx_gemm_grouped_dw (an expert without rows: zeros)
+ *
+ * dtype as for tdx_gemm: TDX_BF16 (bf16 in, fp32 accumulate, one rounding) or TDX_F32.  offsets are device memory, experts + 1 values,
+ * ascending; an expert may have no rows, and rows of no expert (behind the last, or in front of the first) are neither read nor
+ * written.  An expert whose offsets leave [0, rows] or descend is treated as one without rows and reported by
+ * tdx_check_device_status (TDX_ERR_BOUNDS).  bf16 operands whose rows are multiples of 16 bytes apart run on the tensor cores;
+ * any other alignment on the CUDA cores.  K = 0: y = 0.
+ */
+typedef struct {
+    int64_t rows, experts, N, K;
+    int dtype;                    /* tdx_dtype                                                   */
+    const int32_t* offsets;               /* experts + 1                                         */
+    const void* x; int64_t ld_x;          /* rows x K                                            */
+    const void* weight;                   /* experts x N x K, dense                              */
+    void* y; int64_t ld_y;                /* rows x N                                            */
+    const void* dy; int64_t ld_dy;        /* rows x N                                            */
+    void* dx; int64_t ld_dx;              /* rows x K                                            */
+    void* dweight;                        /* experts x N x K, dense                              */
+    void* workspace; size_t workspace_bytes;
+} tdx_grouped_args;
+
+int tdx_gemm_grouped(const tdx_grouped_args* args, void* stream);
+int tdx_gemm_grouped_dx(const tdx_grouped_args* args, void* stream);
+int tdx_gemm_grouped_dw(const tdx_grouped_args* args, void* stream);
+/* Workspace that covers the three (host only; may be 0). */
+int tdx_gemm_grouped_workspace_size(const tdx_grouped_args* args, size_t* bytes);
+
+/*
  * Host-buffer variants: A, B, C (x, w, bias, y) are HOST pointers (pinned memory gives the best
  * copy rate).  The call copies the inputs to device staging buffers owned by the library, runs the
  * same kernels as above, copies the result back and returns after the stream has drained.

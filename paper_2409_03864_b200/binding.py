@@ -98,7 +98,12 @@ class tdx_norm_args(_Args):
                        "size workspace_bytes")
 
 
-for _cls in (tdx_conv1d_args, tdx_scan_args, tdx_w4_args, tdx_norm_args):
+class tdx_grouped_args(_Args):
+    _fields_ = _fields("i64 rows experts N K; int dtype; ptr offsets x; i64 ld_x; ptr weight y; i64 ld_y; ptr dy; i64 ld_dy; ptr dx; i64 ld_dx;"
+                       "ptr dweight workspace; size workspace_bytes")
+
+
+for _cls in (tdx_conv1d_args, tdx_scan_args, tdx_w4_args, tdx_norm_args, tdx_grouped_args):
     _cls._names = frozenset(n for n, _ in _cls._fields_)
     _cls._pointers = frozenset(n for n, t in _cls._fields_ if t is ctypes.c_void_p)
 
@@ -153,10 +158,11 @@ def lib() -> ctypes.CDLL:
         L.tdx_gemm_k_balanced_plan.argtypes = [i64, i64, i64, ci, ci, ci, ip, ci, ip, ip, ip]
         L.tdx_gemm_splitk_static.argtypes = [i64, i64, i64, ci, ci, cf, vp, vp, vp, ci, ci, vp]
         for op in ("causal_conv1d", "causal_conv1d_bwd", "causal_conv1d_step", "selective_scan", "selective_scan_bwd",
-                   "selective_scan_step", "gemm_w4", "block_norm", "block_norm_bwd"):
+                   "selective_scan_step", "gemm_w4", "block_norm", "block_norm_bwd",
+                   "gemm_grouped", "gemm_grouped_dx", "gemm_grouped_dw"):
             getattr(L, "tdx_" + op).argtypes = [vp, vp]
         for op in ("causal_conv1d_workspace_size", "selective_scan_workspace_size", "selective_scan_saved_size",
-                   "block_norm_workspace_size"):
+                   "block_norm_workspace_size", "gemm_grouped_workspace_size"):
             getattr(L, "tdx_" + op).argtypes = [vp, ctypes.POINTER(sz)]
         L.tdx_w4_quantize.argtypes = [i64, i64, ci, ci, vp, i64, vp, vp, vp, vp]
         L.tdx_check_device_status.argtypes = [vp]
@@ -190,6 +196,7 @@ EXPORTS = (
     "tdx_selective_scan", "tdx_selective_scan_bwd", "tdx_selective_scan_step", "tdx_selective_scan_saved_size",
     "tdx_selective_scan_workspace_size", "tdx_gemm_w4", "tdx_w4_quantize",
     "tdx_block_norm", "tdx_block_norm_bwd", "tdx_block_norm_workspace_size",
+    "tdx_gemm_grouped", "tdx_gemm_grouped_dx", "tdx_gemm_grouped_dw", "tdx_gemm_grouped_workspace_size",
 )
 
 
@@ -536,6 +543,26 @@ def tdx_block_norm_bwd(args: tdx_norm_args, stream=None) -> int:
 def tdx_block_norm_workspace_size(args: tdx_norm_args):
     """Returns (status, bytes)."""
     return _args_size(lib().tdx_block_norm_workspace_size, args)
+
+
+def tdx_gemm_grouped(args: tdx_grouped_args, stream=None) -> int:
+    """y = x . W[e]^T for the rows of every expert e."""
+    return lib().tdx_gemm_grouped(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_gemm_grouped_dx(args: tdx_grouped_args, stream=None) -> int:
+    """dx = dy . W[e] for the rows of every expert e."""
+    return lib().tdx_gemm_grouped_dx(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_gemm_grouped_dw(args: tdx_grouped_args, stream=None) -> int:
+    """dweight[e] = dy^T . x over the rows of every expert e."""
+    return lib().tdx_gemm_grouped_dw(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_gemm_grouped_workspace_size(args: tdx_grouped_args):
+    """Returns (status, bytes)."""
+    return _args_size(lib().tdx_gemm_grouped_workspace_size, args)
 
 
 def tdx_check_device_status(stream=None) -> int:

@@ -1,0 +1,79 @@
+// Entry points of the products grouped by expert (see tdx.h).
+#include "layer_host.cuh"
+
+#include "grouped_kernels.cuh"
+
+namespace {
+
+int check_grouped(const tdx_grouped_args* args, tdx::GroupedPass pass, tdx::GroupedParams* p) {
+    if (args == nullptr) return fail(TDX_ERR_INVALID_ARG, "args is NULL");
+    const tdx_grouped_args& a = *args;
+    if (a.rows < 0 || a.experts < 0 || a.N < 0 || a.K < 0) return fail(TDX_ERR_INVALID_ARG, "negative size");
+    if (a.dtype != TDX_F32 && a.dtype != TDX_BF16) return fail(TDX_ERR_INVALID_ARG, "unknown dtype %d", a.dtype);
+    if (a.rows > INT_MAX || a.experts > (1 << 20)) return fail(TDX_ERR_UNSUPPORTED, "more than 2^31 - 1 rows or 2^20 experts");
+    if (a.N > (1 << 24) || a.K > (1 << 24)) return fail(TDX_ERR_UNSUPPORTED, "N or K above 2^24");
+    const size_t el = elem_bytes(a.dtype);
+    const bool outs = pass == tdx::kGroupedForward ? a.rows > 0 && a.N > 0 : pass == tdx::kGroupedDx ? a.rows > 0 && a.K > 0 : a.N > 0 && a.K > 0;
+    const bool any = a.experts > 0 && outs;
+    const bool all = any && a.rows > 0 && a.N > 0 && a.K > 0;     // there are products
+    if (any && a.offsets == nullptr) return fail(TDX_ERR_INVALID_ARG, "offsets is NULL");
+    if (misaligned(a.offsets, 4)) return fail(TDX_ERR_ALIGNMENT, "offsets is not aligned to its elements");
+    if (pass != tdx::kGroupedDw) TDX_TRY(check_tensor("weight", a.weight, all, el));
+    if (pass != tdx::kGroupedDx) TDX_TRY(check_tensor("x", a.x, all, el, a.ld_x, a.K));
+    if (pass != tdx::kGroupedForward) TDX_TRY(check_tensor("dy", a.dy, all, el, a.ld_dy, a.N));
+    std::memset(p, 0, sizeof *p);
+    p->rows = a.rows; p->experts = static_cast<int>(a.experts); p->N = static_cast<int>(a.N); p->K = static_cast<int>(a.K); p->offsets = a.offsets;
+    switch (pass) {
+        case tdx::kGroupedForward:
+            TDX_TRY(check_tensor("y", a.y, any, el, a.ld_y, a.N));
+            p->a = a.x; p->ld_a = a.ld_x; p->b = a.weight; p->out = a.y; p->ld_out = a.ld_y;
+            break;
+        case tdx::kGroupedDx:
+            TDX_TRY(check_tensor("dx", a.dx, any, el, a.ld_dx, a.K));
+            p->a = a.dy; p->ld_a = a.ld_dy; p->b = a.weight; p->out = a.dx; p->ld_out = a.ld_dx;
+            break;
+        default:
+            TDX_TRY(check_tensor("dweight", a.dweight, any, el));
+            p->a = a.dy; p->ld_a = a.ld_dy; p->b = a.x; p->ld_b = a.ld_x; p->out = a.dweight; p->ld_out = a.K;
+    }
+    return TDX_OK;
+}
+
+template <typename T, int PASS, int BM>
+int launch_grouped_simt(const tdx::GroupedParams& p, cudaStream_t st) {
+    const int64_t tiles_n = ceil_div(PASS == tdx::kGroupedForward ? p.N : p.K, tdx::kSimtN);
+    const int64_t tiles_m = PASS == tdx::kGroupedDw ? p.experts * ceil_div(p.N, BM) : tdx::seq_pieces(true, p.experts, p.rows, 0, BM);
+    return launch_seq(tdx::grouped_simt_kernel<T, PASS, BM>, tiles_m * tiles_n, 1, 128, 0, st, p);
+}
+template <typename T, int PASS>
+int launch_grouped_rows(const tdx::GroupedParams& p, cudaStream_t st) {
+    return p.rows <= 16 * static_cast<int64_t>(p.experts) && PASS != tdx::kGroupedDw ? launch_grouped_simt<T, PASS, 16>(p, st) : launch_grouped_simt<T, PASS, 64>(p, st);
+}
+template <int PASS>
+int run_grouped(const tdx_grouped_args* args, void* stream) {
+    tdx::GroupedParams p;
+    TDX_TRY(check_grouped(args, static_cast<tdx::GroupedPass>(PASS), &p));
+    if (p.experts == 0 || (PASS != tdx::kGroupedDw && p.rows == 0) || (PASS != tdx::kGroupedForward && p.K == 0) || (PASS != tdx::kGroupedDx && p.N == 0)) return TDX_OK;
+    tdx_host::Device dev;
+    TDX_TRY(tdx_host::get_device(&dev));
+    p.status = dev.status;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return args->dtype == TDX_F32 ? launch_grouped_rows<float, PASS>(p, st) : launch_grouped_rows<__nv_bfloat16, PASS>(p, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tdx_gemm_grouped(const tdx_grouped_args* args, void* stream) { return run_grouped<tdx::kGroupedForward>(args, stream); }
+int tdx_gemm_grouped_dx(const tdx_grouped_args* args, void* stream) { return run_grouped<tdx::kGroupedDx>(args, stream); }
+int tdx_gemm_grouped_dw(const tdx_grouped_args* args, void* stream) { return run_grouped<tdx::kGroupedDw>(args, stream); }
+
+int tdx_gemm_grouped_workspace_size(const tdx_grouped_args* args, size_t* bytes) {
+    if (args == nullptr || bytes == nullptr) return fail(TDX_ERR_INVALID_ARG, "NULL argument");
+    if (args->rows < 0 || args->experts < 0 || args->N < 0 || args->K < 0) return fail(TDX_ERR_INVALID_ARG, "negative size");
+    *bytes = 0;
+    return TDX_OK;
+}
+
+}  // extern "C"

@@ -26,7 +26,7 @@
 #pragma once
 #include <cuda_bf16.h>
 
-#include "ptx_sm100.cuh"
+#include "bounded_wait.cuh"
 
 namespace tdx {
 
@@ -36,9 +36,7 @@ constexpr int kUmmaK = 16;        // K of one tcgen05.mma for 16-bit inputs
 constexpr int kMaxStages = 8;
 constexpr int kMaxSlots = 8;
 constexpr int kHalfABytes = kHalfM * kBK * 2;          // 16 KiB: one 128-row half of the A slice
-constexpr long long kWaitLimitCycles = 4000000000LL;  // ~2 s at boost clock
 
-enum : int { kTimeoutProducer = 1, kTimeoutMma = 2, kTimeoutEpilogue = 3 };
 
 struct UmmaParams {
     int M, N;                 // logical output rows / columns
@@ -112,28 +110,6 @@ struct UmmaParams {
                               // 16-row patches are cut from that column, so they may straddle two images
     int* status;              // device status word
 };
-
-__device__ __forceinline__ bool wait_bounded_for(uint64_t* bar, uint32_t parity, volatile int* s_abort, int* g_status,
-                                                 int code, long long limit_cycles) {
-    if (ptx::mbar_try_wait(bar, parity)) return true;
-    const long long t0 = clock64();
-    uint32_t spins = 0;
-    for (;;) {
-        if (ptx::mbar_try_wait(bar, parity)) return true;
-        if ((++spins & 63u) == 0u) {
-            if (*s_abort) return false;
-            if (clock64() - t0 > limit_cycles) {
-                *s_abort = 1;
-                atomicCAS(g_status, 0, code);
-                return false;
-            }
-        }
-    }
-}
-__device__ __forceinline__ bool wait_bounded(uint64_t* bar, uint32_t parity, volatile int* s_abort, int* g_status,
-                                             int code) {
-    return wait_bounded_for(bar, parity, s_abort, g_status, code, kWaitLimitCycles);
-}
 
 // Self-test of the bounded wait: one warp waits on a barrier that nothing ever signals, with a short limit; the wait
 // must give up, record `kTimeoutSelfTest` in the status word and let the kernel return normally.

@@ -48,3 +48,34 @@ def test_block_norm_sizes_and_empty_calls():
     assert tdx.tdx_block_norm(norm(rows=0, x=None, sum=None, y=None)) == 0
     assert tdx.tdx_block_norm(norm(channels=0, group=0)) == 0
     assert tdx.lib().tdx_block_norm(None, None) == INVALID and tdx.lib().tdx_block_norm_bwd(None, None) == INVALID
+
+
+def grouped(**change):
+    a = dict(rows=6, experts=2, N=8, K=16, dtype=tdx.TDX_BF16, offsets=P, x=P, ld_x=16, weight=P, y=P, ld_y=8, dy=P, ld_dy=8, dx=P, ld_dx=16, dweight=P,
+             workspace=P, workspace_bytes=1 << 40)
+    return tdx.tdx_grouped_args(**{**a, **change})
+
+
+GROUPED_BAD = [(dict(rows=-1), INVALID), (dict(experts=-1), INVALID), (dict(N=-1), INVALID), (dict(K=-1), INVALID), (dict(dtype=5), INVALID),
+               (dict(offsets=None), INVALID), (dict(offsets=P + 2), ALIGNMENT), (dict(rows=1 << 31), UNSUPPORTED), (dict(experts=1 << 21), UNSUPPORTED),
+               (dict(N=1 << 25, ld_y=1 << 25, ld_dy=1 << 25), UNSUPPORTED)]
+
+
+@pytest.mark.parametrize("call,change,status", [
+    ("", dict(x=None), INVALID), ("", dict(weight=None), INVALID), ("", dict(y=None), INVALID), ("", dict(ld_x=15), INVALID), ("", dict(ld_y=7), INVALID),
+    ("", dict(x=P + 1), ALIGNMENT), ("", dict(weight=P + 1), ALIGNMENT), ("_dx", dict(dy=None), INVALID), ("_dx", dict(dx=None), INVALID),
+    ("_dx", dict(weight=None), INVALID), ("_dx", dict(ld_dx=15), INVALID), ("_dw", dict(dy=None), INVALID), ("_dw", dict(x=None), INVALID),
+    ("_dw", dict(dweight=None), INVALID), ("_dw", dict(ld_dy=7), INVALID), ("_dw", dict(dweight=P + 1), ALIGNMENT),
+    *[(c, *bad) for c in ("", "_dx", "_dw") for bad in GROUPED_BAD]])
+def test_grouped_refusals(call, change, status):
+    assert getattr(tdx, "tdx_gemm_grouped" + call)(grouped(**change)) == status, tdx.tdx_last_error()
+    assert tdx.tdx_last_error()
+
+
+def test_grouped_sizes_and_empty_calls():
+    status, size = tdx.tdx_gemm_grouped_workspace_size(grouped())
+    assert status == 0 and size >= 0
+    assert tdx.tdx_gemm_grouped(grouped(rows=0, x=None, y=None)) == 0
+    assert tdx.tdx_gemm_grouped(grouped(experts=0, offsets=None)) == 0
+    assert tdx.tdx_gemm_grouped_dx(grouped(K=0, dx=None)) == 0 and tdx.tdx_gemm_grouped_dw(grouped(N=0, dweight=None)) == 0
+    assert tdx.lib().tdx_gemm_grouped(None, None) == INVALID
