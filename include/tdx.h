@@ -473,6 +473,54 @@ int tdx_gemm_grouped_dw(const tdx_grouped_args* args, void* stream);
 int tdx_gemm_grouped_workspace_size(const tdx_grouped_args* args, size_t* bytes);
 
 /*
+ * Linear attention with a decay for each head: with l = exp(log_decay[h]) and S = the sequence's state of head h (dim_k x dim_v),
+ *
+ *   S[t] = l * S[t - 1] + k[t]^T v[t],        out[t] = scale * q[t] S[t]
+ *
+ * q, k and v have q_heads, k_heads and v_heads heads side by side in a row, each a divisor of `heads` (0: heads); head h reads head
+ * h / (heads / q_heads) of q, and so on.  log_decay is a constant of the layer and has no gradient; values above 0 grow.  Prompts run in
+ * chunks of rows (inside a chunk as products of matrices), so a value of q, k or v that is not finite may also reach the rows of its
+ * chunk in front of it, up to 63, and their gradients.
+ * bf16: products of bf16 values with fp32 sums; attention weights and the states that a row reads are rounded to bf16 in front of their product,
+ * the states that are handed on (state_out, dstate_in) and all sums are not.
+ * Backward: dq, dk, dv (summed over the heads that share one) and dstate_in from q, k, v, state_in, dout and dstate_out.
+ */
+typedef struct {
+    int64_t batch, max_len, rows;
+    int heads, q_heads, k_heads, v_heads;
+    int dim_k, dim_v;             /* 1 .. 128                                                    */
+    int dtype;                    /* tdx_dtype                                                   */
+    float scale;
+    const float* log_decay;               /* heads                                               */
+    const void* q; int64_t ld_q;          /* rows x (q_heads * dim_k)                            */
+    const void* k; int64_t ld_k;          /* rows x (k_heads * dim_k)                            */
+    const void* v; int64_t ld_v;          /* rows x (v_heads * dim_v)                            */
+    void* out; int64_t ld_out;            /* rows x (heads * dim_v)                              */
+    const int32_t* seq_offsets;
+    const float* state_in;                /* n_slots x heads x dim_k x dim_v                     */
+    float* state_out;
+    int64_t state_stride;
+    const int32_t* slots; int64_t n_slots;
+    const void* dout; int64_t ld_dout;    /* gradients: rows x (heads * dim_v)                   */
+    void* dq; int64_t ld_dq;
+    void* dk; int64_t ld_dk;
+    void* dv; int64_t ld_dv;
+    const float* dstate_out;              /* gradient of the state after, or NULL                */
+    float* dstate_in;                     /* gradient of the state before, or NULL               */
+    void* workspace; size_t workspace_bytes;
+} tdx_attention_args;
+
+/* out and state_out.  Needs a workspace when tdx_decay_attention_workspace_size is not 0. */
+int tdx_decay_attention(const tdx_attention_args* args, void* stream);
+int tdx_decay_attention_bwd(const tdx_attention_args* args, void* stream);
+/* One token for each of `batch` rows: seq_offsets, max_len and rows are not used, state_in and state_out are needed, and a
+ * row without a slot is padding whose out is zero. */
+int tdx_decay_attention_step(const tdx_attention_args* args, void* stream);
+/* Workspace that covers tdx_decay_attention and, when args->dout is set, tdx_decay_attention_bwd (host only; depends on the current
+ * device's SM count, or on a B200's where there is no device). */
+int tdx_decay_attention_workspace_size(const tdx_attention_args* args, size_t* bytes);
+
+/*
  * Host-buffer variants: A, B, C (x, w, bias, y) are HOST pointers (pinned memory gives the best
  * copy rate).  The call copies the inputs to device staging buffers owned by the library, runs the
  * same kernels as above, copies the result back and returns after the stream has drained.

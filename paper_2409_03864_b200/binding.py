@@ -103,7 +103,14 @@ class tdx_grouped_args(_Args):
                        "ptr dweight workspace; size workspace_bytes")
 
 
-for _cls in (tdx_conv1d_args, tdx_scan_args, tdx_w4_args, tdx_norm_args, tdx_grouped_args):
+class tdx_attention_args(_Args):
+    _fields_ = _fields("i64 batch max_len rows; int heads q_heads k_heads v_heads dim_k dim_v dtype; f32 scale; ptr log_decay q; i64 ld_q; ptr k;"
+                       "i64 ld_k; ptr v; i64 ld_v; ptr out; i64 ld_out; ptr seq_offsets state_in state_out; i64 state_stride; ptr slots;"
+                       "i64 n_slots; ptr dout; i64 ld_dout; ptr dq; i64 ld_dq; ptr dk; i64 ld_dk; ptr dv; i64 ld_dv; ptr dstate_out dstate_in"
+                       " workspace; size workspace_bytes")
+
+
+for _cls in (tdx_conv1d_args, tdx_scan_args, tdx_w4_args, tdx_norm_args, tdx_grouped_args, tdx_attention_args):
     _cls._names = frozenset(n for n, _ in _cls._fields_)
     _cls._pointers = frozenset(n for n, t in _cls._fields_ if t is ctypes.c_void_p)
 
@@ -159,10 +166,11 @@ def lib() -> ctypes.CDLL:
         L.tdx_gemm_splitk_static.argtypes = [i64, i64, i64, ci, ci, cf, vp, vp, vp, ci, ci, vp]
         for op in ("causal_conv1d", "causal_conv1d_bwd", "causal_conv1d_step", "selective_scan", "selective_scan_bwd",
                    "selective_scan_step", "gemm_w4", "block_norm", "block_norm_bwd",
-                   "gemm_grouped", "gemm_grouped_dx", "gemm_grouped_dw"):
+                   "gemm_grouped", "gemm_grouped_dx", "gemm_grouped_dw", "decay_attention", "decay_attention_bwd",
+                   "decay_attention_step"):
             getattr(L, "tdx_" + op).argtypes = [vp, vp]
         for op in ("causal_conv1d_workspace_size", "selective_scan_workspace_size", "selective_scan_saved_size",
-                   "block_norm_workspace_size", "gemm_grouped_workspace_size"):
+                   "block_norm_workspace_size", "gemm_grouped_workspace_size", "decay_attention_workspace_size"):
             getattr(L, "tdx_" + op).argtypes = [vp, ctypes.POINTER(sz)]
         L.tdx_w4_quantize.argtypes = [i64, i64, ci, ci, vp, i64, vp, vp, vp, vp]
         L.tdx_check_device_status.argtypes = [vp]
@@ -197,6 +205,7 @@ EXPORTS = (
     "tdx_selective_scan_workspace_size", "tdx_gemm_w4", "tdx_w4_quantize",
     "tdx_block_norm", "tdx_block_norm_bwd", "tdx_block_norm_workspace_size",
     "tdx_gemm_grouped", "tdx_gemm_grouped_dx", "tdx_gemm_grouped_dw", "tdx_gemm_grouped_workspace_size",
+    "tdx_decay_attention", "tdx_decay_attention_bwd", "tdx_decay_attention_step", "tdx_decay_attention_workspace_size",
 )
 
 
@@ -563,6 +572,25 @@ def tdx_gemm_grouped_dw(args: tdx_grouped_args, stream=None) -> int:
 def tdx_gemm_grouped_workspace_size(args: tdx_grouped_args):
     """Returns (status, bytes)."""
     return _args_size(lib().tdx_gemm_grouped_workspace_size, args)
+
+
+def tdx_decay_attention(args: tdx_attention_args, stream=None) -> int:
+    """Linear attention with a decay per head over packed sequences: out, and the states after them."""
+    return lib().tdx_decay_attention(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_decay_attention_bwd(args: tdx_attention_args, stream=None) -> int:
+    return lib().tdx_decay_attention_bwd(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_decay_attention_step(args: tdx_attention_args, stream=None) -> int:
+    """One token per batch row; the states move on by one row."""
+    return lib().tdx_decay_attention_step(ctypes.addressof(args), _stream(stream))
+
+
+def tdx_decay_attention_workspace_size(args: tdx_attention_args):
+    """Returns (status, bytes)."""
+    return _args_size(lib().tdx_decay_attention_workspace_size, args)
 
 
 def tdx_check_device_status(stream=None) -> int:

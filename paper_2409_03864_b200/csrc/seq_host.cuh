@@ -32,15 +32,16 @@ int launch_seq(void (*kernel)(Params...), int64_t grid_x, int64_t grid_y, int th
     return TDX_OK;
 }
 
-// Lets a kernel have more than 48 KB of shared memory: as much as there is, remembered per device, so that later calls skip it.
+// Lets a kernel have more than 48 KB of shared memory: `most` (as much as there is, for a kernel without static shared memory),
+// remembered per device, so that later calls skip it.
 template <typename Kernel>
-int allow_smem(Kernel kernel, std::atomic<bool> (&known)[64], size_t bytes) {
+int allow_smem(Kernel kernel, std::atomic<bool> (&known)[64], size_t bytes, int most = kSmemLimitDefault) {
     if (bytes <= 48 * 1024) return TDX_OK;
     int dev = 0;
     TDX_CUDA(cudaGetDevice(&dev));
     const bool listed = dev >= 0 && dev < 64;
     if (listed && known[dev].load(std::memory_order_acquire)) return TDX_OK;
-    TDX_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimitDefault));
+    TDX_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
     if (listed) known[dev].store(true, std::memory_order_release);
     return TDX_OK;
 }

@@ -79,3 +79,43 @@ def test_grouped_sizes_and_empty_calls():
     assert tdx.tdx_gemm_grouped(grouped(experts=0, offsets=None)) == 0
     assert tdx.tdx_gemm_grouped_dx(grouped(K=0, dx=None)) == 0 and tdx.tdx_gemm_grouped_dw(grouped(N=0, dweight=None)) == 0
     assert tdx.lib().tdx_gemm_grouped(None, None) == INVALID
+
+
+def attention(**change):
+    a = dict(batch=2, max_len=5, rows=10, heads=4, q_heads=4, k_heads=2, v_heads=2, dim_k=8, dim_v=16, dtype=tdx.TDX_BF16, scale=0.5, log_decay=P, q=P, ld_q=32,
+             k=P, ld_k=16, v=P, ld_v=32, out=P, ld_out=64, state_in=P, state_out=P, n_slots=2, dout=P, ld_dout=64, dq=P, ld_dq=32, dk=P, ld_dk=16, dv=P, ld_dv=32,
+             dstate_out=P, dstate_in=P, workspace=P, workspace_bytes=1 << 40)
+    return tdx.tdx_attention_args(**{**a, **change})
+
+
+ATTENTION_BAD = [
+    (dict(batch=-1), INVALID), (dict(heads=-1), INVALID), (dict(rows=9), INVALID), (dict(dtype=3), INVALID), (dict(q_heads=3), INVALID), (dict(k_heads=-2), INVALID),
+    (dict(v_heads=8), INVALID), (dict(dim_k=0), INVALID), (dict(dim_v=-1), INVALID), (dict(dim_k=129, ld_q=1000, ld_k=1000), UNSUPPORTED),
+    (dict(dim_v=200, ld_v=1000, ld_out=1000, ld_dout=1000), UNSUPPORTED), (dict(scale=float("inf")), INVALID), (dict(log_decay=None), INVALID), (dict(q=None), INVALID),
+    (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(ld_q=31), INVALID), (dict(ld_k=15), INVALID), (dict(ld_v=31), INVALID), (dict(n_slots=1), INVALID),
+    (dict(state_stride=100), INVALID), (dict(q=P + 1), ALIGNMENT), (dict(log_decay=P + 2), ALIGNMENT), (dict(slots=P + 2), ALIGNMENT), (dict(seq_offsets=P + 1), ALIGNMENT),
+    (dict(state_in=P + 2), ALIGNMENT), (dict(max_len=1 << 31, rows=1 << 32), UNSUPPORTED)]
+ROWLESS = ("rows", "max_len", "seq_offsets")
+
+
+@pytest.mark.parametrize("call,change,status", [
+    ("", dict(out=None), INVALID), ("", dict(ld_out=63), INVALID), ("", dict(state_out=P + 2), ALIGNMENT), ("_bwd", dict(dout=None), INVALID), ("_bwd", dict(dq=None), INVALID),
+    ("_bwd", dict(dk=None), INVALID), ("_bwd", dict(dv=None), INVALID), ("_bwd", dict(ld_dout=63), INVALID), ("_bwd", dict(ld_dk=15), INVALID),
+    ("_bwd", dict(dstate_in=P + 1), ALIGNMENT), ("_step", dict(state_in=None), INVALID), ("_step", dict(state_out=None), INVALID), ("_step", dict(out=None), INVALID),
+    *[(c, *bad) for c in ("", "_bwd") for bad in ATTENTION_BAD], *[("_step", *bad) for bad in ATTENTION_BAD if not any(n in bad[0] for n in ROWLESS)]])
+def test_attention_refusals(call, change, status):
+    assert getattr(tdx, "tdx_decay_attention" + call)(attention(**change)) == status, tdx.tdx_last_error()
+    assert tdx.tdx_last_error()
+
+
+def test_attention_sizes_and_empty_calls():
+    status, small = tdx.tdx_decay_attention_workspace_size(attention(dout=None))
+    assert status == 0 and small == 0                            # short sequences run whole
+    status, cut = tdx.tdx_decay_attention_workspace_size(attention(batch=1, max_len=4096, rows=4096, dout=None))
+    assert status == 0 and cut > 0
+    status, back = tdx.tdx_decay_attention_workspace_size(attention())
+    assert status == 0 and back >= 10 * 4 * 16 * 4               # one gradient a head before heads that share are summed
+    assert tdx.tdx_decay_attention_workspace_size(attention(dim_k=0))[0] == INVALID
+    assert tdx.tdx_decay_attention(attention(batch=0, rows=0)) == 0 and tdx.tdx_decay_attention_step(attention(batch=0)) == 0
+    assert tdx.tdx_decay_attention_bwd(attention(heads=0, q_heads=0, k_heads=0, v_heads=0)) == 0
+    assert tdx.lib().tdx_decay_attention(None, None) == INVALID and tdx.lib().tdx_decay_attention_step(None, None) == INVALID
