@@ -66,14 +66,21 @@ __device__ __forceinline__ void attn_split(float lo, float hi, uint32_t (&piece)
         if (i + 1 < N) { lo -= attn_lo(piece[i]); hi -= attn_hi(piece[i]); }
     }
 }
-// d += a b over all pairs of pieces that reach 2^-24 of the product
-template <int NA, int NB>
+// d += a b over all pairs of pieces that reach 2^-24 of the product.  EXACT: the products of 16 terms are summed on their own and then
+// added to d in fp32.  The tensor cores cut off what a term has below the sum's last bit instead of rounding, always towards zero: over
+// thousands of rows a sum held there is 3e-6 too small, added up this way it is 2e-7 off.
+template <bool EXACT, int NA, int NB>
 __device__ __forceinline__ void attn_mma_pieces(float (&d)[4], const uint32_t (&a)[NA][4], const uint32_t (&b0)[NB], const uint32_t (&b1)[NB]) {
+    float t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = NA - 1; i >= 0; --i)                            // small terms first
 #pragma unroll
         for (int j = NB - 1; j >= 0; --j)
-            if (i + j < (NA > NB ? NA : NB)) attn_mma(d, a[i], b0[j], b1[j]);
+            if (i + j < (NA > NB ? NA : NB)) attn_mma(EXACT ? t : d, a[i], b0[j], b1[j]);
+    if (EXACT) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] += t[i];
+    }
 }
 
 template <typename T, int KD>
@@ -255,8 +262,8 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
                         attn_ldm_t(f, smem + kStateAt + i * Tiles::kS + (kk * 16 + lane % 16) * PV + b * 32 + lane / 16 * 16);
                         b0[i] = f[0]; b1[i] = f[1]; b2[i] = f[2]; b3[i] = f[3];
                     }
-                    attn_mma_pieces(o[2 * b], fq, b0, b1);
-                    attn_mma_pieces(o[2 * b + 1], fq, b2, b3);
+                    attn_mma_pieces<NP == 3>(o[2 * b], fq, b0, b1);
+                    attn_mma_pieces<NP == 3>(o[2 * b + 1], fq, b2, b3);
                 }
 #pragma unroll
                 for (int b = 0; b < kAttnC / 16; ++b) {          // q k^T up to the diagonal
@@ -268,8 +275,8 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
                             attn_ldm(f, tk + i * Tiles::kK + (b * 16 + lane % 8 + lane / 16 * 8) * PK + kk * 32 + (lane >> 3 & 1) * 16);
                             b0[i] = f[0]; b1[i] = f[1]; b2[i] = f[2]; b3[i] = f[3];
                         }
-                        attn_mma_pieces(s[2 * b], fq, b0, b1);
-                        attn_mma_pieces(s[2 * b + 1], fq, b2, b3);
+                        attn_mma_pieces<NP == 3>(s[2 * b], fq, b0, b1);
+                        attn_mma_pieces<NP == 3>(s[2 * b + 1], fq, b2, b3);
                     }
                 }
             }
@@ -306,8 +313,8 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
                             attn_ldm_t(f, tv + i * Tiles::kV + (kk * 16 + lane % 16) * PV + b * 32 + lane / 16 * 16);
                             b0[i] = f[0]; b1[i] = f[1]; b2[i] = f[2]; b3[i] = f[3];
                         }
-                        attn_mma_pieces(o[2 * b], fp, b0, b1);
-                        attn_mma_pieces(o[2 * b + 1], fp, b2, b3);
+                        attn_mma_pieces<NP == 3>(o[2 * b], fp, b0, b1);
+                        attn_mma_pieces<NP == 3>(o[2 * b + 1], fp, b2, b3);
                     }
                 }
             }
@@ -390,8 +397,8 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
                 }
 #pragma unroll
                 for (int a = 0; a < MT; ++a) {
-                    attn_mma_pieces(st[a][2 * b], fk[a], b0, b1);
-                    attn_mma_pieces(st[a][2 * b + 1], fk[a], b2, b3);
+                    attn_mma_pieces<UP == 3>(st[a][2 * b], fk[a], b0, b1);
+                    attn_mma_pieces<UP == 3>(st[a][2 * b + 1], fk[a], b2, b3);
                 }
             }
         }

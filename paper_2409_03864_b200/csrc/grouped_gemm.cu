@@ -49,6 +49,62 @@ template <typename T, int PASS>
 int launch_grouped_rows(const tdx::GroupedParams& p, cudaStream_t st) {
     return p.rows <= 16 * static_cast<int64_t>(p.experts) && PASS != tdx::kGroupedDw ? launch_grouped_simt<T, PASS, 16>(p, st) : launch_grouped_simt<T, PASS, 64>(p, st);
 }
+
+// The tensor-core kernel reads operands by the copy engine and writes 16 bytes at a time.
+bool grouped_fast(const tdx_grouped_args& a, const tdx::GroupedParams& p, int pass) {
+    if (a.dtype != TDX_BF16 || a.rows == 0 || a.N == 0 || a.K == 0 || a.experts > tdx::kGroupedMostExperts) return false;
+    Widest w(16);
+    w.stride(a.K, 2);
+    w.stride(a.N, 2);
+    w.ptr(p.a); w.stride(p.ld_a, 2);
+    w.ptr(p.b); w.ptr(p.out);
+    if (pass == tdx::kGroupedDw) w.stride(p.ld_b, 2);
+    else w.stride(p.ld_out, 2);
+    return w.bytes == 16;
+}
+
+template <int PASS>
+int launch_grouped_umma(tdx::GroupedParams p, const tdx_host::Device& dev, cudaStream_t st) {
+    p.features = PASS == tdx::kGroupedDx ? p.K : p.N;
+    const int depth = PASS == tdx::kGroupedForward ? p.K : p.N;
+    const int64_t rows_each = ceil_div(p.rows, p.experts);
+    if (PASS == tdx::kGroupedDw) {
+        p.bt = 128;
+        p.halves = p.N > 128 ? 2 : 1;
+    } else {
+        p.bt = rows_each <= 16 ? 32 : rows_each <= 48 ? 64 : 128;
+        p.halves = p.bt == 128 && p.features > 128 ? 2 : 1;
+    }
+    p.box = std::min(p.bt, 64);
+    p.feature_tiles = static_cast<int>(ceil_div(p.features, 128 * p.halves));
+    p.column_tiles = static_cast<int>(ceil_div(p.K, p.bt));
+    p.blocks = static_cast<int>(ceil_div(depth, 64));
+    p.tmem_cols = 32;
+    while (p.tmem_cols < 2 * p.halves * p.bt) p.tmem_cols *= 2;
+    const int stage = p.halves * 16384 + p.bt * 128;
+    const size_t fixed = 1024 + tdx::kGroupedStaging + sizeof(int) * (p.experts + 1);
+    const int room = dev.smem_optin - 1024;                       // barriers are static
+    p.stages = static_cast<int>(std::min<int64_t>(tdx::kGroupedMostStages, (room - static_cast<int64_t>(fixed)) / stage));
+    const uint64_t K = p.K, N = p.N, rows = p.rows, E = p.experts;
+    CUtensorMap a, b;
+    if (PASS == tdx::kGroupedDw) {
+        const uint64_t da[2] = {N, rows}, sa[1] = {static_cast<uint64_t>(p.ld_a) * 2}, db[2] = {K, rows}, sb[1] = {static_cast<uint64_t>(p.ld_b) * 2};
+        const uint32_t box[2] = {64, 64};
+        TDX_TRY(tdx_host::bf16_map(p.a, 2, da, sa, box, &a));
+        TDX_TRY(tdx_host::bf16_map(p.b, 2, db, sb, box, &b));
+    } else {
+        const uint64_t dw[3] = {K, N, E}, sw[2] = {K * 2, K * N * 2}, dx[2] = {static_cast<uint64_t>(depth), rows}, sx[1] = {static_cast<uint64_t>(p.ld_a) * 2};
+        const uint32_t box_w[3] = {64, PASS == tdx::kGroupedForward ? 128u : 64u, 1}, box_x[2] = {64, static_cast<uint32_t>(p.box)};
+        TDX_TRY(tdx_host::bf16_map(p.b, 3, dw, sw, box_w, &a));
+        TDX_TRY(tdx_host::bf16_map(p.a, 2, dx, sx, box_x, &b));
+    }
+    const int64_t items = PASS == tdx::kGroupedDw ? E * p.feature_tiles * static_cast<int64_t>(p.column_tiles) : (p.rows / p.bt + p.experts) * p.feature_tiles;
+    const size_t smem = fixed + static_cast<size_t>(p.stages) * stage;
+    static std::atomic<bool> known[64];
+    TDX_TRY(allow_smem(tdx::grouped_umma_kernel<PASS>, known, smem, room));
+    return launch_seq(tdx::grouped_umma_kernel<PASS>, std::min<int64_t>(items, dev.sm_count), 1, tdx::kGroupedThreads, smem, st, a, b, p);
+}
+
 template <int PASS>
 int run_grouped(const tdx_grouped_args* args, void* stream) {
     tdx::GroupedParams p;
@@ -58,6 +114,7 @@ int run_grouped(const tdx_grouped_args* args, void* stream) {
     TDX_TRY(tdx_host::get_device(&dev));
     p.status = dev.status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (grouped_fast(*args, p, PASS)) return launch_grouped_umma<PASS>(p, dev, st);
     return args->dtype == TDX_F32 ? launch_grouped_rows<float, PASS>(p, st) : launch_grouped_rows<__nv_bfloat16, PASS>(p, st);
 }
 

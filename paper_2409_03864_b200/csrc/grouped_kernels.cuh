@@ -23,11 +23,13 @@ struct GroupedParams {
     void* out;
     long long ld_a, ld_b, ld_out;
     int* status;
-    // tensor-core kernel
-    int stages;
-    int out_tiles;                   // tiles of 128 * HALVES output features
-    int red_blocks;                  // blocks of 64 of the reduction (forward, dx)
-    int col_tiles;                   // dw: tiles of kBT columns
+    // tensor-core kernel: tiles of 128 * halves output features and bt rows (dw: bt columns)
+    int halves, bt, box;             // box: rows of one copy of the activations
+    int stages, tmem_cols;
+    int features;                    // of the output's feature dimension: N, K, or (dw) N
+    int feature_tiles;
+    int blocks;                      // of 64 of the reduction (forward, dx)
+    int column_tiles;                // dw
 };
 
 // The range of an expert's rows; one that leaves [0, rows] or descends is reported and empty.
@@ -140,6 +142,276 @@ __global__ void __launch_bounds__(128) grouped_simt_kernel(const __grid_constant
             const int n = n0 + tn + (j < 4 ? j : 60 + j);
             if (n < n_count) row[n] = seq_from_float<T>(acc[i][j]);
         }
+    }
+}
+
+// ---------------------------------------------------------------- tensor cores
+// Persistent, one block an SM: warp 0 copies 128-byte-swizzled tiles of 64 of the reduction into a ring of stages (TMA), warp 1 issues the
+// tcgen05 products, eight warps turn accumulators into bf16.  The features are the product's M (128 or two times 128) and the rows of an
+// expert its N: an expert's last tile then costs what its rows need, in steps of 16, instead of a whole tile of 128, and a few rows cost
+// 32 columns of a product that streams the weights.  Accumulators are held twice, so a tile's epilogue runs under the next tile's products.
+// dw sums over an expert's rows: both operands are read with the rows as the reduction, and rows of the last block that belong to the
+// next expert are set to zero in shared memory in front of the product (a factor of zero in one operand would leave NaN and infinity).
+constexpr int kGroupedMostExperts = 1024;                        // whose tile counts are kept in shared memory
+constexpr int kGroupedThreads = 320;
+constexpr int kGroupedEpilogueWarps = 8;
+constexpr int kGroupedStagePitch = 80;                           // bytes of a staged row of 32 bf16
+constexpr int kGroupedStaging = kGroupedEpilogueWarps * 32 * kGroupedStagePitch;
+constexpr int kGroupedMostStages = 10;
+
+struct GroupedTile {
+    long long row;                   // first row of the tile (dw: of the expert)
+    int expert, count;               // rows of the tile (dw: of the expert)
+    int feature, column;             // first feature, and (dw) first column
+    int blocks;                      // of 64 of the reduction
+};
+
+template <int PASS>
+__device__ __forceinline__ bool grouped_tile(const GroupedParams& p, const int* first, long long item, GroupedTile* t) {
+    if (PASS == kGroupedDw) {
+        const int per = p.feature_tiles * p.column_tiles;
+        if (item >= static_cast<long long>(per) * p.experts) return false;
+        t->expert = static_cast<int>(item / per);
+        const int in = static_cast<int>(item - static_cast<long long>(t->expert) * per);
+        t->feature = in / p.column_tiles * (128 * p.halves);
+        t->column = in % p.column_tiles * p.bt;
+        const int lo = __ldg(p.offsets + t->expert), hi = __ldg(p.offsets + t->expert + 1);
+        t->row = lo;
+        t->count = seq_accepted(lo, hi, p.rows, p.rows) ? hi - lo : 0;
+        t->blocks = (t->count + 63) / 64;
+        return true;
+    }
+    if (item >= static_cast<long long>(first[p.experts]) * p.feature_tiles) return false;
+    const int number = static_cast<int>(item / p.feature_tiles);
+    int lo = 0, hi = p.experts - 1;                              // the last expert whose tiles start at or before `number`
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (first[mid] <= number) lo = mid;
+        else hi = mid - 1;
+    }
+    // an expert's tiles of rows lie side by side for each tile of features, so that its weights are read together
+    const int tiles = first[lo + 1] - first[lo];
+    const int in = static_cast<int>(item - static_cast<long long>(first[lo]) * p.feature_tiles), f = in / tiles, r = in - f * tiles;
+    const int from = __ldg(p.offsets + lo), to = __ldg(p.offsets + lo + 1);
+    t->expert = lo;
+    t->row = from + static_cast<long long>(r) * p.bt;
+    t->count = min(p.bt, to - from - r * p.bt);
+    t->feature = f * (128 * p.halves);
+    t->column = 0;
+    t->blocks = p.blocks;
+    return true;
+}
+
+template <int PASS>
+__global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
+                                                                          const __grid_constant__ GroupedParams p) {
+    extern __shared__ uint8_t grouped_smem[];
+    __shared__ __align__(8) uint64_t full_bar[kGroupedMostStages], empty_bar[kGroupedMostStages], tfull_bar[2], tempty_bar[2];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort;
+    volatile int* abort_flag = &s_abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t a_bytes = static_cast<uint32_t>(p.halves) * 16384u, stage_bytes = a_bytes + static_cast<uint32_t>(p.bt) * 128u;
+    uint8_t* const ring = grouped_smem + ((1024u - (ptx::smem_u32(grouped_smem) & 1023u)) & 1023u);
+    uint8_t* const staging = ring + static_cast<size_t>(p.stages) * stage_bytes;
+    int* const first = reinterpret_cast<int*>(staging + kGroupedStaging);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            ptx::mbar_init(&full_bar[s], 1);
+            ptx::mbar_init(&empty_bar[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            ptx::mbar_init(&tfull_bar[b], 1);
+            ptx::mbar_init(&tempty_bar[b], kGroupedEpilogueWarps);
+        }
+        s_abort = 0;
+        ptx::fence_barrier_init();
+        ptx::tma_prefetch_desc(&tm_a);
+        ptx::tma_prefetch_desc(&tm_b);
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(&s_tmem, static_cast<uint32_t>(p.tmem_cols));
+        ptx::tmem_relinquish();
+    }
+    ptx::grid_dependency_wait();
+    if (warp == 0) {
+        // the experts' numbers of tiles, added up
+        int sum = 0;
+        if (lane == 0) first[0] = 0;
+        for (int e0 = 0; e0 < p.experts; e0 += 32) {
+            const int e = e0 + lane;
+            int n = e < p.experts ? (grouped_range(p, e).len + p.bt - 1) / p.bt : 0;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int up = __shfl_up_sync(0xffffffffu, n, d);
+                if (lane >= d) n += up;
+            }
+            if (e < p.experts) first[e + 1] = sum + n;
+            sum += __shfl_sync(0xffffffffu, n, 31);
+        }
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = s_tmem;
+
+    if (warp == 0) {
+        if (ptx::elect_one()) {
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            GroupedTile t;
+            for (long long item = blockIdx.x; ok && grouped_tile<PASS>(p, first, item, &t); item += gridDim.x) {
+                const int boxes = PASS == kGroupedDw ? p.bt / 64 : (t.count + p.box - 1) / p.box;
+                const uint32_t bytes = a_bytes + static_cast<uint32_t>(boxes) * (PASS == kGroupedDw ? 8192u : static_cast<uint32_t>(p.box) * 128u);
+                for (int kb = 0; kb < t.blocks; ++kb) {
+                    if (!wait_bounded(&empty_bar[stage], phase ^ 1u, abort_flag, p.status, kTimeoutProducer)) {
+                        ok = false;
+                        break;
+                    }
+                    uint64_t* bar = &full_bar[stage];
+                    ptx::mbar_arrive_expect_tx(bar, bytes);
+                    uint8_t* a = ring + static_cast<size_t>(stage) * stage_bytes;
+                    uint8_t* b = a + a_bytes;
+                    const int at = kb * 64, row = static_cast<int>(t.row);
+                    if (PASS == kGroupedForward) {
+                        for (int h = 0; h < p.halves; ++h) ptx::tma_load_3d(a + h * 16384, &tm_a, bar, at, t.feature + h * 128, t.expert);
+                    } else if (PASS == kGroupedDx) {
+                        for (int i = 0; i < 2 * p.halves; ++i) ptx::tma_load_3d(a + i * 8192, &tm_a, bar, t.feature + i * 64, at, t.expert);
+                    } else {
+                        for (int i = 0; i < 2 * p.halves; ++i) ptx::tma_load_2d(a + i * 8192, &tm_a, bar, t.feature + i * 64, row + at);
+                    }
+                    if (PASS == kGroupedDw) {
+                        for (int i = 0; i < boxes; ++i) ptx::tma_load_2d(b + i * 8192, &tm_b, bar, t.column + i * 64, row + at);
+                    } else {
+                        for (int i = 0; i < boxes; ++i) ptx::tma_load_2d(b + i * p.box * 128, &tm_b, bar, at, row + i * p.box);
+                    }
+                    if (++stage == p.stages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+            }
+            if (!ok) {
+                // let copies that are still in flight land before the block goes away
+                for (int i = 0; i < 64; ++i) __nanosleep(2000);
+            }
+        }
+    } else if (warp == 1) {
+        constexpr bool kATurned = PASS != kGroupedForward, kBTurned = PASS == kGroupedDw;   // the reduction is not the contiguous dimension
+        const uint64_t a_desc0 = ptx::make_smem_desc_sw128(ptx::smem_u32(ring), kATurned ? 8192u : 16u, 1024u);
+        const uint64_t b_desc0 = ptx::make_smem_desc_sw128(ptx::smem_u32(ring) + a_bytes, kBTurned ? 8192u : 16u, 1024u);
+        constexpr uint64_t a_k16 = (kATurned ? 2048u : 32u) >> 4, b_k16 = (kBTurned ? 2048u : 32u) >> 4;
+        int stage = 0, local = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        GroupedTile t;
+        for (long long item = blockIdx.x; ok && grouped_tile<PASS>(p, first, item, &t); item += gridDim.x, ++local) {
+            const int buf = local & 1;
+            if (!wait_bounded(&tempty_bar[buf], (local >> 1 & 1) ^ 1u, abort_flag, p.status, kTimeoutMma)) break;
+            ptx::tc_fence_after_sync();
+            const int n = PASS == kGroupedDw ? p.bt : (t.count + 15) / 16 * 16;
+            const uint32_t idesc = ptx::make_idesc_bf16_f32(128, n, kATurned, kBTurned);
+            const uint32_t d = tmem + static_cast<uint32_t>(buf * p.halves * p.bt);
+            for (int kb = 0; kb < t.blocks; ++kb) {
+                if (!wait_bounded(&full_bar[stage], phase, abort_flag, p.status, kTimeoutMma)) {
+                    ok = false;
+                    break;
+                }
+                int steps = 4;
+                if (PASS == kGroupedDw && kb + 1 == t.blocks) {
+                    // the rows behind the expert's last one, up to the end of the last step of 16
+                    const int left = t.count - kb * 64;
+                    steps = (left + 15) / 16;
+                    uint8_t* base = ring + static_cast<size_t>(stage) * stage_bytes;
+                    const int rows = steps * 16 - left, tiles = 2 * p.halves + p.bt / 64;
+                    for (int i = lane; i < tiles * rows * 8; i += 32) {
+                        const int tile = i / (rows * 8), in = i - tile * rows * 8;
+                        *reinterpret_cast<uint4*>(base + tile * 8192 + (left + in / 8) * 128 + in % 8 * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                }
+                ptx::tc_fence_after_sync();
+                if (ptx::elect_one()) {
+                    const uint64_t at = static_cast<uint64_t>(static_cast<uint32_t>(stage) * stage_bytes) >> 4;
+                    for (int h = 0; h < p.halves; ++h) {
+                        for (int j = 0; j < steps; ++j)
+                            ptx::umma_bf16(d + static_cast<uint32_t>(h * p.bt), a_desc0 + at + h * (16384u >> 4) + j * a_k16, b_desc0 + at + j * b_k16, idesc,
+                                           kb > 0 || j > 0 ? 1u : 0u);
+                    }
+                    ptx::umma_commit(&empty_bar[stage]);
+                    if (kb + 1 == t.blocks) ptx::umma_commit(&tfull_bar[buf]);
+                }
+                __syncwarp();
+                if (++stage == p.stages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
+            if (t.blocks == 0 && ptx::elect_one()) ptx::mbar_arrive(&tfull_bar[buf]);
+            __syncwarp();
+        }
+    } else {
+        const int ew = warp - 2, quarter = warp & 3, half = p.halves == 2 ? ew >> 2 : 0;
+        const int c_first = p.halves == 2 ? 0 : (ew >> 2) * 32, c_step = p.halves == 2 ? 32 : 64;
+        uint8_t* const mine = staging + ew * 32 * kGroupedStagePitch;
+        __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out);
+        int local = 0;
+        GroupedTile t;
+        for (long long item = blockIdx.x; grouped_tile<PASS>(p, first, item, &t); item += gridDim.x, ++local) {
+            const int buf = local & 1;
+            if (!wait_bounded(&tfull_bar[buf], local >> 1 & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+            ptx::tc_fence_after_sync();
+            const int feature = t.feature + half * 128 + quarter * 32;
+            const int columns = PASS == kGroupedDw ? min(p.bt, p.K - t.column) : t.count;
+            for (int c0 = c_first; c0 < columns; c0 += c_step) {
+                uint32_t r[32];
+                ptx::tmem_ld_32x32b_x32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>((buf * p.halves + half) * p.bt + c0), r);
+                ptx::tmem_ld_wait();
+                if (PASS == kGroupedDw) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+                        pk[j] = t.blocks > 0 ? *reinterpret_cast<uint32_t*>(&h) : 0u;     // an expert without rows
+                    }
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        *reinterpret_cast<uint4*>(mine + lane * kGroupedStagePitch + g * 16) = make_uint4(pk[4 * g], pk[4 * g + 1], pk[4 * g + 2], pk[4 * g + 3]);
+                } else {
+                    // a lane has a feature, an output row wants them side by side
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        *reinterpret_cast<__nv_bfloat16*>(mine + j * kGroupedStagePitch + lane * 2) = __float2bfloat16_rn(__uint_as_float(r[j]));
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = lane / 4 + i * 8, part = lane % 4 * 8;
+                    const uint4 v = *reinterpret_cast<const uint4*>(mine + row * kGroupedStagePitch + part * 2);
+                    if (PASS == kGroupedDw) {
+                        const int column = t.column + c0 + part;
+                        if (feature + row < p.N && column < p.K)
+                            *reinterpret_cast<uint4*>(out + (static_cast<long long>(t.expert) * p.N + feature + row) * p.K + column) = v;
+                    } else if (c0 + row < t.count && feature + part < p.features) {
+                        *reinterpret_cast<uint4*>(out + (t.row + c0 + row) * p.ld_out + feature + part) = v;
+                    }
+                }
+                __syncwarp();
+            }
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&tempty_bar[buf]);
+        }
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) {
+        ptx::tc_fence_after_sync();
+        __syncwarp();
+        ptx::tmem_dealloc(tmem, static_cast<uint32_t>(p.tmem_cols));
     }
 }
 

@@ -34,12 +34,12 @@ struct NormParams {
 };
 
 constexpr int kNormThreads = 512;    // at most; 16 channels a thread are then rows of up to 8192
-constexpr int kNormShared = 2 * 16;  // row sums of up to 16 warps, twice
+constexpr int kNormShared = 2 * 32;  // two row sums of up to 16 warps, twice
 
 // The threads that share a row, and the sums they take.
 struct NormRow {
     int lane, warp, warps, thread, threads, slot;   // thread: within the row; slot: the row's number within the block
-    float* sums;                                    // [2][16] of this row
+    float* sums;                                    // [2][32] of this row
     float* vec;                                     // [vectors] of this row (group_lanes = -1)
     int turn;
     __device__ __forceinline__ void sync() const {
@@ -51,13 +51,32 @@ struct NormRow {
 #pragma unroll
         for (int m = 16; m > 0; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
         if (warps == 1) return v;
-        float* s = sums + turn * 16;
+        float* s = sums + turn * 32;
         turn ^= 1;
         if (lane == 0) s[warp] = v;
         sync();
         float t = 0.0f;
         for (int w = 0; w < warps; ++w) t += s[w];
         return t;
+    }
+    // two sums over the row behind one barrier
+    __device__ __forceinline__ void row_sums(float& v, float& w) {
+#pragma unroll
+        for (int m = 16; m > 0; m >>= 1) {
+            v += __shfl_xor_sync(0xffffffffu, v, m);
+            w += __shfl_xor_sync(0xffffffffu, w, m);
+        }
+        if (warps == 1) return;
+        float* s = sums + turn * 32;
+        turn ^= 1;
+        if (lane == 0) *reinterpret_cast<float2*>(s + 2 * warp) = make_float2(v, w);
+        sync();
+        v = w = 0.0f;
+        for (int i = 0; i < warps; ++i) {
+            const float2 t = *reinterpret_cast<const float2*>(s + 2 * i);
+            v += t.x;
+            w += t.y;
+        }
     }
     // v[i]: this thread's part of vector thread + i * threads; becomes the sum over the vector's group
     template <int NV>
@@ -137,21 +156,32 @@ __device__ __forceinline__ NormRow norm_row(const NormParams& p, float* shared) 
 }
 
 template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const __grid_constant__ NormParams p) {
+__global__ void __launch_bounds__(kNormThreads, NV * VEC <= 8 ? 2 : 1) norm_fwd_kernel(const __grid_constant__ NormParams p) {
     extern __shared__ float norm_shared[];
     NormRow r = norm_row(p, norm_shared);
     const int sets = (blockDim.x >> 5) / p.warps;
     seq_grid_wait();
-    for (long long row = static_cast<long long>(blockIdx.x) * sets + r.slot; row < p.rows; row += static_cast<long long>(gridDim.x) * sets) {
-        SeqVec<T, VEC> vx[NV], vg[NV], vr[NV];
+    const long long step = static_cast<long long>(gridDim.x) * sets;
+    SeqVec<T, VEC> nx[NV], ng[NV], nr[NV];
+    auto fetch = [&](long long row) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (r.thread + i * r.threads) * VEC;
-            const bool there = c < p.channels;
-            vx[i] = norm_load<T, VEC>(p.x, p.ld_x, row, c, there);
-            vg[i] = norm_load<T, VEC>(p.gate, p.ld_gate, row, c, there);
-            vr[i] = norm_load<T, VEC>(p.residual, p.ld_residual, row, c, there);
+            const bool there = c < p.channels && row < p.rows;
+            nx[i] = norm_load<T, VEC>(p.x, p.ld_x, row, c, there);
+            ng[i] = norm_load<T, VEC>(p.gate, p.ld_gate, row, c, there);
+            nr[i] = norm_load<T, VEC>(p.residual, p.ld_residual, row, c, there);
         }
+    };
+    constexpr bool kAhead = NV * VEC <= 8;                       // wider threads have no registers to spare
+    long long row = static_cast<long long>(blockIdx.x) * sets + r.slot;
+    if (kAhead) fetch(row);
+    for (; row < p.rows; row += step) {
+        if (!kAhead) fetch(row);
+        SeqVec<T, VEC> vx[NV], vg[NV], vr[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) { vx[i] = nx[i]; vg[i] = ng[i]; vr[i] = nr[i]; }
+        if (kAhead) fetch(row + step);                           // on its way while this row is worked on
         float rstd[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -230,18 +260,48 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_con
 #pragma unroll
         for (int j = 0; j < VEC; ++j) sum_in[i][j] = sum_scale[i][j] = sum_out[i][j] = 0.0f;
     seq_grid_wait();
-    for (long long row = set; row < p.rows; row += static_cast<long long>(gridDim.x) * sets) {
-        SeqVec<T, VEC> vx[NV], vg[NV], vr[NV], vs[NV], vy[NV];
+    const long long step = static_cast<long long>(gridDim.x) * sets;
+    // with up to 8 channels a thread the registers hold the next row's vectors and the parameters too
+    constexpr bool kAhead = NV * VEC <= 8;
+    SeqVec<T, VEC> vx[NV], vg[NV], vr[NV], vs[NV], vy[NV], nx[NV], ng[NV], nr[NV], ns[NV], ny[NV];
+    auto fetch = [&](long long row) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (r.thread + i * r.threads) * VEC;
-            const bool there = c < p.channels;
-            vx[i] = norm_load<T, VEC>(p.x, p.ld_x, row, c, there);
-            vg[i] = norm_load<T, VEC>(p.gate, p.ld_gate, row, c, there);
-            vr[i] = norm_load<T, VEC>(p.residual, p.ld_residual, row, c, there && p.dy != nullptr);
-            vs[i] = norm_load<T, VEC>(p.dsum, p.ld_dsum, row, c, there);
-            vy[i] = norm_load<T, VEC>(p.dy, p.ld_dy, row, c, there);
+            const bool there = c < p.channels && row < p.rows;
+            nx[i] = norm_load<T, VEC>(p.x, p.ld_x, row, c, there);
+            ng[i] = norm_load<T, VEC>(p.gate, p.ld_gate, row, c, there);
+            nr[i] = norm_load<T, VEC>(p.residual, p.ld_residual, row, c, there && p.dy != nullptr);
+            ns[i] = norm_load<T, VEC>(p.dsum, p.ld_dsum, row, c, there);
+            ny[i] = norm_load<T, VEC>(p.dy, p.ld_dy, row, c, there);
         }
+    };
+    if (kAhead) fetch(set);
+    float keep_in[NV][VEC], keep_scale[NV][VEC], keep_out[NV][VEC];
+    if (kAhead) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (r.thread + i * r.threads) * VEC;
+            if (c < p.channels) {
+                norm_param(p.norm_in ? p.weight_in : nullptr, c, keep_in[i]);
+                norm_param(p.scale, c, keep_scale[i]);
+                norm_param(p.weight_out, c, keep_out[i]);
+            }
+        }
+    }
+    auto param = [&](const float* from, const float (&kept)[VEC], int c, float (&f)[VEC]) {
+        if (kAhead) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) f[j] = kept[j];
+        } else {
+            norm_param(from, c, f);
+        }
+    };
+    for (long long row = set; row < p.rows; row += step) {
+        if (!kAhead) fetch(row);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) { vx[i] = nx[i]; vg[i] = ng[i]; vr[i] = nr[i]; vs[i] = ns[i]; vy[i] = ny[i]; }
+        if (kAhead) fetch(row + step);
         float rstd[NV];
         if (p.norm_in) {
 #pragma unroll
@@ -260,7 +320,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_con
             for (int i = 0; i < NV; ++i) rstd[i] = 1.0f;
         }
         // the way forward once more: xh = x rstd, a; then ds
-        float ds[NV][VEC], a[NV][VEC];
+        float ds[NV][VEC], a[NV][VEC], sig[NV][VEC];
         float square = 0.0f, inner = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -268,19 +328,22 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_con
             if (c < p.channels) {
                 float w[VEC];
                 seq_unpack(vx[i], a[i]);
-                norm_param(p.norm_in ? p.weight_in : nullptr, c, w);
+                param(p.norm_in ? p.weight_in : nullptr, keep_in[i], c, w);
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) a[i][j] *= rstd[i] * w[j];
                 if (p.gate != nullptr) {
                     float g[VEC];
                     seq_unpack(vg[i], g);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) a[i][j] *= g[j] * sigmoid_f<T>(g[j]);
+                    for (int j = 0; j < VEC; ++j) {
+                        sig[i][j] = sigmoid_f<T>(g[j]);
+                        a[i][j] *= g[j] * sig[i][j];
+                    }
                 }
                 if (p.dy != nullptr) {
                     float k[VEC], add[VEC], dy[VEC], wo[VEC];
-                    norm_param(p.scale, c, k);
-                    norm_param(p.weight_out, c, wo);
+                    param(p.scale, keep_scale[i], c, k);
+                    param(p.weight_out, keep_out[i], c, wo);
                     seq_unpack(vr[i], add);
                     seq_unpack(vy[i], dy);
 #pragma unroll
@@ -294,8 +357,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_con
         }
         float rs = 0.0f, mean = 0.0f;
         if (p.dy != nullptr) {
-            square = r.row_sum(square);
-            inner = r.row_sum(inner);
+            r.row_sums(square, inner);
             rs = rsqrtf(fmaf(square, p.inv_channels, p.eps));
             mean = inner * rs * p.inv_channels;                  // mean(t sh)
         }
@@ -306,11 +368,11 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_con
             group[i] = 0.0f;
             if (c < p.channels) {
                 float k[VEC], w[VEC], x[VEC];
-                norm_param(p.scale, c, k);
+                param(p.scale, keep_scale[i], c, k);
                 seq_unpack(vs[i], ds[i]);
                 if (p.dy != nullptr) {
                     float add[VEC], dy[VEC], wo[VEC];
-                    norm_param(p.weight_out, c, wo);
+                    param(p.weight_out, keep_out[i], c, wo);
                     seq_unpack(vr[i], add);
                     seq_unpack(vy[i], dy);
 #pragma unroll
@@ -322,7 +384,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_con
                 }
                 if (p.dresidual != nullptr) norm_store<T, VEC>(p.dresidual, p.ld_dresidual, row, c, ds[i]);
                 seq_unpack(vx[i], x);
-                norm_param(p.norm_in ? p.weight_in : nullptr, c, w);
+                param(p.norm_in ? p.weight_in : nullptr, keep_in[i], c, w);
                 float g[VEC], dg[VEC];
                 seq_unpack(vg[i], g);
 #pragma unroll
@@ -331,9 +393,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_con
                     const float da = ds[i][j] * k[j], xh = x[j] * rstd[i];
                     float du = da;
                     if (p.gate != nullptr) {
-                        const float sig = sigmoid_f<T>(g[j]);
-                        dg[j] = da * (xh * w[j]) * sig * fmaf(g[j], 1.0f - sig, 1.0f);
-                        du = da * (g[j] * sig);
+                        dg[j] = da * (xh * w[j]) * sig[i][j] * fmaf(g[j], 1.0f - sig[i][j], 1.0f);
+                        du = da * (g[j] * sig[i][j]);
                     }
                     sum_in[i][j] = fmaf(du, xh, sum_in[i][j]);
                     ds[i][j] = du * w[j];                        // t' from here on
