@@ -69,18 +69,19 @@ int launch_grouped_umma(tdx::GroupedParams p, const tdx_host::Device& dev, cudaS
     const int depth = PASS == tdx::kGroupedForward ? p.K : p.N;
     const int64_t rows_each = ceil_div(p.rows, p.experts);
     if (PASS == tdx::kGroupedDw) {
-        p.bt = 128;
+        p.bt = p.K > 128 ? 256 : 128;
         p.halves = p.N > 128 ? 2 : 1;
     } else {
-        p.bt = rows_each <= 16 ? 32 : rows_each <= 48 ? 64 : 128;
-        p.halves = p.bt == 128 && p.features > 128 ? 2 : 1;
+        p.bt = rows_each <= 16 ? 32 : rows_each <= 48 ? 64 : rows_each <= 128 ? 128 : 256;
+        p.halves = p.bt >= 128 && p.features > 128 ? 2 : 1;
     }
+    p.buffers = 2 * p.halves * p.bt <= 512 ? 2 : 1;
     p.box = std::min(p.bt, 64);
     p.feature_tiles = static_cast<int>(ceil_div(p.features, 128 * p.halves));
     p.column_tiles = static_cast<int>(ceil_div(p.K, p.bt));
     p.blocks = static_cast<int>(ceil_div(depth, 64));
     p.tmem_cols = 32;
-    while (p.tmem_cols < 2 * p.halves * p.bt) p.tmem_cols *= 2;
+    while (p.tmem_cols < p.buffers * p.halves * p.bt) p.tmem_cols *= 2;
     const int stage = p.halves * 16384 + p.bt * 128;
     const size_t fixed = 1024 + tdx::kGroupedStaging + sizeof(int) * (p.experts + 1);
     const int room = dev.smem_optin - 1024;                       // barriers are static

@@ -26,6 +26,7 @@ struct GroupedParams {
     // tensor-core kernel: tiles of 128 * halves output features and bt rows (dw: bt columns)
     int halves, bt, box;             // box: rows of one copy of the activations
     int stages, tmem_cols;
+    int buffers;                     // accumulators of a tile: 2, or 1 where one takes all 512 columns
     int features;                    // of the output's feature dimension: N, K, or (dw) N
     int feature_tiles;
     int blocks;                      // of 64 of the reduction (forward, dx)
@@ -308,8 +309,8 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
         bool ok = true;
         GroupedTile t;
         for (long long item = blockIdx.x; ok && grouped_tile<PASS>(p, first, item, &t); item += gridDim.x, ++local) {
-            const int buf = local & 1;
-            if (!wait_bounded(&tempty_bar[buf], (local >> 1 & 1) ^ 1u, abort_flag, p.status, kTimeoutMma)) break;
+            const int buf = local % p.buffers, use = local / p.buffers;
+            if (!wait_bounded(&tempty_bar[buf], (use & 1) ^ 1u, abort_flag, p.status, kTimeoutMma)) break;
             ptx::tc_fence_after_sync();
             const int n = PASS == kGroupedDw ? p.bt : (t.count + 15) / 16 * 16;
             const uint32_t idesc = ptx::make_idesc_bf16_f32(128, n, kATurned, kBTurned);
@@ -361,8 +362,8 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
         int local = 0;
         GroupedTile t;
         for (long long item = blockIdx.x; grouped_tile<PASS>(p, first, item, &t); item += gridDim.x, ++local) {
-            const int buf = local & 1;
-            if (!wait_bounded(&tfull_bar[buf], local >> 1 & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+            const int buf = local % p.buffers, use = local / p.buffers;
+            if (!wait_bounded(&tfull_bar[buf], use & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
             ptx::tc_fence_after_sync();
             const int feature = t.feature + half * 128 + quarter * 32;
             const int columns = PASS == kGroupedDw ? min(p.bt, p.K - t.column) : t.count;
