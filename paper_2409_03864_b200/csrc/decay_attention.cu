@@ -2,6 +2,7 @@
 #include "layer_host.cuh"
 
 #include "attention_kernels.cuh"
+#include "attention_umma.cuh"
 
 namespace {
 
@@ -53,19 +54,28 @@ int check_attention(const tdx_attention_args* args, AttnPass pass, AttnShape* sh
     return TDX_OK;
 }
 
-// How a sum is spread over the SMs.  Heads, slices of 64 columns and sequences run side by side; where they give fewer than two
-// blocks an SM (as many as are resident), sequences are cut into segments, which costs a second look at k and v for what each
-// segment adds to the state.
-void plan_attention(const tdx_attention_args& a, int d2, int sm_count, tdx::AttnParams* p) {
+// How a sum is spread over the SMs: the rows of a segment.  Heads (and, on the CUDA cores' kernel, slices of 64 columns) and sequences
+// run side by side; where they do not fill the SMs evenly, sequences are cut into segments, which costs a look at k and v of all but the
+// last one for what they add to the state (about half a segment's time) and two chunks' time a block for its start.  The number of segments
+// with the least estimated time is taken.
+void plan_attention(const tdx_attention_args& a, int d2, bool umma, int sm_count, tdx::AttnParams* p) {
     const int64_t longest = std::max<int64_t>(1, std::min(a.max_len, a.rows));
     const int64_t side = a.seq_offsets ? std::max<int64_t>(1, a.rows / longest) : std::max<int64_t>(1, a.batch);
-    p->slices = static_cast<int>(ceil_div(d2, tdx::kAttnV));
-    const int64_t tiles = std::max<int64_t>(1, static_cast<int64_t>(p->slices) * a.heads);
-    p->seg = ceil_div(longest, tdx::kAttnC) * tdx::kAttnC;
-    const int64_t want = 2 * sm_count / tiles;                   // segments of all sequences together
-    if (want > side) {
-        const int64_t seg = std::max<int64_t>(256, ceil_div(ceil_div(a.seq_offsets ? a.rows : longest * side, want), tdx::kAttnC) * tdx::kAttnC);
-        if (seg < p->seg) p->seg = seg;
+    const int64_t chunk = umma ? tdx::kAttnRows : tdx::kAttnC, slots = umma ? sm_count : 2 * sm_count;
+    p->slices = umma ? 1 : static_cast<int>(ceil_div(d2, tdx::kAttnV));
+    const int64_t tiles = std::max<int64_t>(1, static_cast<int64_t>(p->slices) * a.heads) * side;
+    double least = 0.0;
+    p->seg = ceil_div(longest, chunk) * chunk;
+    for (int64_t n = 1; n <= 64; ++n) {
+        const int64_t seg = std::max<int64_t>(256, ceil_div(ceil_div(longest, n), chunk) * chunk), cuts = ceil_div(longest, seg);
+        if (n > 1 && cuts < n) continue;
+        const double chunks = static_cast<double>(std::min(seg, longest)) / chunk;
+        double cost = ceil_div(tiles * cuts, slots) * (chunks + 2.0);
+        if (cuts > 1) cost += ceil_div(tiles * (cuts - 1), slots) * (0.5 * chunks + 2.0);
+        if (n == 1 || cost < least) {
+            least = cost;
+            p->seg = seg;
+        }
     }
     p->dense = std::max<int64_t>(1, ceil_div(a.max_len, p->seg));
 }
@@ -81,9 +91,11 @@ AttnWorkspace attention_workspace(const tdx_attention_args& a, const AttnShape& 
     tdx::AttnParams p;
     for (int sum = 0; sum < (back ? 4 : 1); ++sum) {
         const int d1 = sum == kAttnOut || sum == kAttnDv ? a.dim_k : a.dim_v, d2 = sum == kAttnOut || sum == kAttnDv ? a.dim_v : a.dim_k;
-        plan_attention(a, d2, sm_count, &p);
-        if (attention_cut(a, p))
-            w.carry = std::max(w.carry, static_cast<size_t>(attention_numbers(a, p)) * a.heads * p.slices * attention_padded(d1) * tdx::kAttnV * sizeof(float));
+        for (int umma = 0; umma < 2; ++umma) {                   // whichever the alignment allows
+            plan_attention(a, d2, umma != 0, sm_count, &p);
+            const size_t each = umma ? tdx::kAttnRows * tdx::kAttnRows : p.slices * attention_padded(d1) * tdx::kAttnV;
+            if (attention_cut(a, p)) w.carry = std::max(w.carry, static_cast<size_t>(attention_numbers(a, p)) * a.heads * each * sizeof(float));
+        }
     }
     w.carry = round_256(w.carry);
     if (back && (shape.q_heads < a.heads || shape.k_heads < a.heads || shape.v_heads < a.heads))
@@ -108,6 +120,19 @@ template <typename T, int KD>
 int launch_attention_pieces(const tdx::AttnParams& p, int64_t numbers, bool cut, cudaStream_t st) {
     if (sizeof(T) == 4 || p.state_out != nullptr) return launch_attention_passes<T, KD, 3>(p, numbers, cut, st);
     return launch_attention_passes<T, KD, sizeof(T) == 4 ? 3 : 2>(p, numbers, cut, st);
+}
+
+template <bool STATE, int UP>
+int launch_attention_umma(const CUtensorMap (&maps)[3], const tdx::AttnParams& p, int64_t numbers, cudaStream_t st) {
+    static std::atomic<bool> known[64];
+    constexpr size_t kBytes = tdx::AttnUmma<STATE, UP>::kBytes + 1024;
+    TDX_TRY(allow_smem(tdx::attn_umma_kernel<STATE, UP>, known, kBytes, static_cast<int>(kBytes)));
+    return launch_seq(tdx::attn_umma_kernel<STATE, UP>, numbers * p.heads, 1, tdx::kAttnUmmaThreads, kBytes, st, maps[0], maps[1], maps[2], p);
+}
+template <int UP>
+int launch_attention_umma_passes(const CUtensorMap (&maps)[3], const tdx::AttnParams& p, int64_t numbers, bool cut, cudaStream_t st) {
+    if (cut) TDX_TRY((launch_attention_umma<true, UP>(maps, p, numbers, st)));
+    return launch_attention_umma<false, UP>(maps, p, numbers, st);
 }
 
 template <typename T>
@@ -151,10 +176,23 @@ int run_attention(const tdx_attention_args& a, const AttnShape& shape, AttnSum s
     p.s2 = turned ? a.dim_v : 1;
     p.status = dev.status;
     p.carry = static_cast<float*>(a.workspace);
-    plan_attention(a, p.d2, dev.sm_count, &p);
+    const bool umma = sizeof(T) == 2 && p.vec && a.rows > 0;
+    plan_attention(a, p.d2, umma, dev.sm_count, &p);
     const int64_t numbers = attention_numbers(a, p);
     const bool cut = attention_cut(a, p);
-    TDX_TRY(attention_padded(p.d1) == 64 ? (launch_attention_pieces<T, 64>(p, numbers, cut, st)) : (launch_attention_pieces<T, 128>(p, numbers, cut, st)));
+    if (umma) {
+        CUtensorMap maps[3];
+        const Role roles[3] = {first, second, third};
+        for (int i = 0; i < 3; ++i) {
+            const uint64_t dims[3] = {static_cast<uint64_t>(roles[i].dim), static_cast<uint64_t>(roles[i].heads), static_cast<uint64_t>(a.rows)};
+            const uint64_t strides[2] = {static_cast<uint64_t>(roles[i].dim) * 2, static_cast<uint64_t>(roles[i].ld) * 2};
+            const uint32_t box[3] = {64, 1, tdx::kAttnRows};
+            TDX_TRY(tdx_host::bf16_map(roles[i].at, 3, dims, strides, box, &maps[i]));
+        }
+        TDX_TRY(p.state_out ? launch_attention_umma_passes<3>(maps, p, numbers, cut, st) : launch_attention_umma_passes<2>(maps, p, numbers, cut, st));
+    } else {
+        TDX_TRY(attention_padded(p.d1) == 64 ? (launch_attention_pieces<T, 64>(p, numbers, cut, st)) : (launch_attention_pieces<T, 128>(p, numbers, cut, st)));
+    }
     if (!shared || a.rows == 0) return TDX_OK;
     const int64_t blocks = std::min<int64_t>(ceil_div(a.rows * out.heads * p.d2, 256), 16 * dev.sm_count);
     return launch_seq(tdx::attn_share_kernel<T>, blocks, 1, 256, 0, st, p.batch, p.max_len, p.rows, p.offsets, out.heads, a.heads / out.heads, p.d2,

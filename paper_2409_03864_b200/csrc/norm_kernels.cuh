@@ -55,8 +55,9 @@ struct NormRow {
         turn ^= 1;
         if (lane == 0) s[warp] = v;
         sync();
-        float t = 0.0f;
-        for (int w = 0; w < warps; ++w) t += s[w];
+        float t = (lane & 15) < warps ? s[lane & 15] : 0.0f;
+#pragma unroll
+        for (int m = 8; m > 0; m >>= 1) t += __shfl_xor_sync(0xffffffffu, t, m);
         return t;
     }
     // two sums over the row behind one barrier
@@ -71,11 +72,13 @@ struct NormRow {
         turn ^= 1;
         if (lane == 0) *reinterpret_cast<float2*>(s + 2 * warp) = make_float2(v, w);
         sync();
-        v = w = 0.0f;
-        for (int i = 0; i < warps; ++i) {
-            const float2 t = *reinterpret_cast<const float2*>(s + 2 * i);
-            v += t.x;
-            w += t.y;
+        const float2 t = (lane & 15) < warps ? *reinterpret_cast<const float2*>(s + 2 * (lane & 15)) : make_float2(0.0f, 0.0f);
+        v = t.x;
+        w = t.y;
+#pragma unroll
+        for (int m = 8; m > 0; m >>= 1) {
+            v += __shfl_xor_sync(0xffffffffu, v, m);
+            w += __shfl_xor_sync(0xffffffffu, w, m);
         }
     }
     // v[i]: this thread's part of vector thread + i * threads; becomes the sum over the vector's group
