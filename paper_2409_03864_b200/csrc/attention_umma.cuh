@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     __shared__ __align__(8) uint64_t full_q, free_q, full_kv[2], free_kv[2], bar_w, bar_p, bar_k, bar_o, bar_u, bar_state, bar_o_free;
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
-    __shared__ float power[kAttnRows + 1];
+    __shared__ float power[kAttnRows + 1], weight[2 * kAttnRows];  // l^n; weight[128 + n] = scale_in l^n, 0 for negative n
     volatile int* abort_flag = &s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint8_t* const smem = attn_raw + ((1024u - (ptx::smem_u32(attn_raw) & 1023u)) & 1023u);
@@ -93,6 +93,10 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     const int less = p.back && piece.index == 0 ? 1 : 0;         // see attn_kernel
     const double log_l = static_cast<double>(__ldg(p.log_decay + head));
     if (tid <= kAttnRows) power[tid] = tid == 0 ? 1.0f : static_cast<float>(exp(log_l * tid));
+    if (tid < kAttnRows) {
+        weight[tid] = 0.0f;
+        weight[kAttnRows + tid] = (tid == 0 ? 1.0f : static_cast<float>(exp(log_l * tid))) * p.scale_in;
+    }
     // rows of K~ that stand for columns of k behind d1 are never written again
     if (p.d1 <= 64) {
         for (int s = 0; s < Lay::kSets; ++s)
@@ -196,12 +200,22 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                         ptx::tmem_ld_32x32b_x32(tmem + lanes + kAttnTmemW + g * 32, w);
                         ptx::tmem_ld_wait();
                         float f[32];
-                        const int apart = p.back ? g * 32 - i : i - g * 32;   // of column 0
+                        if (p.back) {
+                            const float* at = weight + kAttnRows + g * 32 - i;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const int d = p.back ? apart + j : apart - j;
-                            const bool there = d >= 0 && (!p.back || g * 32 + j < n);
-                            f[j] = there ? __uint_as_float(w[j]) * (power[max(d, 0)] * p.scale_in) : 0.0f;
+                            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(w[j]) * at[j];
+                            if (g == quarter || n < kAttnRows) {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) f[j] = g * 32 + j >= i && g * 32 + j < n ? f[j] : 0.0f;
+                            }
+                        } else {
+                            const float* at = weight + kAttnRows + i - g * 32;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(w[j]) * at[-j];
+                            if (g == quarter) {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) f[j] = g * 32 + j <= i ? f[j] : 0.0f;
+                            }
                         }
 #pragma unroll
                         for (int j = 0; j < 16; ++j) packed[j] = attn_pair(f[2 * j], f[2 * j + 1]);
@@ -289,7 +303,7 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
             uint8_t* const k = smem + Lay::kKv + set * 2 * kAttnTile;
             for (int at = worker; at < halves1 * (kAttnHalf / 16); at += 256) {
                 const int row = at / 8 % kAttnRows;
-                const float w = row < n ? power[p.back ? row : n - 1 - row] * p.scale_in : 0.0f;
+                const float w = weight[kAttnRows + (p.back ? row : n - 1 - row)];
                 const uint4 v = *reinterpret_cast<const uint4*>(k + at * 16);
                 const uint32_t in[4] = {v.x, v.y, v.z, v.w};
                 uint32_t out[UP][4];
