@@ -20,6 +20,7 @@ struct AttnParams {
     void* out;
     long long ld_out;
     int out_f32;                            // out is fp32 for every head (its heads are summed afterwards)
+    int wide;                               // rows of out are 32-byte aligned
     int vec;                                // rows of q, k, v (and out) are 16-byte aligned, dims multiples of 16 bytes
     float scale_in, scale_out;              // on k^T v and on out
     int back;                               // from the last row to the first
@@ -32,6 +33,8 @@ struct AttnParams {
     int s1, s2;                             // strides of a state's d1 and d2
     long long seg, dense;                   // rows of a segment; segments of a dense sequence
     float* carry;                           // [number][head][slice][KD][kAttnV]: what a segment adds to the state
+    long long sub, sub_dense;               // attn_umma_kernel: rows of a piece of a segment, and pieces of a dense sequence
+    int carry_turned;                       // attn_umma_kernel: carry was written by a sum with d1 and d2 exchanged
     int slices;                             // of kAttnV columns of v
     int* status;
 };

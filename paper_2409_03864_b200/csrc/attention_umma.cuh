@@ -1,13 +1,16 @@
 // The sums of attention_kernels.cuh on tcgen05, for bf16 rows that the copy engine can read: chunks of 128 rows, one block a segment
 // and head, the state in registers.
 //
-//   warp 0        copies: k and v of a chunk into one of two sets of tiles while the other is worked on, q as soon as the last one is used
-//   warp 1        products: W = q k^T;  O1 = q S0;  O2 = P v;  U = K~^T v
-//   warps 2 - 5   P = W l^(i-j) below the diagonal, bf16, back into tensor memory, from where it is a product's operand;
-//                 out = l^(i+1) O1 + O2
-//   warps 6 - 13  K~ = l^(n-1-j) k in bf16 pieces (the first in place of k); S1 = l^n S0 + U in fp32 registers, 64 a thread; S1 as bf16 for
-//                 the next chunk's O1
+//   warp 0         copies: k and v of a chunk into one of two sets of tiles while the other is worked on, q as soon as the last one is used
+//   warp 1         products: W = q k^T;  O1 = q S0;  O2 = P v;  U = K~^T v
+//   warps 4 - 11   P = W l^(i-j) below the diagonal, bf16, back into tensor memory, from where it is a product's operand; then
+//                  out = l^(i+1) O1 + O2
+//   warps 12 - 15  K~ = l^(n-1-j) k in bf16 pieces, the first in place of k
+//   warps 16 - 23  S1 = l^n S0 + U in fp32 registers, 64 a thread; S1 as bf16 for the next chunk's O1
 //
+// The roles are apart so that a chunk's K~ and W are made while the state and the output of the one in front of it are still worked on:
+// with P and out in four warps and K~ and the state in the same eight a chunk of 128 x 128 took 7,700 cycles.  Registers move from
+// the first four warps and the keys' to the state's.
 // A chunk of 128 x 128 takes about 5,500 cycles of an SM's share of the memory bandwidth and about 2,600 cycles of products, so one
 // chunk at a time with its operands fetched ahead is enough.  U starts from zero in every chunk: the tensor cores cut sums off instead of
 // rounding them, which over a whole sequence shows in the state (3e-6), over 128 rows it does not.
@@ -22,7 +25,7 @@ namespace tdx {
 constexpr int kAttnRows = 128;                                   // rows of a chunk here
 constexpr int kAttnTile = 128 * 256;                             // bytes of 128 rows of 128 bf16, as two halves of 64 columns
 constexpr int kAttnHalf = kAttnTile / 2;
-constexpr int kAttnUmmaThreads = 14 * 32;
+constexpr int kAttnUmmaThreads = 24 * 32;
 enum : uint32_t { kAttnTmemW = 0, kAttnTmemO1 = 128, kAttnTmemO2 = 256, kAttnTmemU = 384 };
 
 // D[tmem] (+)= A[tmem] * B[smem desc]: A's rows are lanes, its columns bf16 pairs
@@ -42,6 +45,28 @@ __device__ __forceinline__ void attn_tmem_st_x16(uint32_t at, const uint32_t (&r
         "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+// 32 bytes in one access (a thread has a row of its own: half as many lines per byte to look up as with 16)
+__device__ __forceinline__ void attn_store_32(void* to, const uint32_t* r) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+__device__ __forceinline__ void attn_prefetch_3d(const CUtensorMap* map, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+// Registers of a warpgroup; 768 threads are launched with 80 each, and 128 * (40 + 2 * 88 + 56 + 2 * 104) of them are asked for,
+// which is as many.
+template <int N>
+__device__ __forceinline__ void attn_fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void attn_more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+__device__ __forceinline__ void attn_tmem_ld_x16(uint32_t at, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+          "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(at)
+        : "memory");
+}
 __device__ __forceinline__ void attn_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 template <bool STATE, int UP>
@@ -51,13 +76,13 @@ struct AttnUmma {
     static constexpr int kBytes = kLow + (UP - 1) * kAttnTile;
 };
 
-template <bool STATE, int UP>
+template <bool STATE, bool BACK, int UP>
 __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     attn_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                      const __grid_constant__ AttnParams p) {
     typedef AttnUmma<STATE, UP> Lay;
     extern __shared__ uint8_t attn_raw[];
-    __shared__ __align__(8) uint64_t full_q, free_q, full_kv[2], free_kv[2], bar_w, bar_p, bar_k, bar_o, bar_u, bar_state, bar_o_free;
+    __shared__ __align__(8) uint64_t full_q, free_q, full_kv[2], free_kv[2], bar_w, bar_p, bar_k, bar_o, bar_u, bar_state, bar_o_free, bar_pair[4];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     __shared__ float power[kAttnRows + 1], weight[2 * kAttnRows];  // l^n; weight[128 + n] = scale_in l^n, 0 for negative n
@@ -68,29 +93,33 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     if (tid == 0) {
         ptx::mbar_init(&full_q, 1); ptx::mbar_init(&free_q, 1);
         for (int i = 0; i < 2; ++i) { ptx::mbar_init(&full_kv[i], 1); ptx::mbar_init(&free_kv[i], 1); }
-        ptx::mbar_init(&bar_w, 1); ptx::mbar_init(&bar_p, 4); ptx::mbar_init(&bar_k, 8); ptx::mbar_init(&bar_o, 1); ptx::mbar_init(&bar_u, 1);
-        ptx::mbar_init(&bar_state, 8); ptx::mbar_init(&bar_o_free, 4);
+        ptx::mbar_init(&bar_w, 1); ptx::mbar_init(&bar_p, 8); ptx::mbar_init(&bar_k, 4); ptx::mbar_init(&bar_o, 1); ptx::mbar_init(&bar_u, 1);
+        ptx::mbar_init(&bar_state, 8); ptx::mbar_init(&bar_o_free, 8);
+        for (int i = 0; i < 4; ++i) ptx::mbar_init(&bar_pair[i], 2);
         s_abort = 0;
         ptx::fence_barrier_init();
         if (!STATE) ptx::tma_prefetch_desc(&tm_q);
         ptx::tma_prefetch_desc(&tm_k);
         ptx::tma_prefetch_desc(&tm_v);
     }
+    seq_launch_dependents();
     seq_grid_wait();
     const int head = static_cast<int>(blockIdx.x % p.heads);
     const long long number = blockIdx.x / p.heads;
     if (!STATE && head == 0) seq_check(p.offsets, number, p.batch, p.max_len, p.rows, p.status);
-    const SeqPiece piece = seq_piece(p.offsets, p.batch, p.dense, p.seg, number);
+    // segments, or for the pass over the states the shorter pieces that it cuts them into
+    const long long seg = STATE ? p.sub : p.seg;
+    const SeqPiece piece = seq_piece(p.offsets, p.batch, STATE ? p.sub_dense : p.dense, seg, number);
     const SeqRange r = seq_range(p.offsets, piece.b, p.max_len, p.rows, p.status);
-    const long long start = piece.index * p.seg;
+    const long long start = piece.index * seg;
     const long long slot = !STATE && (p.state_in != nullptr || p.state_out != nullptr) ? state_slot(p.slots, piece.b, p.n_slots, p.status) : -1;
     const long long state_at = slot * p.state_stride + static_cast<long long>(head) * p.d1 * p.d2;
-    const bool ends = start + p.seg >= r.len;
+    const bool ends = start + seg >= r.len;
     if (start >= r.len && !(piece.index == 0 && !STATE)) return;
-    if (STATE && ends) return;
-    const int count = static_cast<int>(ends ? r.len - start : p.seg);
+    if (STATE && start / p.seg == (r.len - 1) / p.seg) return;   // in the last segment: nobody asks for it
+    const int count = static_cast<int>(ends ? r.len - start : seg);
     const int chunks = (count + kAttnRows - 1) / kAttnRows;
-    const int less = p.back && piece.index == 0 ? 1 : 0;         // see attn_kernel
+    const int less = BACK && piece.index == 0 ? 1 : 0;         // see attn_kernel
     const double log_l = static_cast<double>(__ldg(p.log_decay + head));
     if (tid <= kAttnRows) power[tid] = tid == 0 ? 1.0f : static_cast<float>(exp(log_l * tid));
     if (tid < kAttnRows) {
@@ -115,145 +144,179 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     ptx::tc_fence_after_sync();
     const uint32_t tmem = s_tmem;
     // chunk c has the rows first .. first + n - 1 in their own order, whatever the direction is
-    const long long row0 = r.first + (p.back ? r.len - start : start);
+    const long long row0 = r.first + (BACK ? r.len - start : start);
     auto rows_of = [&](int c) { return min(kAttnRows, count - c * kAttnRows); };
-    auto first_of = [&](int c) { return p.back ? row0 - static_cast<long long>(c) * kAttnRows - rows_of(c) : row0 + static_cast<long long>(c) * kAttnRows; };
+    auto first_of = [&](int c) { return BACK ? row0 - static_cast<long long>(c) * kAttnRows - rows_of(c) : row0 + static_cast<long long>(c) * kAttnRows; };
     const int steps1 = (p.d1 + 15) / 16, halves1 = (p.d1 + 63) / 64, halves2 = (p.d2 + 63) / 64, n2 = (p.d2 + 15) / 16 * 16;
 
-    if (warp == 0) {
-        if (ptx::elect_one()) {
-            const int hq = head / p.q_share, hk = head / p.k_share, hv = head / p.v_share;
-            bool ok = true;
-            for (int c = 0; ok && c < chunks; ++c) {
-                const int row = static_cast<int>(first_of(c)), set = c % Lay::kSets, use = c / Lay::kSets;
-                if (!STATE) {
-                    if (c > 0 && !wait_bounded(&free_q, (c - 1) & 1, abort_flag, p.status, kTimeoutProducer)) { ok = false; break; }
-                    ptx::mbar_arrive_expect_tx(&full_q, halves1 * kAttnHalf);
-                    for (int h = 0; h < halves1; ++h) ptx::tma_load_3d(smem + Lay::kQ + h * kAttnHalf, &tm_q, &full_q, h * 64, hq, row);
+    if (warp < 4) {
+        attn_fewer_registers<40>();
+        if (warp == 0) {
+            if (ptx::elect_one()) {
+                const int hq = head / p.q_share, hk = head / p.k_share, hv = head / p.v_share;
+                bool ok = true;
+                for (int c = 0; ok && c < chunks; ++c) {
+                    const int row = static_cast<int>(first_of(c)), set = c % Lay::kSets, use = c / Lay::kSets;
+                    if (use > 0 && !wait_bounded_idle(&free_kv[set], (use - 1) & 1, abort_flag, p.status, kTimeoutProducer)) { ok = false; break; }
+                    uint8_t* kv = smem + Lay::kKv + set * 2 * kAttnTile;
+                    ptx::mbar_arrive_expect_tx(&full_kv[set], (halves1 + halves2) * kAttnHalf);
+                    for (int h = 0; h < halves1; ++h) ptx::tma_load_3d(kv + h * kAttnHalf, &tm_k, &full_kv[set], h * 64, hk, row);
+                    for (int h = 0; h < halves2; ++h) ptx::tma_load_3d(kv + kAttnTile + h * kAttnHalf, &tm_v, &full_kv[set], h * 64, hv, row);
+                    if (!STATE) {
+                        // q has one tile only: it is brought as far as L2 until the one before has been used
+                        if (c > 0)
+                            for (int h = 0; h < halves1; ++h) attn_prefetch_3d(&tm_q, h * 64, hq, row);
+                        if (c > 0 && !wait_bounded_idle(&free_q, (c - 1) & 1, abort_flag, p.status, kTimeoutProducer)) { ok = false; break; }
+                        ptx::mbar_arrive_expect_tx(&full_q, halves1 * kAttnHalf);
+                        for (int h = 0; h < halves1; ++h) ptx::tma_load_3d(smem + Lay::kQ + h * kAttnHalf, &tm_q, &full_q, h * 64, hq, row);
+                    }
                 }
-                if (use > 0 && !wait_bounded(&free_kv[set], (use - 1) & 1, abort_flag, p.status, kTimeoutProducer)) { ok = false; break; }
-                uint8_t* kv = smem + Lay::kKv + set * 2 * kAttnTile;
-                ptx::mbar_arrive_expect_tx(&full_kv[set], (halves1 + halves2) * kAttnHalf);
-                for (int h = 0; h < halves1; ++h) ptx::tma_load_3d(kv + h * kAttnHalf, &tm_k, &full_kv[set], h * 64, hk, row);
-                for (int h = 0; h < halves2; ++h) ptx::tma_load_3d(kv + kAttnTile + h * kAttnHalf, &tm_v, &full_kv[set], h * 64, hv, row);
+                if (!ok) {
+                    // let copies that are still in flight land before the block goes away
+                    for (int i = 0; i < 64; ++i) __nanosleep(2000);
+                }
             }
-            if (!ok) {
-                // let copies that are still in flight land before the block goes away
-                for (int i = 0; i < 64; ++i) __nanosleep(2000);
+        } else if (warp == 1) {
+            if (ptx::elect_one()) {
+                const uint32_t base = ptx::smem_u32(smem);
+                // K-major operands: 16 of the reduction are 32 bytes further in a 128-byte row, 64 are a half tile; others: 16 rows of 128 bytes
+                auto k_major = [&](uint32_t at, int step) { return ptx::make_smem_desc_sw128(at + (step >> 2) * kAttnHalf + (step & 3) * 32, 16u, 1024u); };
+                auto mn_major = [&](uint32_t at, int step) { return ptx::make_smem_desc_sw128(at + step * 2048, kAttnHalf, 1024u); };
+                const uint32_t idesc_w = ptx::make_idesc_bf16_f32(128, 128, 0, 0), idesc_o = ptx::make_idesc_bf16_f32(128, n2, 0, 1),
+                               idesc_u = ptx::make_idesc_bf16_f32(128, n2, 1, 1);
+                bool ok = true;
+                auto wait = [&](uint64_t* bar, int use) { return ok = ok && wait_bounded_idle(bar, use & 1, abort_flag, p.status, kTimeoutMma); };
+                for (int c = 0; ok && c < chunks; ++c) {
+                    const int set = c % Lay::kSets;
+                    const uint32_t k = base + Lay::kKv + set * 2 * kAttnTile, v = k + kAttnTile;
+                    if (!wait(&full_kv[set], c / Lay::kSets)) break;
+                    if (!STATE) {
+                        // (W takes the place of P, which O2 of the chunk before has to be done with)
+                        if (!wait(&full_q, c) || (c > 0 && !wait(&bar_o, c - 1))) break;
+                        ptx::tc_fence_after_sync();
+                        for (int s = 0; s < steps1; ++s) ptx::umma_bf16(tmem + kAttnTmemW, k_major(base + Lay::kQ, s), k_major(k, s), idesc_w, s > 0);
+                        ptx::umma_commit(&bar_w);
+                    }
+                    // (the state in front of the chunk: U has been read)
+                    if (!wait(&bar_state, c)) break;
+                    if (!STATE) {
+                        if (c > 0 && !wait(&bar_o_free, c - 1)) break;
+                        ptx::tc_fence_after_sync();
+                        for (int s = 0; s < steps1; ++s) ptx::umma_bf16(tmem + kAttnTmemO1, k_major(base + Lay::kQ, s), mn_major(base + Lay::kState, s), idesc_o, s > 0);
+                        ptx::umma_commit(&free_q);
+                    }
+                    if (!STATE) {
+                        // (the keys' warps set the rows of v behind a short chunk to zero)
+                        if (!wait(&bar_p, c) || (rows_of(c) < kAttnRows && !wait(&bar_k, c))) break;
+                        ptx::tc_fence_after_sync();
+                        for (int s = 0; s < 8; ++s) attn_umma_ta(tmem + kAttnTmemO2, tmem + kAttnTmemW + s * 8, mn_major(v, s), idesc_o, s > 0);
+                        ptx::umma_commit(&bar_o);
+                    }
+                    if (!wait(&bar_k, c)) break;
+                    ptx::tc_fence_after_sync();
+                    for (int u = UP - 1; u >= 0; --u) {              // small terms first
+                        const uint32_t from = u == 0 ? k : base + Lay::kLow + (u - 1) * kAttnTile;
+                        for (int s = 0; s < 8; ++s) ptx::umma_bf16(tmem + kAttnTmemU, mn_major(from, s), mn_major(v, s), idesc_u, u < UP - 1 || s > 0);
+                    }
+                    ptx::umma_commit(&free_kv[set]);
+                    ptx::umma_commit(&bar_u);
+                }
             }
         }
-    } else if (warp == 1) {
-        if (ptx::elect_one()) {
-            const uint32_t base = ptx::smem_u32(smem);
-            // K-major operands: 16 of the reduction are 32 bytes further in a 128-byte row, 64 are a half tile; others: 16 rows of 128 bytes
-            auto k_major = [&](uint32_t at, int step) { return ptx::make_smem_desc_sw128(at + (step >> 2) * kAttnHalf + (step & 3) * 32, 16u, 1024u); };
-            auto mn_major = [&](uint32_t at, int step) { return ptx::make_smem_desc_sw128(at + step * 2048, kAttnHalf, 1024u); };
-            const uint32_t idesc_w = ptx::make_idesc_bf16_f32(128, 128, 0, 0), idesc_o = ptx::make_idesc_bf16_f32(128, n2, 0, 1),
-                           idesc_u = ptx::make_idesc_bf16_f32(128, n2, 1, 1);
-            bool ok = true;
-            auto wait = [&](uint64_t* bar, int use) { return ok = ok && wait_bounded(bar, use & 1, abort_flag, p.status, kTimeoutMma); };
-            for (int c = 0; ok && c < chunks; ++c) {
-                const int set = c % Lay::kSets;
-                const uint32_t k = base + Lay::kKv + set * 2 * kAttnTile, v = k + kAttnTile;
-                if (!wait(&full_kv[set], c / Lay::kSets)) break;
-                if (!STATE) {
-                    // (W takes the place of P, which O2 of the chunk before has to be done with)
-                    if (!wait(&full_q, c) || (c > 0 && !wait(&bar_o, c - 1))) break;
-                    ptx::tc_fence_after_sync();
-                    for (int s = 0; s < steps1; ++s) ptx::umma_bf16(tmem + kAttnTmemW, k_major(base + Lay::kQ, s), k_major(k, s), idesc_w, s > 0);
-                    ptx::umma_commit(&bar_w);
-                    if (!wait(&bar_state, c) || (c > 0 && !wait(&bar_o_free, c - 1))) break;
-                    ptx::tc_fence_after_sync();
-                    for (int s = 0; s < steps1; ++s) ptx::umma_bf16(tmem + kAttnTmemO1, k_major(base + Lay::kQ, s), mn_major(base + Lay::kState, s), idesc_o, s > 0);
-                    ptx::umma_commit(&free_q);
-                }
-                if (!wait(&bar_k, c) || (!STATE && !wait(&bar_p, c))) break;
-                ptx::tc_fence_after_sync();
-                if (!STATE) {
-                    for (int s = 0; s < 8; ++s) attn_umma_ta(tmem + kAttnTmemO2, tmem + kAttnTmemW + s * 8, mn_major(v, s), idesc_o, s > 0);
-                    ptx::umma_commit(&bar_o);
-                }
-                for (int u = UP - 1; u >= 0; --u) {              // small terms first
-                    const uint32_t from = u == 0 ? k : base + Lay::kLow + (u - 1) * kAttnTile;
-                    for (int s = 0; s < 8; ++s) ptx::umma_bf16(tmem + kAttnTmemU, mn_major(from, s), mn_major(v, s), idesc_u, u < UP - 1 || s > 0);
-                }
-                ptx::umma_commit(&free_kv[set]);
-                ptx::umma_commit(&bar_u);
-            }
-        }
-    } else if (warp < 6) {
+    } else if (warp < 12) {
+        attn_more_registers<88>();
         if (!STATE) {
-            const int quarter = warp & 3, i = quarter * 32 + lane;
-            const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+            // two warps a quarter of the rows, every second group of 32 columns each
+            const int quarter = warp & 3, part = (warp - 4) >> 2, i = quarter * 32 + lane;
+            const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+            const int from = BACK ? quarter : 0, to = BACK ? 3 : quarter;   // groups on this side of the diagonal
             for (int c = 0; c < chunks; ++c) {
                 const int n = rows_of(c), shift = c == 0 ? less : 0;
-                if (!wait_bounded(&bar_w, c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+                if (!wait_bounded_idle(&bar_w, c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
                 ptx::tc_fence_after_sync();
-#pragma unroll 1
-                for (int g = 0; g < 4; ++g) {
-                    uint32_t packed[16];
-                    if (p.back ? g < quarter : g > quarter) {
+                uint32_t packed[2][16];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) packed[j] = 0u;
+                for (int h = 0; h < 2; ++h) {
+                    const int g = part + 2 * h;
+                    if (g < from || g > to) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) packed[h][j] = 0u;
                     } else {
                         uint32_t w[32];
-                        ptx::tmem_ld_32x32b_x32(tmem + lanes + kAttnTmemW + g * 32, w);
-                        ptx::tmem_ld_wait();
                         float f[32];
-                        if (p.back) {
-                            const float* at = weight + kAttnRows + g * 32 - i;
+                        ptx::tmem_ld_32x32b_x32(lanes + kAttnTmemW + g * 32, w);
+                        ptx::tmem_ld_wait();
+                        if (BACK) {
+                            const float* l = weight + kAttnRows + g * 32 - i;
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(w[j]) * at[j];
+                            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(w[j]) * l[j];
                             if (g == quarter || n < kAttnRows) {
 #pragma unroll
                                 for (int j = 0; j < 32; ++j) f[j] = g * 32 + j >= i && g * 32 + j < n ? f[j] : 0.0f;
                             }
                         } else {
-                            const float* at = weight + kAttnRows + i - g * 32;
+                            const float* l = weight + kAttnRows + i - g * 32;
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(w[j]) * at[-j];
+                            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(w[j]) * l[-j];
                             if (g == quarter) {
 #pragma unroll
                                 for (int j = 0; j < 32; ++j) f[j] = g * 32 + j <= i ? f[j] : 0.0f;
                             }
                         }
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) packed[j] = attn_pair(f[2 * j], f[2 * j + 1]);
+                        for (int j = 0; j < 16; ++j) packed[h][j] = attn_pair(f[2 * j], f[2 * j + 1]);
                     }
-                    // columns 16 g and up: nothing of W that is still to be read
-                    attn_tmem_st_x16(tmem + lanes + kAttnTmemW + g * 16, packed);
                 }
+                // P takes the place of W's first half, once both warps have read theirs
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&bar_pair[quarter]);
+                if (!wait_bounded_idle(&bar_pair[quarter], c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+                ptx::tc_fence_after_sync();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) attn_tmem_st_x16(lanes + kAttnTmemW + (part + 2 * h) * 16, packed[h]);
                 attn_tmem_st_wait();
                 ptx::tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&bar_p);
-                if (!wait_bounded(&bar_o, c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+
+                if (!wait_bounded_idle(&bar_o, c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
                 ptx::tc_fence_after_sync();
-                const float far = (i < n ? power[p.back ? n - i - shift : i + 1 - shift] : 0.0f) * p.scale_out;
-                const long long to = (first_of(c) + i) * p.ld_out + static_cast<long long>(head) * p.d2;
+                const float far = (i < n ? power[BACK ? n - i - shift : i + 1 - shift] : 0.0f) * p.scale_out;
+                const long long to_row = (first_of(c) + i) * p.ld_out + static_cast<long long>(head) * p.d2;
 #pragma unroll 1
-                for (int g = 0; g * 32 < p.d2; ++g) {
-                    uint32_t o1[32], o2[32];
-                    ptx::tmem_ld_32x32b_x32(tmem + lanes + kAttnTmemO1 + g * 32, o1);
-                    ptx::tmem_ld_32x32b_x32(tmem + lanes + kAttnTmemO2 + g * 32, o2);
-                    ptx::tmem_ld_wait();
-                    float f[32];
+                for (int g = part * 2; g < part * 2 + 2; ++g) {
+                    // 16 columns at a time of both sums
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) f[j] = fmaf(__uint_as_float(o1[j]), far, __uint_as_float(o2[j]) * p.scale_out);
-                    if (i < n) {
+                    for (int h = 0; h < 2; ++h) {
+                        const int col = g * 32 + h * 16;
+                        if (col >= p.d2) break;
+                        uint32_t o1[16], o2[16], out[8];
+                        attn_tmem_ld_x16(lanes + kAttnTmemO1 + col, o1);
+                        attn_tmem_ld_x16(lanes + kAttnTmemO2 + col, o2);
+                        ptx::tmem_ld_wait();
+                        float f[16];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (g * 32 + j * 8 < p.d2) {
-                                if (p.out_f32) {
-                                    float4* at = reinterpret_cast<float4*>(static_cast<float*>(p.out) + to + g * 32 + j * 8);
-                                    at[0] = make_float4(f[8 * j], f[8 * j + 1], f[8 * j + 2], f[8 * j + 3]);
-                                    at[1] = make_float4(f[8 * j + 4], f[8 * j + 5], f[8 * j + 6], f[8 * j + 7]);
+                        for (int j = 0; j < 16; ++j) f[j] = fmaf(__uint_as_float(o1[j]), far, __uint_as_float(o2[j]) * p.scale_out);
+                        if (i < n) {
+                            if (p.out_f32) {
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    if (col + j * 4 < p.d2)
+                                        *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to_row + col + j * 4) = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) out[j] = attn_pair(f[2 * j], f[2 * j + 1]);
+                                __nv_bfloat16* at = static_cast<__nv_bfloat16*>(p.out) + to_row + col;
+                                if (p.wide) {
+                                    attn_store_32(at, out);
                                 } else {
-                                    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + to + g * 32 + j * 8) =
-                                        make_uint4(attn_pair(f[8 * j], f[8 * j + 1]), attn_pair(f[8 * j + 2], f[8 * j + 3]), attn_pair(f[8 * j + 4], f[8 * j + 5]), attn_pair(f[8 * j + 6], f[8 * j + 7]));
+                                    *reinterpret_cast<uint4*>(at) = make_uint4(out[0], out[1], out[2], out[3]);
+                                    if (col + 8 < p.d2) *reinterpret_cast<uint4*>(at + 8) = make_uint4(out[4], out[5], out[6], out[7]);
                                 }
                             }
                         }
+                        __syncwarp();
                     }
                 }
                 ptx::tc_fence_before_sync();
@@ -261,97 +324,139 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                 if (lane == 0) ptx::mbar_arrive(&bar_o_free);
             }
         }
+    } else if (warp < 16) {
+        attn_fewer_registers<56>();
+        const int worker = tid - 12 * 32;
+        for (int c = 0; c < chunks; ++c) {
+            const int n = rows_of(c), set = c % Lay::kSets;
+            if (!wait_bounded_idle(&full_kv[set], (c / Lay::kSets) & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+            // q k^T has been read from k before it is overwritten, and U of the chunk before from the other pieces
+            if (!STATE && !wait_bounded_idle(&bar_w, c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+            if (c > 0 && !wait_bounded_idle(&bar_u, (c - 1) & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+            uint8_t* const k = smem + Lay::kKv + set * 2 * kAttnTile;
+            // two 16-byte pieces a thread at a time
+#pragma unroll 1
+            for (int first = worker; first < halves1 * (kAttnHalf / 16); first += 256) {
+                uint4 in[2];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) in[q] = *reinterpret_cast<const uint4*>(k + (first + q * 128) * 16);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int at = first + q * 128, row = at / 8 % kAttnRows;
+                    const float w = weight[kAttnRows + (BACK ? row : n - 1 - row)];
+                    if (row >= n) in[q] = make_uint4(0u, 0u, 0u, 0u);
+                    const f32x2 ww = pack2(w, w), minus = pack2(-1.0f, -1.0f);
+                    const uint32_t pair[4] = {in[q].x, in[q].y, in[q].z, in[q].w};
+                    uint32_t out[UP][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        f32x2 left = mul2(pack2(attn_lo(pair[j]), attn_hi(pair[j])), ww);
+#pragma unroll
+                        for (int u = 0; u < UP; ++u) {           // as in attn_split
+                            float lo, hi;
+                            unpack2(left, lo, hi);
+                            out[u][j] = attn_pair(lo, hi);
+                            if (u + 1 < UP) left = fma2(pack2(attn_lo(out[u][j]), attn_hi(out[u][j])), minus, left);
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < UP; ++u)
+                        *reinterpret_cast<uint4*>((u == 0 ? k : smem + Lay::kLow + (u - 1) * kAttnTile) + at * 16) = make_uint4(out[u][0], out[u][1], out[u][2], out[u][3]);
+                }
+            }
+            if (n < kAttnRows) {
+                for (int h = 0; h < halves2; ++h)
+                    for (int at = worker; at < (kAttnRows - n) * 8; at += 128) *reinterpret_cast<uint4*>(k + kAttnTile + h * kAttnHalf + n * 128 + at * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&bar_k);
+        }
     } else {
+        attn_more_registers<104>();
         // this thread's part of the state: row m, columns 64 side and up
-        const int quarter = warp & 3, side = (warp - 6) >> 2, m = quarter * 32 + lane, worker = tid - 6 * 32;
+        const int quarter = warp & 3, side = (warp - 16) >> 2, m = quarter * 32 + lane;
         const bool mine = side < halves2;
         float st[64];
-        const long long carry_size = kAttnRows * kAttnRows, carry_step = carry_size * p.heads;
-        float* const carry = p.carry + (number * p.heads + head) * carry_size + static_cast<long long>(side) * 64 * kAttnRows + m;
 #pragma unroll
-        for (int j = 0; j < 64; ++j) {
-            const int n = side * 64 + j;
-            st[j] = !STATE && p.state_in != nullptr && slot >= 0 && m < p.d1 && n < p.d2 ? __ldg(p.state_in + state_at + static_cast<long long>(m) * p.s1 + static_cast<long long>(n) * p.s2) : 0.0f;
+        for (int j = 0; j < 64; ++j) st[j] = 0.0f;
+        if (!STATE && p.state_in != nullptr && slot >= 0 && m < p.d1) {
+            const float* from = p.state_in + state_at + static_cast<long long>(m) * p.s1 + static_cast<long long>(side) * 64 * p.s2;
+            const int there = p.d2 - side * 64;
+#pragma unroll
+            for (int j = 0; j < 64; ++j) {
+                if (j < there) st[j] = __ldg(from);
+                from += p.s2;
+            }
         }
+        // what a segment's pieces add to the state: [column][row], so that a warp's rows lie side by side, or (a sum with the roles of
+        // the state's dimensions exchanged) [row][column]
+        const long long carry_size = kAttnRows * kAttnRows, carry_step = carry_size * p.heads;
         if (!STATE && piece.index > 0 && mine) {
-            const float all = static_cast<float>(exp(log_l * static_cast<double>(p.seg))), first = p.back ? static_cast<float>(exp(log_l * static_cast<double>(p.seg - 1))) : all;
-            for (int s = 0; s < piece.index; ++s) {
-                const float* from = carry + (s - piece.index) * carry_step;
+            const int pieces = piece.index * static_cast<int>(p.seg / p.sub);
+            const float* from = p.carry + ((p.offsets == nullptr ? piece.b * p.sub_dense : __ldg(p.offsets + piece.b) / p.sub + piece.b) * p.heads + head) * carry_size +
+                                (p.carry_turned ? static_cast<long long>(m) * kAttnRows + side * 64 : static_cast<long long>(side) * 64 * kAttnRows + m);
+            const int apart = p.carry_turned ? 1 : kAttnRows;
+            const float all = static_cast<float>(exp(log_l * static_cast<double>(p.sub))), first = BACK ? static_cast<float>(exp(log_l * static_cast<double>(p.sub - 1))) : all;
+#pragma unroll 1
+            for (int s = 0; s < pieces; ++s, from += carry_step) {
                 const float f = s == 0 ? first : all;
+                const float* at = from;
 #pragma unroll
-                for (int j = 0; j < 64; ++j) st[j] = fmaf(st[j], f, from[j * kAttnRows]);
+                for (int j = 0; j < 64; ++j) {
+                    st[j] = fmaf(st[j], f, *at);
+                    at += apart;
+                }
             }
         }
         // the state in front of a chunk, rounded to bf16 for its product with q
         auto publish = [&]() {
-            if (mine) {
+            if (!STATE && mine) {
 #pragma unroll
                 for (int g = 0; g < 8; ++g)
                     *reinterpret_cast<uint4*>(smem + Lay::kState + side * kAttnHalf + m * 128 + ((g ^ (m & 7)) << 4)) =
                         make_uint4(attn_pair(st[8 * g], st[8 * g + 1]), attn_pair(st[8 * g + 2], st[8 * g + 3]), attn_pair(st[8 * g + 4], st[8 * g + 5]), attn_pair(st[8 * g + 6], st[8 * g + 7]));
             }
-            ptx::fence_proxy_async_smem();
+            if (!STATE) ptx::fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&bar_state);
         };
-        if (!STATE && chunks > 0) publish();
+        if (chunks > 0) publish();
         for (int c = 0; c < chunks; ++c) {
-            const int n = rows_of(c), shift = c == 0 ? less : 0, set = c % Lay::kSets;
-            if (!wait_bounded(&full_kv[set], (c / Lay::kSets) & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
-            // q k^T has been read from k before it is overwritten
-            if (!STATE && !wait_bounded(&bar_w, c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
-            uint8_t* const k = smem + Lay::kKv + set * 2 * kAttnTile;
-            for (int at = worker; at < halves1 * (kAttnHalf / 16); at += 256) {
-                const int row = at / 8 % kAttnRows;
-                const float w = weight[kAttnRows + (p.back ? row : n - 1 - row)];
-                const uint4 v = *reinterpret_cast<const uint4*>(k + at * 16);
-                const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-                uint32_t out[UP][4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t up[UP];
-                    attn_split(attn_lo(in[j]) * w, attn_hi(in[j]) * w, up);
-#pragma unroll
-                    for (int u = 0; u < UP; ++u) out[u][j] = row < n ? up[u] : 0u;
-                }
-#pragma unroll
-                for (int u = 0; u < UP; ++u)
-                    *reinterpret_cast<uint4*>((u == 0 ? k : smem + Lay::kLow + (u - 1) * kAttnTile) + at * 16) = make_uint4(out[u][0], out[u][1], out[u][2], out[u][3]);
-            }
-            if (n < kAttnRows) {
-                for (int h = 0; h < halves2; ++h)
-                    for (int at = worker; at < (kAttnRows - n) * 8; at += 256) *reinterpret_cast<uint4*>(k + kAttnTile + h * kAttnHalf + n * 128 + at * 16) = make_uint4(0u, 0u, 0u, 0u);
-            }
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&bar_k);
-            if (!wait_bounded(&bar_u, c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+            const int n = rows_of(c), shift = c == 0 ? less : 0;
+            if (!wait_bounded_idle(&bar_u, c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
             ptx::tc_fence_after_sync();
             if (mine) {
                 const float f = power[n - shift];
+                const uint32_t at = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + kAttnTmemU + side * 64;
+                uint32_t u[2][16];
+                attn_tmem_ld_x16(at, u[0]);
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    uint32_t u[32];
-                    ptx::tmem_ld_32x32b_x32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + kAttnTmemU + side * 64 + g * 32, u);
+                for (int g = 0; g < 4; ++g) {
                     ptx::tmem_ld_wait();
+                    if (g < 3) attn_tmem_ld_x16(at + (g + 1) * 16, u[(g + 1) & 1]);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) st[g * 32 + j] = fmaf(st[g * 32 + j], f, __uint_as_float(u[j]));
+                    for (int j = 0; j < 16; ++j) st[g * 16 + j] = fmaf(st[g * 16 + j], f, __uint_as_float(u[g & 1][j]));
                 }
             }
             ptx::tc_fence_before_sync();
-            // (without q the next chunk's products wait for bar_k, which comes after this read)
-            if (!STATE && c + 1 < chunks) publish();
+            if (c + 1 < chunks) publish();
         }
         if (STATE) {
             if (mine) {
+                float* to = p.carry + (number * p.heads + head) * carry_size + static_cast<long long>(side) * 64 * kAttnRows + m;
 #pragma unroll
-                for (int j = 0; j < 64; ++j) carry[j * kAttnRows] = st[j];
+                for (int j = 0; j < 64; ++j) to[j * kAttnRows] = st[j];
             }
         } else if (ends && p.state_out != nullptr && slot >= 0 && m < p.d1) {
-            const float f = p.back && r.len > 0 ? static_cast<float>(exp(log_l)) : 1.0f;   // see attn_kernel
+            const float f = BACK && r.len > 0 ? static_cast<float>(exp(log_l)) : 1.0f;   // see attn_kernel
+            float* to = p.state_out + state_at + static_cast<long long>(m) * p.s1 + static_cast<long long>(side) * 64 * p.s2;
+            const int there = p.d2 - side * 64;
 #pragma unroll
-            for (int j = 0; j < 64; ++j)
-                if (side * 64 + j < p.d2) p.state_out[state_at + static_cast<long long>(m) * p.s1 + static_cast<long long>(side * 64 + j) * p.s2] = st[j] * f;
+            for (int j = 0; j < 64; ++j) {
+                if (j < there) *to = st[j] * f;
+                to += p.s2;
+            }
         }
     }
     ptx::tc_fence_before_sync();

@@ -31,4 +31,30 @@ __device__ __forceinline__ bool wait_bounded(uint64_t* bar, uint32_t parity, vol
     return wait_bounded_for(bar, parity, s_abort, g_status, code, kWaitLimitCycles);
 }
 
+// The same for kernels whose waiting warps stand beside working ones: the hardware may hold the thread for up to 20 us at a time, so
+// that it does not take issue slots by polling.
+__device__ __forceinline__ bool wait_bounded_idle(uint64_t* bar, uint32_t parity, volatile int* s_abort, int* g_status, int code) {
+    if (ptx::mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (;;) {
+        uint32_t ok;
+        asm volatile(
+            "{\n"
+            ".reg .pred p;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+            "selp.u32 %0, 1, 0, p;\n"
+            "}\n"
+            : "=r"(ok)
+            : "r"(ptx::smem_u32(bar)), "r"(parity), "r"(20000u)
+            : "memory");
+        if (ok) return true;
+        if (*s_abort) return false;
+        if (clock64() - t0 > kWaitLimitCycles) {
+            *s_abort = 1;
+            atomicCAS(g_status, 0, code);
+            return false;
+        }
+    }
+}
+
 }  // namespace tdx

@@ -78,9 +78,21 @@ void plan_attention(const tdx_attention_args& a, int d2, bool umma, int sm_count
         }
     }
     p->dense = std::max<int64_t>(1, ceil_div(a.max_len, p->seg));
+    // the pass over the states has all segments but the last: pieces of them, as many as fill the SMs
+    p->sub = p->seg;
+    if (umma) {
+        const int64_t busy = tiles * std::max<int64_t>(1, ceil_div(longest, p->seg) - 1), most = p->seg / tdx::kAttnRows;
+        int64_t k = std::min(most, std::max<int64_t>(1, sm_count / busy));
+        while (most % k) --k;
+        p->sub = p->seg / k;
+    }
+    p->sub_dense = std::max<int64_t>(1, ceil_div(a.max_len, p->sub));
 }
 int64_t attention_numbers(const tdx_attention_args& a, const tdx::AttnParams& p) {
     return tdx::seq_pieces(a.seq_offsets != nullptr, a.batch, a.rows, p.dense, p.seg);
+}
+int64_t attention_sub_numbers(const tdx_attention_args& a, const tdx::AttnParams& p) {
+    return tdx::seq_pieces(a.seq_offsets != nullptr, a.batch, a.rows, p.sub_dense, p.sub);
 }
 bool attention_cut(const tdx_attention_args& a, const tdx::AttnParams& p) { return std::min(a.max_len, a.rows) > p.seg; }
 int attention_padded(int d1) { return d1 > 64 ? 128 : 64; }
@@ -94,7 +106,7 @@ AttnWorkspace attention_workspace(const tdx_attention_args& a, const AttnShape& 
         for (int umma = 0; umma < 2; ++umma) {                   // whichever the alignment allows
             plan_attention(a, d2, umma != 0, sm_count, &p);
             const size_t each = umma ? tdx::kAttnRows * tdx::kAttnRows : p.slices * attention_padded(d1) * tdx::kAttnV;
-            if (attention_cut(a, p)) w.carry = std::max(w.carry, static_cast<size_t>(attention_numbers(a, p)) * a.heads * each * sizeof(float));
+            if (attention_cut(a, p)) w.carry = std::max(w.carry, static_cast<size_t>(attention_sub_numbers(a, p)) * a.heads * each * sizeof(float));
         }
     }
     w.carry = round_256(w.carry);
@@ -122,17 +134,22 @@ int launch_attention_pieces(const tdx::AttnParams& p, int64_t numbers, bool cut,
     return launch_attention_passes<T, KD, sizeof(T) == 4 ? 3 : 2>(p, numbers, cut, st);
 }
 
-template <bool STATE, int UP>
+template <bool STATE, bool BACK, int UP>
 int launch_attention_umma(const CUtensorMap (&maps)[3], const tdx::AttnParams& p, int64_t numbers, cudaStream_t st) {
     static std::atomic<bool> known[64];
     constexpr size_t kBytes = tdx::AttnUmma<STATE, UP>::kBytes + 1024;
-    TDX_TRY(allow_smem(tdx::attn_umma_kernel<STATE, UP>, known, kBytes, static_cast<int>(kBytes)));
-    return launch_seq(tdx::attn_umma_kernel<STATE, UP>, numbers * p.heads, 1, tdx::kAttnUmmaThreads, kBytes, st, maps[0], maps[1], maps[2], p);
+    TDX_TRY(allow_smem(tdx::attn_umma_kernel<STATE, BACK, UP>, known, kBytes, static_cast<int>(kBytes)));
+    return launch_seq(tdx::attn_umma_kernel<STATE, BACK, UP>, numbers * p.heads, 1, tdx::kAttnUmmaThreads, kBytes, st, maps[0], maps[1], maps[2], p);
 }
-template <int UP>
-int launch_attention_umma_passes(const CUtensorMap (&maps)[3], const tdx::AttnParams& p, int64_t numbers, bool cut, cudaStream_t st) {
-    if (cut) TDX_TRY((launch_attention_umma<true, UP>(maps, p, numbers, st)));
-    return launch_attention_umma<false, UP>(maps, p, numbers, st);
+// states: the number of pieces of the pass over the states, 0 where there is none to make
+template <bool BACK, int UP>
+int launch_attention_umma_passes(const CUtensorMap (&maps)[3], const tdx::AttnParams& p, int64_t numbers, int64_t states, cudaStream_t st) {
+    if (states > 0) TDX_TRY((launch_attention_umma<true, BACK, UP>(maps, p, states, st)));
+    return launch_attention_umma<false, BACK, UP>(maps, p, numbers, st);
+}
+template <bool BACK>
+int launch_attention_umma_pieces(const CUtensorMap (&maps)[3], const tdx::AttnParams& p, int64_t numbers, int64_t states, cudaStream_t st) {
+    return p.state_out ? launch_attention_umma_passes<BACK, 3>(maps, p, numbers, states, st) : launch_attention_umma_passes<BACK, 2>(maps, p, numbers, states, st);
 }
 
 template <typename T>
@@ -160,10 +177,21 @@ int run_attention(const tdx_attention_args& a, const AttnShape& shape, AttnSum s
         p.ld_out = static_cast<int64_t>(a.heads) * p.d2;
         p.out_f32 = 1;
     }
+    // one answer for all sums of a pass: those of the backward pass share what a segment adds to the state
     Widest widest(16);
-    for (const Role& r : {first, second, third}) { widest.ptr(r.at); widest.stride(r.ld, el); widest.stride(r.dim, el); }
-    if (!shared) { widest.ptr(p.out); widest.stride(p.ld_out, el); }
+    auto rows = [&](const void* at, int64_t ld) { widest.ptr(at); widest.stride(ld, el); };
+    widest.stride(a.dim_k, el);
+    widest.stride(a.dim_v, el);
+    rows(a.q, a.ld_q); rows(a.k, a.ld_k); rows(a.v, a.ld_v);
+    if (sum == kAttnOut) {
+        rows(a.out, a.ld_out);
+    } else {
+        rows(a.dout, a.ld_dout); rows(a.dq, a.ld_dq); rows(a.dk, a.ld_dk); rows(a.dv, a.ld_dv);
+    }
     p.vec = widest.bytes == 16;
+    Widest wide(32);
+    wide.ptr(p.out); wide.stride(p.ld_out, el); wide.stride(p.d2, el);
+    p.wide = wide.bytes == 32;
     const bool late = sum == kAttnDk || sum == kAttnDv;
     p.scale_in = late ? a.scale : 1.0f;
     p.scale_out = late ? 1.0f : a.scale;
@@ -189,7 +217,10 @@ int run_attention(const tdx_attention_args& a, const AttnShape& shape, AttnSum s
             const uint32_t box[3] = {64, 1, tdx::kAttnRows};
             TDX_TRY(tdx_host::bf16_map(roles[i].at, 3, dims, strides, box, &maps[i]));
         }
-        TDX_TRY(p.state_out ? launch_attention_umma_passes<3>(maps, p, numbers, cut, st) : launch_attention_umma_passes<2>(maps, p, numbers, cut, st));
+        // the state's gradient is the same for dk, which comes behind dv, with its dimensions exchanged
+        p.carry_turned = sum == kAttnDk;
+        const int64_t states = cut && sum != kAttnDk ? attention_sub_numbers(a, p) : 0;
+        TDX_TRY(p.back ? launch_attention_umma_pieces<true>(maps, p, numbers, states, st) : launch_attention_umma_pieces<false>(maps, p, numbers, states, st));
     } else {
         TDX_TRY(attention_padded(p.d1) == 64 ? (launch_attention_pieces<T, 64>(p, numbers, cut, st)) : (launch_attention_pieces<T, 128>(p, numbers, cut, st)));
     }
@@ -214,8 +245,8 @@ int run_attention_pass(const tdx_attention_args* args, AttnPass pass, void* stre
     auto run = [&](AttnSum sum) { return a.dtype == TDX_F32 ? run_attention<float>(a, shape, sum, dev, w, st) : run_attention<__nv_bfloat16>(a, shape, sum, dev, w, st); };
     if (!back) return run(kAttnOut);
     TDX_TRY(run(kAttnDq));
-    TDX_TRY(run(kAttnDk));
-    return run(kAttnDv);
+    TDX_TRY(run(kAttnDv));
+    return run(kAttnDk);
 }
 
 }  // namespace
