@@ -50,9 +50,7 @@ __device__ __forceinline__ void attn_store_32(void* to, const uint32_t* r) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
-__device__ __forceinline__ void attn_prefetch_3d(const CUtensorMap* map, int c0, int c1, int c2) {
-    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(c0), "r"(c1), "r"(c2) : "memory");
-}
+__device__ __forceinline__ void attn_prefetch(const __nv_bfloat16* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 // Registers of a warpgroup; 768 threads are launched with 80 each, and 128 * (40 + 2 * 88 + 56 + 2 * 104) of them are asked for,
 // which is as many.
 template <int N>
@@ -69,6 +67,20 @@ __device__ __forceinline__ void attn_tmem_ld_x16(uint32_t at, uint32_t (&r)[16])
 }
 __device__ __forceinline__ void attn_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// d (+)= a b over `steps` of 16 of the reduction; A1, B1: descriptor units a step, A4, B4: four steps
+template <uint64_t A1, uint64_t A4, uint64_t B1, uint64_t B4>
+__device__ __forceinline__ void attn_products(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, int steps, uint32_t accumulate) {
+#pragma unroll 1
+    for (int s = 0; s < steps; s += 4, a += A4, b += B4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (s + j < steps) {
+                ptx::umma_bf16(d, a + j * A1, b + j * B1, idesc, accumulate);
+                accumulate = 1u;
+            }
+    }
+}
+
 template <bool STATE, int UP>
 struct AttnUmma {
     static constexpr int kSets = STATE || UP == 2 ? 2 : 1;        // of k and v
@@ -82,7 +94,7 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                      const __grid_constant__ AttnParams p) {
     typedef AttnUmma<STATE, UP> Lay;
     extern __shared__ uint8_t attn_raw[];
-    __shared__ __align__(8) uint64_t full_q, free_q, full_kv[2], free_kv[2], bar_w, bar_p, bar_k, bar_o, bar_u, bar_state, bar_o_free, bar_pair[4];
+    __shared__ __align__(8) uint64_t full_q, free_q, full_kv[2], free_kv[2], bar_w, bar_p, bar_k, bar_o, bar_u, bar_state, bar_o_free;
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     __shared__ float power[kAttnRows + 1], weight[2 * kAttnRows];  // l^n; weight[128 + n] = scale_in l^n, 0 for negative n
@@ -95,7 +107,6 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
         for (int i = 0; i < 2; ++i) { ptx::mbar_init(&full_kv[i], 1); ptx::mbar_init(&free_kv[i], 1); }
         ptx::mbar_init(&bar_w, 1); ptx::mbar_init(&bar_p, 8); ptx::mbar_init(&bar_k, 4); ptx::mbar_init(&bar_o, 1); ptx::mbar_init(&bar_u, 1);
         ptx::mbar_init(&bar_state, 8); ptx::mbar_init(&bar_o_free, 8);
-        for (int i = 0; i < 4; ++i) ptx::mbar_init(&bar_pair[i], 2);
         s_abort = 0;
         ptx::fence_barrier_init();
         if (!STATE) ptx::tma_prefetch_desc(&tm_q);
@@ -163,9 +174,6 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                     for (int h = 0; h < halves1; ++h) ptx::tma_load_3d(kv + h * kAttnHalf, &tm_k, &full_kv[set], h * 64, hk, row);
                     for (int h = 0; h < halves2; ++h) ptx::tma_load_3d(kv + kAttnTile + h * kAttnHalf, &tm_v, &full_kv[set], h * 64, hv, row);
                     if (!STATE) {
-                        // q has one tile only: it is brought as far as L2 until the one before has been used
-                        if (c > 0)
-                            for (int h = 0; h < halves1; ++h) attn_prefetch_3d(&tm_q, h * 64, hq, row);
                         if (c > 0 && !wait_bounded_idle(&free_q, (c - 1) & 1, abort_flag, p.status, kTimeoutProducer)) { ok = false; break; }
                         ptx::mbar_arrive_expect_tx(&full_q, halves1 * kAttnHalf);
                         for (int h = 0; h < halves1; ++h) ptx::tma_load_3d(smem + Lay::kQ + h * kAttnHalf, &tm_q, &full_q, h * 64, hq, row);
@@ -176,12 +184,33 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                     for (int i = 0; i < 64; ++i) __nanosleep(2000);
                 }
             }
+        } else if (warp == 2) {
+            // The chunk after next on its way into L2.  The two sets of tiles alone leave a copy one chunk's time, which is about what the
+            // copies of all blocks together take from memory; asked for by the copy engine it would stand in front of the copies.
+            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + head / p.q_share * p.d1;
+            const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(p.k) + head / p.k_share * p.d1;
+            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + head / p.v_share * p.d2;
+            for (int c = 0; c + 2 < chunks; ++c) {
+                if (!wait_bounded_idle(STATE ? &full_kv[c % Lay::kSets] : &bar_w, (STATE ? c / Lay::kSets : c) & 1, abort_flag, p.status, kTimeoutProducer)) break;
+                const long long row = first_of(c + 2);
+                const int n = rows_of(c + 2);
+                for (int i = lane; i < n; i += 32) {
+                    for (int h = 0; h < halves1; ++h) {
+                        attn_prefetch(k + (row + i) * p.ld_k + h * 64);
+                        if (!STATE) attn_prefetch(q + (row + i) * p.ld_q + h * 64);
+                    }
+                    for (int h = 0; h < halves2; ++h) attn_prefetch(v + (row + i) * p.ld_v + h * 64);
+                }
+            }
         } else if (warp == 1) {
             if (ptx::elect_one()) {
                 const uint32_t base = ptx::smem_u32(smem);
-                // K-major operands: 16 of the reduction are 32 bytes further in a 128-byte row, 64 are a half tile; others: 16 rows of 128 bytes
-                auto k_major = [&](uint32_t at, int step) { return ptx::make_smem_desc_sw128(at + (step >> 2) * kAttnHalf + (step & 3) * 32, 16u, 1024u); };
-                auto mn_major = [&](uint32_t at, int step) { return ptx::make_smem_desc_sw128(at + step * 2048, kAttnHalf, 1024u); };
+                // Steps of 16 of the reduction, in 16-byte units: K-major operands are 32 bytes further in a 128-byte row, 64 of the reduction are a
+                // half tile; the others 16 rows of 128 bytes further.  Loops stay loops: unrolled, the roles' code together did not fit
+                // the instruction caches, and every step of this thread waited for its instructions.
+                auto k_major = [&](uint32_t at) { return ptx::make_smem_desc_sw128(at, 16u, 1024u); };
+                auto mn_major = [&](uint32_t at) { return ptx::make_smem_desc_sw128(at, kAttnHalf, 1024u); };
+                constexpr uint64_t kK1 = 32 >> 4, kK4 = kAttnHalf >> 4, kMn1 = 2048 >> 4, kMn4 = 4 * kMn1;
                 const uint32_t idesc_w = ptx::make_idesc_bf16_f32(128, 128, 0, 0), idesc_o = ptx::make_idesc_bf16_f32(128, n2, 0, 1),
                                idesc_u = ptx::make_idesc_bf16_f32(128, n2, 1, 1);
                 bool ok = true;
@@ -194,7 +223,7 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                         // (W takes the place of P, which O2 of the chunk before has to be done with)
                         if (!wait(&full_q, c) || (c > 0 && !wait(&bar_o, c - 1))) break;
                         ptx::tc_fence_after_sync();
-                        for (int s = 0; s < steps1; ++s) ptx::umma_bf16(tmem + kAttnTmemW, k_major(base + Lay::kQ, s), k_major(k, s), idesc_w, s > 0);
+                        attn_products<kK1, kK4, kK1, kK4>(tmem + kAttnTmemW, k_major(base + Lay::kQ), k_major(k), idesc_w, steps1, 0u);
                         ptx::umma_commit(&bar_w);
                     }
                     // (the state in front of the chunk: U has been read)
@@ -202,22 +231,24 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                     if (!STATE) {
                         if (c > 0 && !wait(&bar_o_free, c - 1)) break;
                         ptx::tc_fence_after_sync();
-                        for (int s = 0; s < steps1; ++s) ptx::umma_bf16(tmem + kAttnTmemO1, k_major(base + Lay::kQ, s), mn_major(base + Lay::kState, s), idesc_o, s > 0);
+                        attn_products<kK1, kK4, kMn1, kMn4>(tmem + kAttnTmemO1, k_major(base + Lay::kQ), mn_major(base + Lay::kState), idesc_o, steps1, 0u);
                         ptx::umma_commit(&free_q);
                     }
                     if (!STATE) {
                         // (the keys' warps set the rows of v behind a short chunk to zero)
                         if (!wait(&bar_p, c) || (rows_of(c) < kAttnRows && !wait(&bar_k, c))) break;
                         ptx::tc_fence_after_sync();
-                        for (int s = 0; s < 8; ++s) attn_umma_ta(tmem + kAttnTmemO2, tmem + kAttnTmemW + s * 8, mn_major(v, s), idesc_o, s > 0);
+                        const uint64_t of_v = mn_major(v);
+#pragma unroll 1
+                        for (int s = 0; s < 8; ++s)
+                            attn_umma_ta(tmem + kAttnTmemO2, tmem + kAttnTmemW + (s >> 2) * 64 + (s & 3) * 8, of_v + s * kMn1, idesc_o, s > 0);
                         ptx::umma_commit(&bar_o);
                     }
                     if (!wait(&bar_k, c)) break;
                     ptx::tc_fence_after_sync();
-                    for (int u = UP - 1; u >= 0; --u) {              // small terms first
-                        const uint32_t from = u == 0 ? k : base + Lay::kLow + (u - 1) * kAttnTile;
-                        for (int s = 0; s < 8; ++s) ptx::umma_bf16(tmem + kAttnTmemU, mn_major(from, s), mn_major(v, s), idesc_u, u < UP - 1 || s > 0);
-                    }
+#pragma unroll 1
+                    for (int u = UP - 1; u >= 0; --u)                // small terms first
+                        attn_products<kMn1, kMn4, kMn1, kMn4>(tmem + kAttnTmemU, mn_major(u == 0 ? k : base + Lay::kLow + (u - 1) * kAttnTile), mn_major(v), idesc_u, 8, u < UP - 1);
                     ptx::umma_commit(&free_kv[set]);
                     ptx::umma_commit(&bar_u);
                 }
@@ -226,55 +257,36 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     } else if (warp < 12) {
         attn_more_registers<88>();
         if (!STATE) {
-            // two warps a quarter of the rows, every second group of 32 columns each
+            // two warps a quarter of the rows: 64 columns each
             const int quarter = warp & 3, part = (warp - 4) >> 2, i = quarter * 32 + lane;
             const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-            const int from = BACK ? quarter : 0, to = BACK ? 3 : quarter;   // groups on this side of the diagonal
             for (int c = 0; c < chunks; ++c) {
                 const int n = rows_of(c), shift = c == 0 ? less : 0;
                 if (!wait_bounded_idle(&bar_w, c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
                 ptx::tc_fence_after_sync();
-                uint32_t packed[2][16];
+#pragma unroll 1
+                for (int g = part * 2; g < part * 2 + 2; ++g) {
+                    uint32_t packed[16];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int g = part + 2 * h;
-                    if (g < from || g > to) {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) packed[h][j] = 0u;
-                    } else {
+                    for (int j = 0; j < 16; ++j) packed[j] = 0u;
+                    if (BACK ? g >= quarter : g <= quarter) {    // on this side of the diagonal
                         uint32_t w[32];
                         float f[32];
                         ptx::tmem_ld_32x32b_x32(lanes + kAttnTmemW + g * 32, w);
+                        const float* l = weight + kAttnRows + (BACK ? g * 32 - i : i - g * 32);
                         ptx::tmem_ld_wait();
-                        if (BACK) {
-                            const float* l = weight + kAttnRows + g * 32 - i;
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(w[j]) * l[j];
-                            if (g == quarter || n < kAttnRows) {
+                        for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(w[j]) * l[BACK ? j : -j];
+                        if (g == quarter || (BACK && n < kAttnRows)) {
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) f[j] = g * 32 + j >= i && g * 32 + j < n ? f[j] : 0.0f;
-                            }
-                        } else {
-                            const float* l = weight + kAttnRows + i - g * 32;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(w[j]) * l[-j];
-                            if (g == quarter) {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) f[j] = g * 32 + j <= i ? f[j] : 0.0f;
-                            }
+                            for (int j = 0; j < 32; ++j) f[j] = (BACK ? g * 32 + j >= i && g * 32 + j < n : g * 32 + j <= i) ? f[j] : 0.0f;
                         }
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) packed[h][j] = attn_pair(f[2 * j], f[2 * j + 1]);
+                        for (int j = 0; j < 16; ++j) packed[j] = attn_pair(f[2 * j], f[2 * j + 1]);
                     }
+                    // P takes the place of the first of this warp's two groups of W
+                    attn_tmem_st_x16(lanes + kAttnTmemW + part * 64 + (g & 1) * 16, packed);
                 }
-                // P takes the place of W's first half, once both warps have read theirs
-                ptx::tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&bar_pair[quarter]);
-                if (!wait_bounded_idle(&bar_pair[quarter], c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
-                ptx::tc_fence_after_sync();
-#pragma unroll
-                for (int h = 0; h < 2; ++h) attn_tmem_st_x16(lanes + kAttnTmemW + (part + 2 * h) * 16, packed[h]);
                 attn_tmem_st_wait();
                 ptx::tc_fence_before_sync();
                 __syncwarp();
@@ -285,39 +297,33 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                 const float far = (i < n ? power[BACK ? n - i - shift : i + 1 - shift] : 0.0f) * p.scale_out;
                 const long long to_row = (first_of(c) + i) * p.ld_out + static_cast<long long>(head) * p.d2;
 #pragma unroll 1
-                for (int g = part * 2; g < part * 2 + 2; ++g) {
-                    // 16 columns at a time of both sums
+                for (int col = part * 64; col < min(part * 64 + 64, p.d2); col += 16) {
+                    uint32_t o1[16], o2[16], out[8];
+                    attn_tmem_ld_x16(lanes + kAttnTmemO1 + col, o1);
+                    attn_tmem_ld_x16(lanes + kAttnTmemO2 + col, o2);
+                    ptx::tmem_ld_wait();
+                    float f[16];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int col = g * 32 + h * 16;
-                        if (col >= p.d2) break;
-                        uint32_t o1[16], o2[16], out[8];
-                        attn_tmem_ld_x16(lanes + kAttnTmemO1 + col, o1);
-                        attn_tmem_ld_x16(lanes + kAttnTmemO2 + col, o2);
-                        ptx::tmem_ld_wait();
-                        float f[16];
+                    for (int j = 0; j < 16; ++j) f[j] = fmaf(__uint_as_float(o1[j]), far, __uint_as_float(o2[j]) * p.scale_out);
+                    if (i < n) {
+                        if (p.out_f32) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) f[j] = fmaf(__uint_as_float(o1[j]), far, __uint_as_float(o2[j]) * p.scale_out);
-                        if (i < n) {
-                            if (p.out_f32) {
+                            for (int j = 0; j < 4; ++j)
+                                if (col + j * 4 < p.d2)
+                                    *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to_row + col + j * 4) = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+                        } else {
 #pragma unroll
-                                for (int j = 0; j < 4; ++j)
-                                    if (col + j * 4 < p.d2)
-                                        *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to_row + col + j * 4) = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+                            for (int j = 0; j < 8; ++j) out[j] = attn_pair(f[2 * j], f[2 * j + 1]);
+                            __nv_bfloat16* at = static_cast<__nv_bfloat16*>(p.out) + to_row + col;
+                            if (p.wide) {
+                                attn_store_32(at, out);
                             } else {
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) out[j] = attn_pair(f[2 * j], f[2 * j + 1]);
-                                __nv_bfloat16* at = static_cast<__nv_bfloat16*>(p.out) + to_row + col;
-                                if (p.wide) {
-                                    attn_store_32(at, out);
-                                } else {
-                                    *reinterpret_cast<uint4*>(at) = make_uint4(out[0], out[1], out[2], out[3]);
-                                    if (col + 8 < p.d2) *reinterpret_cast<uint4*>(at + 8) = make_uint4(out[4], out[5], out[6], out[7]);
-                                }
+                                *reinterpret_cast<uint4*>(at) = make_uint4(out[0], out[1], out[2], out[3]);
+                                if (col + 8 < p.d2) *reinterpret_cast<uint4*>(at + 8) = make_uint4(out[4], out[5], out[6], out[7]);
                             }
                         }
-                        __syncwarp();
                     }
+                    __syncwarp();
                 }
                 ptx::tc_fence_before_sync();
                 __syncwarp();
@@ -396,16 +402,22 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
             const int pieces = piece.index * static_cast<int>(p.seg / p.sub);
             const float* from = p.carry + ((p.offsets == nullptr ? piece.b * p.sub_dense : __ldg(p.offsets + piece.b) / p.sub + piece.b) * p.heads + head) * carry_size +
                                 (p.carry_turned ? static_cast<long long>(m) * kAttnRows + side * 64 : static_cast<long long>(side) * 64 * kAttnRows + m);
-            const int apart = p.carry_turned ? 1 : kAttnRows;
             const float all = static_cast<float>(exp(log_l * static_cast<double>(p.sub))), first = BACK ? static_cast<float>(exp(log_l * static_cast<double>(p.sub - 1))) : all;
 #pragma unroll 1
             for (int s = 0; s < pieces; ++s, from += carry_step) {
                 const float f = s == 0 ? first : all;
-                const float* at = from;
+                if (BACK && p.carry_turned) {
 #pragma unroll
-                for (int j = 0; j < 64; ++j) {
-                    st[j] = fmaf(st[j], f, *at);
-                    at += apart;
+                    for (int j = 0; j < 64; j += 4) {
+                        const float4 v = *reinterpret_cast<const float4*>(from + j);
+                        st[j] = fmaf(st[j], f, v.x);
+                        st[j + 1] = fmaf(st[j + 1], f, v.y);
+                        st[j + 2] = fmaf(st[j + 2], f, v.z);
+                        st[j + 3] = fmaf(st[j + 3], f, v.w);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 64; ++j) st[j] = fmaf(st[j], f, from[j * kAttnRows]);
                 }
             }
         }

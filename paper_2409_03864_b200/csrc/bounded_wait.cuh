@@ -31,13 +31,13 @@ __device__ __forceinline__ bool wait_bounded(uint64_t* bar, uint32_t parity, vol
     return wait_bounded_for(bar, parity, s_abort, g_status, code, kWaitLimitCycles);
 }
 
-// The same for kernels whose waiting warps stand beside working ones: the hardware may hold the thread for up to 20 us at a time, so
-// that it does not take issue slots by polling.
+// The same in few instructions, for kernels of many roles whose code is large beside the instruction caches.  The hardware may hold the
+// thread for up to 20 us at a time, so that it does not take issue slots by polling; the limit is two turns of the clock's upper half, 2 to
+// 5 s.
 __device__ __forceinline__ bool wait_bounded_idle(uint64_t* bar, uint32_t parity, volatile int* s_abort, int* g_status, int code) {
-    if (ptx::mbar_try_wait(bar, parity)) return true;
-    const long long t0 = clock64();
-    for (;;) {
-        uint32_t ok;
+    uint32_t ok, began, now;
+    asm volatile("mov.u32 %0, %%clock_hi;" : "=r"(began));
+    do {
         asm volatile(
             "{\n"
             ".reg .pred p;\n"
@@ -48,13 +48,13 @@ __device__ __forceinline__ bool wait_bounded_idle(uint64_t* bar, uint32_t parity
             : "r"(ptx::smem_u32(bar)), "r"(parity), "r"(20000u)
             : "memory");
         if (ok) return true;
-        if (*s_abort) return false;
-        if (clock64() - t0 > kWaitLimitCycles) {
+        asm volatile("mov.u32 %0, %%clock_hi;" : "=r"(now));
+        if (now - began >= 2u) {
             *s_abort = 1;
             atomicCAS(g_status, 0, code);
-            return false;
         }
-    }
+    } while (!*s_abort);
+    return false;
 }
 
 }  // namespace tdx
