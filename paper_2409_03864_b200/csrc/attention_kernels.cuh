@@ -30,10 +30,12 @@ struct AttnParams {
     long long n_slots, state_stride;
     const float* state_in;                  // the state before the first row that is worked on (for `back`: behind the last)
     float* state_out;
+    int state_vec;                          // attn_umma_kernel: states are read and written 16 bytes at a time along d2
     int s1, s2;                             // strides of a state's d1 and d2
     long long seg, dense;                   // rows of a segment; segments of a dense sequence
     float* carry;                           // [number][head][slice][KD][kAttnV]: what a segment adds to the state
     long long sub, sub_dense;               // attn_umma_kernel: rows of a piece of a segment, and pieces of a dense sequence
+    int all_pieces;                         // attn_umma_kernel: the last segment's pieces are wanted too, for state_out
     int carry_turned;                       // attn_umma_kernel: carry was written by a sum with d1 and d2 exchanged
     int slices;                             // of kAttnV columns of v
     int* status;

@@ -5,7 +5,7 @@
 //   warp 1         products: W = q k^T;  O1 = q S0;  O2 = P v;  U = K~^T v
 //   warps 4 - 11   P = W l^(i-j) below the diagonal, bf16, back into tensor memory, from where it is a product's operand; then
 //                  out = l^(i+1) O1 + O2
-//   warps 12 - 15  K~ = l^(n-1-j) k in bf16 pieces, the first in place of k
+//   warps 12 - 15  K~ = l^(n-1-j) k in bf16 pieces, the first in place of k (warps 4 - 15 where there are no outputs)
 //   warps 16 - 23  S1 = l^n S0 + U in fp32 registers, 64 a thread; S1 as bf16 for the next chunk's O1
 //
 // The roles are apart so that a chunk's K~ and W are made while the state and the output of the one in front of it are still worked on:
@@ -51,7 +51,7 @@ __device__ __forceinline__ void attn_store_32(void* to, const uint32_t* r) {
                  : "memory");
 }
 __device__ __forceinline__ void attn_prefetch(const __nv_bfloat16* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-// Registers of a warpgroup; 768 threads are launched with 80 each, and 128 * (40 + 2 * 88 + 56 + 2 * 104) of them are asked for,
+// Registers of a warpgroup; 768 threads are launched with 80 each, and 128 * (56 + 2 * 80 + 56 + 2 * 104) of them are asked for,
 // which is as many.
 template <int N>
 __device__ __forceinline__ void attn_fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -81,12 +81,19 @@ __device__ __forceinline__ void attn_products(uint32_t d, uint64_t a, uint64_t b
     }
 }
 
+// Tiles in shared memory: two of k and (where there is room) v, which are in use until a chunk's U, one of q, which is free after O1.  (Two of q
+// and one of v, and W of the next chunk in front of U, took 5.2 us a chunk of 128 x 128 instead of 4.0.)
 template <bool STATE, int UP>
 struct AttnUmma {
-    static constexpr int kSets = STATE || UP == 2 ? 2 : 1;        // of k and v
-    static constexpr int kQ = 0, kState = STATE ? 0 : kAttnTile, kKv = STATE ? 0 : 2 * kAttnTile, kLow = kKv + kSets * 2 * kAttnTile;
+    static constexpr int kQs = STATE ? 0 : 1, kVs = STATE || UP == 2 ? 2 : 1;
+    static constexpr int kQ = 0, kState = kQ + kQs * kAttnTile, kK = kState + (STATE ? 0 : kAttnTile), kV = kK + 2 * kAttnTile, kLow = kV + kVs * kAttnTile;
     static constexpr int kBytes = kLow + (UP - 1) * kAttnTile;
 };
+
+// number of the first piece of a sequence
+__device__ __forceinline__ long long attn_first_piece(const AttnParams& p, long long b) {
+    return p.offsets == nullptr ? b * p.sub_dense : __ldg(p.offsets + b) / p.sub + b;
+}
 
 template <bool STATE, bool BACK, int UP>
 __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
@@ -94,7 +101,7 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                      const __grid_constant__ AttnParams p) {
     typedef AttnUmma<STATE, UP> Lay;
     extern __shared__ uint8_t attn_raw[];
-    __shared__ __align__(8) uint64_t full_q, free_q, full_kv[2], free_kv[2], bar_w, bar_p, bar_k, bar_o, bar_u, bar_state, bar_o_free;
+    __shared__ __align__(8) uint64_t full_q[2], free_q[2], full_k[2], free_k[2], full_v[2], free_v[2], bar_w[2], bar_p, bar_k, bar_o, bar_u, bar_state, bar_o_free;
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     __shared__ float power[kAttnRows + 1], weight[2 * kAttnRows];  // l^n; weight[128 + n] = scale_in l^n, 0 for negative n
@@ -103,9 +110,9 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     uint8_t* const smem = attn_raw + ((1024u - (ptx::smem_u32(attn_raw) & 1023u)) & 1023u);
 
     if (tid == 0) {
-        ptx::mbar_init(&full_q, 1); ptx::mbar_init(&free_q, 1);
-        for (int i = 0; i < 2; ++i) { ptx::mbar_init(&full_kv[i], 1); ptx::mbar_init(&free_kv[i], 1); }
-        ptx::mbar_init(&bar_w, 1); ptx::mbar_init(&bar_p, 8); ptx::mbar_init(&bar_k, 4); ptx::mbar_init(&bar_o, 1); ptx::mbar_init(&bar_u, 1);
+        for (int i = 0; i < 2; ++i)
+            for (uint64_t* bar : {&full_q[i], &free_q[i], &full_k[i], &free_k[i], &full_v[i], &free_v[i]}) ptx::mbar_init(bar, 1);
+        ptx::mbar_init(&bar_w[0], 1); ptx::mbar_init(&bar_w[1], 1); ptx::mbar_init(&bar_p, 8); ptx::mbar_init(&bar_k, STATE ? 12 : 4); ptx::mbar_init(&bar_o, 1); ptx::mbar_init(&bar_u, 1);
         ptx::mbar_init(&bar_state, 8); ptx::mbar_init(&bar_o_free, 8);
         s_abort = 0;
         ptx::fence_barrier_init();
@@ -127,20 +134,51 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     const long long state_at = slot * p.state_stride + static_cast<long long>(head) * p.d1 * p.d2;
     const bool ends = start + seg >= r.len;
     if (start >= r.len && !(piece.index == 0 && !STATE)) return;
-    if (STATE && start / p.seg == (r.len - 1) / p.seg) return;   // in the last segment: nobody asks for it
+    if (STATE && !p.all_pieces && start / p.seg == (r.len - 1) / p.seg) return;   // in the last segment: nobody asks for it
     const int count = static_cast<int>(ends ? r.len - start : seg);
     const int chunks = (count + kAttnRows - 1) / kAttnRows;
     const int less = BACK && piece.index == 0 ? 1 : 0;         // see attn_kernel
     const double log_l = static_cast<double>(__ldg(p.log_decay + head));
-    if (tid <= kAttnRows) power[tid] = tid == 0 ? 1.0f : static_cast<float>(exp(log_l * tid));
-    if (tid < kAttnRows) {
-        weight[tid] = 0.0f;
-        weight[kAttnRows + tid] = (tid == 0 ? 1.0f : static_cast<float>(exp(log_l * tid))) * p.scale_in;
+    const long long row0 = r.first + (BACK ? r.len - start : start);
+    auto rows_of = [&](int c) { return min(kAttnRows, count - c * kAttnRows); };
+    // Chunk c has the rows first_of(c) .. + rows_of(c) - 1 in their own order, whatever the direction is.
+    auto first_of = [&](int c) { return BACK ? row0 - static_cast<long long>(c) * kAttnRows - rows_of(c) : row0 + static_cast<long long>(c) * kAttnRows; };
+    const int steps1 = (p.d1 + 15) / 16, halves1 = (p.d1 + 63) / 64, halves2 = (p.d2 + 63) / 64, n2 = (p.d2 + 15) / 16 * 16;
+    // copies of a chunk's tiles, by one thread
+    const int hq = head / p.q_share, hk = head / p.k_share, hv = head / p.v_share;
+    auto copy_k = [&](int c) {
+        uint64_t* bar = &full_k[c & 1];
+        ptx::mbar_arrive_expect_tx(bar, halves1 * kAttnHalf);
+        for (int h = 0; h < halves1; ++h) ptx::tma_load_3d(smem + Lay::kK + (c & 1) * kAttnTile + h * kAttnHalf, &tm_k, bar, h * 64, hk, static_cast<int>(first_of(c)));
+    };
+    auto copy_q = [&](int c) {
+        const int set = c % max(Lay::kQs, 1);
+        ptx::mbar_arrive_expect_tx(&full_q[set], halves1 * kAttnHalf);
+        for (int h = 0; h < halves1; ++h) ptx::tma_load_3d(smem + Lay::kQ + set * kAttnTile + h * kAttnHalf, &tm_q, &full_q[set], h * 64, hq, static_cast<int>(first_of(c)));
+    };
+    auto copy_v = [&](int c) {
+        const int set = c % Lay::kVs;
+        ptx::mbar_arrive_expect_tx(&full_v[set], halves2 * kAttnHalf);
+        for (int h = 0; h < halves2; ++h) ptx::tma_load_3d(smem + Lay::kV + set * kAttnTile + h * kAttnHalf, &tm_v, &full_v[set], h * 64, hv, static_cast<int>(first_of(c)));
+    };
+    if (tid == 0 && chunks > 0) {                                // under way while the others make the tables
+        copy_k(0);
+        if (!STATE) copy_q(0);
+        copy_v(0);
+    }
+    if (tid >= 32 && tid <= 32 + kAttnRows) {
+        const int n = tid - 32;
+        const float l = n == 0 ? 1.0f : static_cast<float>(exp(log_l * n));
+        power[n] = l;
+        if (n < kAttnRows) {
+            weight[n] = 0.0f;
+            weight[kAttnRows + n] = l * p.scale_in;
+        }
     }
     // rows of K~ that stand for columns of k behind d1 are never written again
     if (p.d1 <= 64) {
-        for (int s = 0; s < Lay::kSets; ++s)
-            for (int i = tid; i < kAttnHalf / 16; i += kAttnUmmaThreads) *reinterpret_cast<uint4*>(smem + Lay::kKv + s * 2 * kAttnTile + kAttnHalf + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+        for (int s = 0; s < 2; ++s)
+            for (int i = tid; i < kAttnHalf / 16; i += kAttnUmmaThreads) *reinterpret_cast<uint4*>(smem + Lay::kK + s * kAttnTile + kAttnHalf + i * 16) = make_uint4(0u, 0u, 0u, 0u);
         for (int s = 0; s < UP - 1; ++s)
             for (int i = tid; i < kAttnHalf / 16; i += kAttnUmmaThreads) *reinterpret_cast<uint4*>(smem + Lay::kLow + s * kAttnTile + kAttnHalf + i * 16) = make_uint4(0u, 0u, 0u, 0u);
         ptx::fence_proxy_async_smem();
@@ -154,53 +192,57 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     __syncthreads();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = s_tmem;
-    // chunk c has the rows first .. first + n - 1 in their own order, whatever the direction is
-    const long long row0 = r.first + (BACK ? r.len - start : start);
-    auto rows_of = [&](int c) { return min(kAttnRows, count - c * kAttnRows); };
-    auto first_of = [&](int c) { return BACK ? row0 - static_cast<long long>(c) * kAttnRows - rows_of(c) : row0 + static_cast<long long>(c) * kAttnRows; };
-    const int steps1 = (p.d1 + 15) / 16, halves1 = (p.d1 + 63) / 64, halves2 = (p.d2 + 63) / 64, n2 = (p.d2 + 15) / 16 * 16;
-
+    // Each barrier completes once a chunk (those of a set of tiles once a use of the set), and whoever waits for a completion takes part in
+    // what the one after it depends on, so that no waiting warp can be two behind; W runs a chunk ahead of the keys' warps and has two.
     if (warp < 4) {
-        attn_fewer_registers<40>();
+        attn_fewer_registers<56>();
         if (warp == 0) {
-            if (ptx::elect_one()) {
-                const int hq = head / p.q_share, hk = head / p.k_share, hv = head / p.v_share;
-                bool ok = true;
-                for (int c = 0; ok && c < chunks; ++c) {
-                    const int row = static_cast<int>(first_of(c)), set = c % Lay::kSets, use = c / Lay::kSets;
-                    if (use > 0 && !wait_bounded_idle(&free_kv[set], (use - 1) & 1, abort_flag, p.status, kTimeoutProducer)) { ok = false; break; }
-                    uint8_t* kv = smem + Lay::kKv + set * 2 * kAttnTile;
-                    ptx::mbar_arrive_expect_tx(&full_kv[set], (halves1 + halves2) * kAttnHalf);
-                    for (int h = 0; h < halves1; ++h) ptx::tma_load_3d(kv + h * kAttnHalf, &tm_k, &full_kv[set], h * 64, hk, row);
-                    for (int h = 0; h < halves2; ++h) ptx::tma_load_3d(kv + kAttnTile + h * kAttnHalf, &tm_v, &full_kv[set], h * 64, hv, row);
-                    if (!STATE) {
-                        if (c > 0 && !wait_bounded_idle(&free_q, (c - 1) & 1, abort_flag, p.status, kTimeoutProducer)) { ok = false; break; }
-                        ptx::mbar_arrive_expect_tx(&full_q, halves1 * kAttnHalf);
-                        for (int h = 0; h < halves1; ++h) ptx::tma_load_3d(smem + Lay::kQ + h * kAttnHalf, &tm_q, &full_q, h * 64, hq, row);
+            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + hq * p.d1;
+            const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(p.k) + hk * p.d1;
+            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + hv * p.d2;
+            bool ok = true;
+            auto wait = [&](uint64_t* bar, int use) { return ok = ok && (use < 0 || wait_bounded_idle(bar, use & 1, abort_flag, p.status, kTimeoutProducer)); };
+            constexpr int kQs = Lay::kQs > 0 ? Lay::kQs : 1, kVs = Lay::kVs;
+#pragma unroll 1
+            for (int c = 0; c < chunks; ++c) {
+                // in the order in which the tiles become free
+                if (c > 0) {
+                    if (!wait(&free_k[c & 1], c / 2 - 1)) break;
+                    if (ptx::elect_one()) copy_k(c);
+                    if (kVs == 2) {
+                        if (!wait(&free_v[c & 1], c / 2 - 1)) break;
+                        if (ptx::elect_one()) copy_v(c);
+                    }
+                    __syncwarp();
+                }
+                // The chunk after next on its way into L2: the tiles alone leave a copy one chunk's time.  (Asked for by the copy engine it would
+                // stand in front of the copies.)
+                if (c + 2 < chunks) {
+                    const long long ahead = first_of(c + 2);
+                    const int n = rows_of(c + 2);
+                    for (int i = lane; i < n; i += 32) {
+                        for (int h = 0; h < halves1; ++h) {
+                            attn_prefetch(k + (ahead + i) * p.ld_k + h * 64);
+                            if (!STATE) attn_prefetch(q + (ahead + i) * p.ld_q + h * 64);
+                        }
+                        for (int h = 0; h < halves2; ++h) attn_prefetch(v + (ahead + i) * p.ld_v + h * 64);
                     }
                 }
-                if (!ok) {
-                    // let copies that are still in flight land before the block goes away
-                    for (int i = 0; i < 64; ++i) __nanosleep(2000);
+                if (c > 0) {
+                    if (!STATE) {
+                        if (!wait(&free_q[c % kQs], c / kQs - 1)) break;
+                        if (ptx::elect_one()) copy_q(c);
+                    }
+                    if (kVs == 1) {
+                        if (!wait(&free_v[0], c - 1)) break;
+                        if (ptx::elect_one()) copy_v(c);
+                    }
+                    __syncwarp();
                 }
             }
-        } else if (warp == 2) {
-            // The chunk after next on its way into L2.  The two sets of tiles alone leave a copy one chunk's time, which is about what the
-            // copies of all blocks together take from memory; asked for by the copy engine it would stand in front of the copies.
-            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + head / p.q_share * p.d1;
-            const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(p.k) + head / p.k_share * p.d1;
-            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + head / p.v_share * p.d2;
-            for (int c = 0; c + 2 < chunks; ++c) {
-                if (!wait_bounded_idle(STATE ? &full_kv[c % Lay::kSets] : &bar_w, (STATE ? c / Lay::kSets : c) & 1, abort_flag, p.status, kTimeoutProducer)) break;
-                const long long row = first_of(c + 2);
-                const int n = rows_of(c + 2);
-                for (int i = lane; i < n; i += 32) {
-                    for (int h = 0; h < halves1; ++h) {
-                        attn_prefetch(k + (row + i) * p.ld_k + h * 64);
-                        if (!STATE) attn_prefetch(q + (row + i) * p.ld_q + h * 64);
-                    }
-                    for (int h = 0; h < halves2; ++h) attn_prefetch(v + (row + i) * p.ld_v + h * 64);
-                }
+            if (!ok) {
+                // let copies that are still in flight land before the block goes away
+                for (int i = 0; i < 64; ++i) __nanosleep(2000);
             }
         } else if (warp == 1) {
             if (ptx::elect_one()) {
@@ -215,28 +257,18 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                                idesc_u = ptx::make_idesc_bf16_f32(128, n2, 1, 1);
                 bool ok = true;
                 auto wait = [&](uint64_t* bar, int use) { return ok = ok && wait_bounded_idle(bar, use & 1, abort_flag, p.status, kTimeoutMma); };
-                for (int c = 0; ok && c < chunks; ++c) {
-                    const int set = c % Lay::kSets;
-                    const uint32_t k = base + Lay::kKv + set * 2 * kAttnTile, v = k + kAttnTile;
-                    if (!wait(&full_kv[set], c / Lay::kSets)) break;
-                    if (!STATE) {
-                        // (W takes the place of P, which O2 of the chunk before has to be done with)
-                        if (!wait(&full_q, c) || (c > 0 && !wait(&bar_o, c - 1))) break;
+                constexpr int kQs = Lay::kQs > 0 ? Lay::kQs : 1, kVs = Lay::kVs;
+#pragma unroll 1
+                for (int c = STATE ? 0 : -1; ok && c < chunks; ++c) {
+                    const uint32_t k = base + Lay::kK + (c & 1) * kAttnTile, v = base + Lay::kV + (c & (kVs - 1)) * kAttnTile;
+                    if (!STATE && c >= 0) {
+                        // (the state in front of the chunk is there, and U has been read)
+                        if (!wait(&bar_state, c) || (c > 0 && !wait(&bar_o_free, c - 1))) break;
                         ptx::tc_fence_after_sync();
-                        attn_products<kK1, kK4, kK1, kK4>(tmem + kAttnTmemW, k_major(base + Lay::kQ), k_major(k), idesc_w, steps1, 0u);
-                        ptx::umma_commit(&bar_w);
-                    }
-                    // (the state in front of the chunk: U has been read)
-                    if (!wait(&bar_state, c)) break;
-                    if (!STATE) {
-                        if (c > 0 && !wait(&bar_o_free, c - 1)) break;
-                        ptx::tc_fence_after_sync();
-                        attn_products<kK1, kK4, kMn1, kMn4>(tmem + kAttnTmemO1, k_major(base + Lay::kQ), mn_major(base + Lay::kState), idesc_o, steps1, 0u);
-                        ptx::umma_commit(&free_q);
-                    }
-                    if (!STATE) {
+                        attn_products<kK1, kK4, kMn1, kMn4>(tmem + kAttnTmemO1, k_major(base + Lay::kQ + c % kQs * kAttnTile), mn_major(base + Lay::kState), idesc_o, steps1, 0u);
+                        ptx::umma_commit(&free_q[c % kQs]);
                         // (the keys' warps set the rows of v behind a short chunk to zero)
-                        if (!wait(&bar_p, c) || (rows_of(c) < kAttnRows && !wait(&bar_k, c))) break;
+                        if (!wait(&full_v[c % kVs], c / kVs) || !wait(&bar_p, c) || (rows_of(c) < kAttnRows && !wait(&bar_k, c))) break;
                         ptx::tc_fence_after_sync();
                         const uint64_t of_v = mn_major(v);
 #pragma unroll 1
@@ -244,25 +276,36 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                             attn_umma_ta(tmem + kAttnTmemO2, tmem + kAttnTmemW + (s >> 2) * 64 + (s & 3) * 8, of_v + s * kMn1, idesc_o, s > 0);
                         ptx::umma_commit(&bar_o);
                     }
+                    if (c >= 0) {
+                    if (STATE && (!wait(&full_k[c & 1], c / 2) || !wait(&full_v[c % kVs], c / kVs) || !wait(&bar_state, c))) break;
                     if (!wait(&bar_k, c)) break;
                     ptx::tc_fence_after_sync();
 #pragma unroll 1
                     for (int u = UP - 1; u >= 0; --u)                // small terms first
                         attn_products<kMn1, kMn4, kMn1, kMn4>(tmem + kAttnTmemU, mn_major(u == 0 ? k : base + Lay::kLow + (u - 1) * kAttnTile), mn_major(v), idesc_u, 8, u < UP - 1);
-                    ptx::umma_commit(&free_kv[set]);
+                    ptx::umma_commit(&free_k[c & 1]);
+                    ptx::umma_commit(&free_v[c % kVs]);
                     ptx::umma_commit(&bar_u);
+                    }
+                    if (!STATE && c + 1 < chunks) {
+                        // the next chunk's W: its k and q are there, and O2 is done with P, whose place W takes
+                        const int next = c + 1;
+                        if (!wait(&full_k[next & 1], next / 2) || !wait(&full_q[next % kQs], next / kQs) || (c >= 0 && !wait(&bar_o, c))) break;
+                        ptx::tc_fence_after_sync();
+                        attn_products<kK1, kK4, kK1, kK4>(tmem + kAttnTmemW, k_major(base + Lay::kQ + next % kQs * kAttnTile), k_major(base + Lay::kK + (next & 1) * kAttnTile), idesc_w, steps1, 0u);
+                        ptx::umma_commit(&bar_w[next & 1]);
+                    }
                 }
             }
         }
-    } else if (warp < 12) {
-        attn_more_registers<88>();
-        if (!STATE) {
+    } else if (!STATE && warp < 12) {
+        {
             // two warps a quarter of the rows: 64 columns each
             const int quarter = warp & 3, part = (warp - 4) >> 2, i = quarter * 32 + lane;
             const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
             for (int c = 0; c < chunks; ++c) {
                 const int n = rows_of(c), shift = c == 0 ? less : 0;
-                if (!wait_bounded_idle(&bar_w, c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+                if (!wait_bounded_idle(&bar_w[c & 1], c >> 1 & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
                 ptx::tc_fence_after_sync();
 #pragma unroll 1
                 for (int g = part * 2; g < part * 2 + 2; ++g) {
@@ -332,23 +375,27 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
         }
     } else if (warp < 16) {
         attn_fewer_registers<56>();
-        const int worker = tid - 12 * 32;
+        constexpr int kWorkers = STATE ? 12 * 32 : 4 * 32;       // without outputs their warps make keys too
+        const int worker = tid - (16 * 32 - kWorkers);
         for (int c = 0; c < chunks; ++c) {
-            const int n = rows_of(c), set = c % Lay::kSets;
-            if (!wait_bounded_idle(&full_kv[set], (c / Lay::kSets) & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+            const int n = rows_of(c);
+            if (!wait_bounded_idle(&full_k[c & 1], c >> 1 & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+            if (n < kAttnRows && !wait_bounded_idle(&full_v[c % Lay::kVs], c / Lay::kVs & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
             // q k^T has been read from k before it is overwritten, and U of the chunk before from the other pieces
-            if (!STATE && !wait_bounded_idle(&bar_w, c & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+            if (!STATE && !wait_bounded_idle(&bar_w[c & 1], c >> 1 & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
             if (c > 0 && !wait_bounded_idle(&bar_u, (c - 1) & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
-            uint8_t* const k = smem + Lay::kKv + set * 2 * kAttnTile;
-            // two 16-byte pieces a thread at a time
+            uint8_t* const k = smem + Lay::kK + (c & 1) * kAttnTile;
+            // twice 16 bytes a thread at a time
+            const int parts = halves1 * (kAttnHalf / 16);
 #pragma unroll 1
-            for (int first = worker; first < halves1 * (kAttnHalf / 16); first += 256) {
+            for (int first = worker; first < parts; first += 2 * kWorkers) {
                 uint4 in[2];
 #pragma unroll
-                for (int q = 0; q < 2; ++q) in[q] = *reinterpret_cast<const uint4*>(k + (first + q * 128) * 16);
+                for (int q = 0; q < 2; ++q)
+                    in[q] = first + q * kWorkers < parts ? *reinterpret_cast<const uint4*>(k + (first + q * kWorkers) * 16) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    const int at = first + q * 128, row = at / 8 % kAttnRows;
+                    const int at = first + q * kWorkers, row = at / 8 % kAttnRows;
                     const float w = weight[kAttnRows + (BACK ? row : n - 1 - row)];
                     if (row >= n) in[q] = make_uint4(0u, 0u, 0u, 0u);
                     const f32x2 ww = pack2(w, w), minus = pack2(-1.0f, -1.0f);
@@ -365,14 +412,16 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                             if (u + 1 < UP) left = fma2(pack2(attn_lo(out[u][j]), attn_hi(out[u][j])), minus, left);
                         }
                     }
+                    if (at < parts) {
 #pragma unroll
-                    for (int u = 0; u < UP; ++u)
-                        *reinterpret_cast<uint4*>((u == 0 ? k : smem + Lay::kLow + (u - 1) * kAttnTile) + at * 16) = make_uint4(out[u][0], out[u][1], out[u][2], out[u][3]);
+                        for (int u = 0; u < UP; ++u)
+                            *reinterpret_cast<uint4*>((u == 0 ? k : smem + Lay::kLow + (u - 1) * kAttnTile) + at * 16) = make_uint4(out[u][0], out[u][1], out[u][2], out[u][3]);
+                    }
                 }
             }
             if (n < kAttnRows) {
                 for (int h = 0; h < halves2; ++h)
-                    for (int at = worker; at < (kAttnRows - n) * 8; at += 128) *reinterpret_cast<uint4*>(k + kAttnTile + h * kAttnHalf + n * 128 + at * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    for (int at = worker; at < (kAttnRows - n) * 8; at += kWorkers) *reinterpret_cast<uint4*>(smem + Lay::kV + c % Lay::kVs * kAttnTile + h * kAttnHalf + n * 128 + at * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
             ptx::fence_proxy_async_smem();
             __syncwarp();
@@ -384,23 +433,32 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
         const int quarter = warp & 3, side = (warp - 16) >> 2, m = quarter * 32 + lane;
         const bool mine = side < halves2;
         float st[64];
+        // What the pieces in front of a row add to the state: [column][row], so that a warp's rows lie side by side, or (a sum with the roles
+        // of the state's dimensions exchanged) [row][column].
+        const long long carry_size = kAttnRows * kAttnRows, carry_step = carry_size * p.heads;
 #pragma unroll
         for (int j = 0; j < 64; ++j) st[j] = 0.0f;
         if (!STATE && p.state_in != nullptr && slot >= 0 && m < p.d1) {
             const float* from = p.state_in + state_at + static_cast<long long>(m) * p.s1 + static_cast<long long>(side) * 64 * p.s2;
             const int there = p.d2 - side * 64;
+            if (p.state_vec) {
 #pragma unroll
-            for (int j = 0; j < 64; ++j) {
-                if (j < there) st[j] = __ldg(from);
-                from += p.s2;
+                for (int j = 0; j < 64; j += 4)
+                    if (j < there) {
+                        const float4 v = __ldg(reinterpret_cast<const float4*>(from + j));
+                        st[j] = v.x; st[j + 1] = v.y; st[j + 2] = v.z; st[j + 3] = v.w;
+                    }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 64; ++j) {
+                    if (j < there) st[j] = __ldg(from);
+                    from += p.s2;
+                }
             }
         }
-        // what a segment's pieces add to the state: [column][row], so that a warp's rows lie side by side, or (a sum with the roles of
-        // the state's dimensions exchanged) [row][column]
-        const long long carry_size = kAttnRows * kAttnRows, carry_step = carry_size * p.heads;
         if (!STATE && piece.index > 0 && mine) {
             const int pieces = piece.index * static_cast<int>(p.seg / p.sub);
-            const float* from = p.carry + ((p.offsets == nullptr ? piece.b * p.sub_dense : __ldg(p.offsets + piece.b) / p.sub + piece.b) * p.heads + head) * carry_size +
+            const float* from = p.carry + (attn_first_piece(p, piece.b) * p.heads + head) * carry_size +
                                 (p.carry_turned ? static_cast<long long>(m) * kAttnRows + side * 64 : static_cast<long long>(side) * 64 * kAttnRows + m);
             const float all = static_cast<float>(exp(log_l * static_cast<double>(p.sub))), first = BACK ? static_cast<float>(exp(log_l * static_cast<double>(p.sub - 1))) : all;
 #pragma unroll 1
@@ -460,14 +518,20 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
 #pragma unroll
                 for (int j = 0; j < 64; ++j) to[j * kAttnRows] = st[j];
             }
-        } else if (ends && p.state_out != nullptr && slot >= 0 && m < p.d1) {
+        } else if (UP == 3 && ends && p.state_out != nullptr && slot >= 0 && m < p.d1) {
             const float f = BACK && r.len > 0 ? static_cast<float>(exp(log_l)) : 1.0f;   // see attn_kernel
             float* to = p.state_out + state_at + static_cast<long long>(m) * p.s1 + static_cast<long long>(side) * 64 * p.s2;
             const int there = p.d2 - side * 64;
+            if (p.state_vec) {
 #pragma unroll
-            for (int j = 0; j < 64; ++j) {
-                if (j < there) *to = st[j] * f;
-                to += p.s2;
+                for (int j = 0; j < 64; j += 4)
+                    if (j < there) *reinterpret_cast<float4*>(to + j) = make_float4(st[j] * f, st[j + 1] * f, st[j + 2] * f, st[j + 3] * f);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 64; ++j) {
+                    if (j < there) *to = st[j] * f;
+                    to += p.s2;
+                }
             }
         }
     }
@@ -478,6 +542,42 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
         __syncwarp();
         ptx::tmem_dealloc(tmem, 512);
     }
+}
+
+// The states behind sequences in several segments, from what their pieces add (made of three pieces of the keys): a block has 32 x 32
+// of one head's state, its rows side by side while it adds, its columns for the states in and out.
+__global__ void __launch_bounds__(256) attn_state_kernel(const __grid_constant__ AttnParams p) {
+    __shared__ float tile[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n0 = blockIdx.x % 4 * 32, m0 = blockIdx.x / 4 % 4 * 32;
+    const int head = static_cast<int>(blockIdx.x / 16 % p.heads);
+    const long long b = blockIdx.x / 16 / p.heads;
+    seq_grid_wait();
+    if (m0 >= p.d1 || n0 >= p.d2) return;
+    const SeqRange r = seq_range(p.offsets, b, p.max_len, p.rows, p.status);
+    const long long slot = state_slot(p.slots, b, p.n_slots, p.status);
+    if (slot < 0) return;
+    const long long at = slot * p.state_stride + static_cast<long long>(head) * p.d1 * p.d2;
+    const double log_l = static_cast<double>(__ldg(p.log_decay + head));
+    const long long pieces = (r.len + p.sub - 1) / p.sub, last = r.len - (pieces - 1) * p.sub;
+    const float* carry = p.carry + (attn_first_piece(p, b) * p.heads + head) * kAttnRows * kAttnRows;
+    for (int i = warp; i < 32; i += 8)
+        tile[i][lane] = p.state_in != nullptr && m0 + i < p.d1 && n0 + lane < p.d2 ? __ldg(p.state_in + at + static_cast<long long>(m0 + i) * p.s1 + static_cast<long long>(n0 + lane) * p.s2) : 0.0f;
+    __syncthreads();
+    float st[4];
+    for (int i = 0; i < 4; ++i) st[i] = tile[lane][warp + i * 8];
+    const float all = static_cast<float>(exp(log_l * static_cast<double>(p.sub)));
+    for (long long s = 0; s < pieces; ++s) {
+        const long long rows = s + 1 < pieces ? p.sub : last, left = p.back && s == 0 ? rows - 1 : rows;   // see attn_kernel
+        const float f = left == 0 ? 1.0f : left == p.sub ? all : static_cast<float>(exp(log_l * static_cast<double>(left)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st[i] = fmaf(st[i], f, carry[s * p.heads * kAttnRows * kAttnRows + (n0 + warp + i * 8) * kAttnRows + m0 + lane]);
+    }
+    __syncthreads();
+    const float f = p.back && r.len > 0 ? static_cast<float>(exp(log_l)) : 1.0f;
+    for (int i = 0; i < 4; ++i) tile[lane][warp + i * 8] = st[i] * f;
+    __syncthreads();
+    for (int i = warp; i < 32; i += 8)
+        if (m0 + i < p.d1 && n0 + lane < p.d2) p.state_out[at + static_cast<long long>(m0 + i) * p.s1 + static_cast<long long>(n0 + lane) * p.s2] = tile[i][lane];
 }
 
 }  // namespace tdx

@@ -58,7 +58,7 @@ int check_attention(const tdx_attention_args* args, AttnPass pass, AttnShape* sh
 // run side by side; where they do not fill the SMs evenly, sequences are cut into segments, which costs a look at k and v of all but the
 // last one for what they add to the state (about half a segment's time) and two chunks' time a block for its start.  The number of segments
 // with the least estimated time is taken.
-void plan_attention(const tdx_attention_args& a, int d2, bool umma, int sm_count, tdx::AttnParams* p) {
+void plan_attention(const tdx_attention_args& a, int d2, bool umma, bool all_pieces, int sm_count, tdx::AttnParams* p) {
     const int64_t longest = std::max<int64_t>(1, std::min(a.max_len, a.rows));
     const int64_t side = a.seq_offsets ? std::max<int64_t>(1, a.rows / longest) : std::max<int64_t>(1, a.batch);
     const int64_t chunk = umma ? tdx::kAttnRows : tdx::kAttnC, slots = umma ? sm_count : 2 * sm_count;
@@ -78,10 +78,11 @@ void plan_attention(const tdx_attention_args& a, int d2, bool umma, int sm_count
         }
     }
     p->dense = std::max<int64_t>(1, ceil_div(a.max_len, p->seg));
-    // the pass over the states has all segments but the last: pieces of them, as many as fill the SMs
+    // the pass over the states has all segments but the last (with state_out that one too): pieces of them, as many as fill the SMs
     p->sub = p->seg;
+    p->all_pieces = all_pieces;
     if (umma) {
-        const int64_t busy = tiles * std::max<int64_t>(1, ceil_div(longest, p->seg) - 1), most = p->seg / tdx::kAttnRows;
+        const int64_t busy = tiles * std::max<int64_t>(1, ceil_div(longest, p->seg) - (all_pieces ? 0 : 1)), most = p->seg / tdx::kAttnRows;
         int64_t k = std::min(most, std::max<int64_t>(1, sm_count / busy));
         while (most % k) --k;
         p->sub = p->seg / k;
@@ -103,8 +104,9 @@ AttnWorkspace attention_workspace(const tdx_attention_args& a, const AttnShape& 
     tdx::AttnParams p;
     for (int sum = 0; sum < (back ? 4 : 1); ++sum) {
         const int d1 = sum == kAttnOut || sum == kAttnDv ? a.dim_k : a.dim_v, d2 = sum == kAttnOut || sum == kAttnDv ? a.dim_v : a.dim_k;
-        for (int umma = 0; umma < 2; ++umma) {                   // whichever the alignment allows
-            plan_attention(a, d2, umma != 0, sm_count, &p);
+        for (int way = 0; way < 3; ++way) {                      // whichever the alignment allows, with and without state_out
+            const bool umma = way > 0;
+            plan_attention(a, d2, umma, way == 2, sm_count, &p);
             const size_t each = umma ? tdx::kAttnRows * tdx::kAttnRows : p.slices * attention_padded(d1) * tdx::kAttnV;
             if (attention_cut(a, p)) w.carry = std::max(w.carry, static_cast<size_t>(attention_sub_numbers(a, p)) * a.heads * each * sizeof(float));
         }
@@ -141,15 +143,17 @@ int launch_attention_umma(const CUtensorMap (&maps)[3], const tdx::AttnParams& p
     TDX_TRY(allow_smem(tdx::attn_umma_kernel<STATE, BACK, UP>, known, kBytes, static_cast<int>(kBytes)));
     return launch_seq(tdx::attn_umma_kernel<STATE, BACK, UP>, numbers * p.heads, 1, tdx::kAttnUmmaThreads, kBytes, st, maps[0], maps[1], maps[2], p);
 }
-// states: the number of pieces of the pass over the states, 0 where there is none to make
-template <bool BACK, int UP>
-int launch_attention_umma_passes(const CUtensorMap (&maps)[3], const tdx::AttnParams& p, int64_t numbers, int64_t states, cudaStream_t st) {
-    if (states > 0) TDX_TRY((launch_attention_umma<true, BACK, UP>(maps, p, states, st)));
-    return launch_attention_umma<false, BACK, UP>(maps, p, numbers, st);
-}
+// states: the number of pieces of the pass over the states, 0 where there is none to make.  States that are handed on come from three
+// bf16 pieces of the keys: out of the pass over the states where there is one, else (which leaves one tile of v) on the way.
 template <bool BACK>
-int launch_attention_umma_pieces(const CUtensorMap (&maps)[3], const tdx::AttnParams& p, int64_t numbers, int64_t states, cudaStream_t st) {
-    return p.state_out ? launch_attention_umma_passes<BACK, 3>(maps, p, numbers, states, st) : launch_attention_umma_passes<BACK, 2>(maps, p, numbers, states, st);
+int launch_attention_umma_passes(const CUtensorMap (&maps)[3], const tdx::AttnParams& p, int64_t numbers, int64_t states, bool cut, cudaStream_t st) {
+    if (p.state_out && cut) {
+        TDX_TRY((launch_attention_umma<true, BACK, 3>(maps, p, states, st)));
+        TDX_TRY(launch_seq(tdx::attn_state_kernel, p.batch * p.heads * 16, 1, 256, 0, st, p));
+        return launch_attention_umma<false, BACK, 2>(maps, p, numbers, st);
+    }
+    if (states > 0) TDX_TRY((launch_attention_umma<true, BACK, 2>(maps, p, states, st)));
+    return p.state_out ? launch_attention_umma<false, BACK, 3>(maps, p, numbers, st) : launch_attention_umma<false, BACK, 2>(maps, p, numbers, st);
 }
 
 template <typename T>
@@ -202,10 +206,12 @@ int run_attention(const tdx_attention_args& a, const AttnShape& shape, AttnSum s
     const bool turned = sum == kAttnDq || sum == kAttnDk;        // the state's columns are this sum's first dimension
     p.s1 = turned ? 1 : a.dim_v;
     p.s2 = turned ? a.dim_v : 1;
+    p.state_vec = !turned && a.dim_v % 4 == 0 && p.state_stride % 4 == 0 && !misaligned(p.state_in, 16) && !misaligned(p.state_out, 16);
     p.status = dev.status;
     p.carry = static_cast<float*>(a.workspace);
     const bool umma = sizeof(T) == 2 && p.vec && a.rows > 0;
-    plan_attention(a, p.d2, umma, dev.sm_count, &p);
+    const bool all_pieces = (sum == kAttnOut ? a.state_out : late ? a.dstate_in : nullptr) != nullptr;
+    plan_attention(a, p.d2, umma, all_pieces, dev.sm_count, &p);
     const int64_t numbers = attention_numbers(a, p);
     const bool cut = attention_cut(a, p);
     if (umma) {
@@ -220,7 +226,7 @@ int run_attention(const tdx_attention_args& a, const AttnShape& shape, AttnSum s
         // the state's gradient is the same for dk, which comes behind dv, with its dimensions exchanged
         p.carry_turned = sum == kAttnDk;
         const int64_t states = cut && sum != kAttnDk ? attention_sub_numbers(a, p) : 0;
-        TDX_TRY(p.back ? launch_attention_umma_pieces<true>(maps, p, numbers, states, st) : launch_attention_umma_pieces<false>(maps, p, numbers, states, st));
+        TDX_TRY(p.back ? launch_attention_umma_passes<true>(maps, p, numbers, states, cut, st) : launch_attention_umma_passes<false>(maps, p, numbers, states, cut, st));
     } else {
         TDX_TRY(attention_padded(p.d1) == 64 ? (launch_attention_pieces<T, 64>(p, numbers, cut, st)) : (launch_attention_pieces<T, 128>(p, numbers, cut, st)));
     }
