@@ -20,6 +20,8 @@
 #include "attention_kernels.cuh"
 #include "bounded_wait.cuh"
 
+#include <limits.h>
+
 namespace tdx {
 
 constexpr int kAttnRows = 128;                                   // rows of a chunk here
@@ -51,7 +53,7 @@ __device__ __forceinline__ void attn_store_32(void* to, const uint32_t* r) {
                  : "memory");
 }
 __device__ __forceinline__ void attn_prefetch(const __nv_bfloat16* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-// Registers of a warpgroup; 768 threads are launched with 80 each, and 128 * (56 + 2 * 80 + 56 + 2 * 104) of them are asked for,
+// Registers of a warpgroup; 768 threads are launched with 80 each, and 128 * (40 + 2 * 88 + 56 + 2 * 104) of them are asked for,
 // which is as many.
 template <int N>
 __device__ __forceinline__ void attn_fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -103,9 +105,9 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     extern __shared__ uint8_t attn_raw[];
     __shared__ __align__(8) uint64_t full_q[2], free_q[2], full_k[2], free_k[2], full_v[2], free_v[2], bar_w[2], bar_p, bar_k, bar_o, bar_u, bar_state, bar_o_free;
     __shared__ uint32_t s_tmem;
-    __shared__ int s_abort;
+    __shared__ int s_abort, s_progress;
     __shared__ float power[kAttnRows + 1], weight[2 * kAttnRows];  // l^n; weight[128 + n] = scale_in l^n, 0 for negative n
-    volatile int* abort_flag = &s_abort;
+    volatile int *abort_flag = &s_abort, *progress = &s_progress;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint8_t* const smem = attn_raw + ((1024u - (ptx::smem_u32(attn_raw) & 1023u)) & 1023u);
 
@@ -114,7 +116,7 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
             for (uint64_t* bar : {&full_q[i], &free_q[i], &full_k[i], &free_k[i], &full_v[i], &free_v[i]}) ptx::mbar_init(bar, 1);
         ptx::mbar_init(&bar_w[0], 1); ptx::mbar_init(&bar_w[1], 1); ptx::mbar_init(&bar_p, 8); ptx::mbar_init(&bar_k, STATE ? 12 : 4); ptx::mbar_init(&bar_o, 1); ptx::mbar_init(&bar_u, 1);
         ptx::mbar_init(&bar_state, 8); ptx::mbar_init(&bar_o_free, 8);
-        s_abort = 0;
+        s_abort = s_progress = 0;
         ptx::fence_barrier_init();
         if (!STATE) ptx::tma_prefetch_desc(&tm_q);
         ptx::tma_prefetch_desc(&tm_k);
@@ -195,11 +197,8 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     // Each barrier completes once a chunk (those of a set of tiles once a use of the set), and whoever waits for a completion takes part in
     // what the one after it depends on, so that no waiting warp can be two behind; W runs a chunk ahead of the keys' warps and has two.
     if (warp < 4) {
-        attn_fewer_registers<56>();
+        attn_fewer_registers<40>();
         if (warp == 0) {
-            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + hq * p.d1;
-            const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(p.k) + hk * p.d1;
-            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + hv * p.d2;
             bool ok = true;
             auto wait = [&](uint64_t* bar, int use) { return ok = ok && (use < 0 || wait_bounded_idle(bar, use & 1, abort_flag, p.status, kTimeoutProducer)); };
             constexpr int kQs = Lay::kQs > 0 ? Lay::kQs : 1, kVs = Lay::kVs;
@@ -215,19 +214,7 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                     }
                     __syncwarp();
                 }
-                // The chunk after next on its way into L2: the tiles alone leave a copy one chunk's time.  (Asked for by the copy engine it would
-                // stand in front of the copies.)
-                if (c + 2 < chunks) {
-                    const long long ahead = first_of(c + 2);
-                    const int n = rows_of(c + 2);
-                    for (int i = lane; i < n; i += 32) {
-                        for (int h = 0; h < halves1; ++h) {
-                            attn_prefetch(k + (ahead + i) * p.ld_k + h * 64);
-                            if (!STATE) attn_prefetch(q + (ahead + i) * p.ld_q + h * 64);
-                        }
-                        for (int h = 0; h < halves2; ++h) attn_prefetch(v + (ahead + i) * p.ld_v + h * 64);
-                    }
-                }
+                if (lane == 0) *progress = c + 1;
                 if (c > 0) {
                     if (!STATE) {
                         if (!wait(&free_q[c % kQs], c / kQs - 1)) break;
@@ -240,9 +227,29 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                     __syncwarp();
                 }
             }
+            if (lane == 0) *progress = INT_MAX;
             if (!ok) {
                 // let copies that are still in flight land before the block goes away
                 for (int i = 0; i < 64; ++i) __nanosleep(2000);
+            }
+        } else if (warp == 2) {
+            // The chunk after next on its way into L2 once chunk c's copies are asked for: the tiles alone leave a copy one chunk's time.  (Asked for
+            // by the copy engine it would stand in front of the copies.)  The copies' warp says how far it is, at its end that it is done.
+            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + hq * p.d1;
+            const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(p.k) + hk * p.d1;
+            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + hv * p.d2;
+#pragma unroll 1
+            for (int c = 0; c + 2 < chunks; ++c) {
+                while (*progress <= c) __nanosleep(100);
+                const long long ahead = first_of(c + 2);
+                const int n = rows_of(c + 2);
+                for (int i = lane; i < n; i += 32) {
+                    for (int h = 0; h < halves1; ++h) {
+                        attn_prefetch(k + (ahead + i) * p.ld_k + h * 64);
+                        if (!STATE) attn_prefetch(q + (ahead + i) * p.ld_q + h * 64);
+                    }
+                    for (int h = 0; h < halves2; ++h) attn_prefetch(v + (ahead + i) * p.ld_v + h * 64);
+                }
             }
         } else if (warp == 1) {
             if (ptx::elect_one()) {
@@ -299,6 +306,7 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
             }
         }
     } else if (!STATE && warp < 12) {
+        attn_more_registers<88>();
         {
             // two warps a quarter of the rows: 64 columns each
             const int quarter = warp & 3, part = (warp - 4) >> 2, i = quarter * 32 + lane;
