@@ -118,11 +118,31 @@ int check_norm(const tdx_norm_args* args, bool back, tdx::NormParams* p) {
     return TDX_OK;
 }
 
+template <typename T, int VEC, int NV, int HAS>
+int launch_norm_has(bool back, const tdx::NormParams& p, const NormPlan& plan, cudaStream_t st) {
+    const int threads = plan.warps * plan.sets * 32;
+    return back ? launch_seq(tdx::norm_bwd_kernel<T, VEC, NV, HAS>, plan.grid, 1, threads, plan.smem, st, p)
+                : launch_seq(tdx::norm_fwd_kernel<T, VEC, NV, HAS>, plan.grid, 1, threads, plan.smem, st, p);
+}
+// Kernels of their own for what calls usually have, where rows are 16-byte aligned and up to 512 threads hold them with one access each:
+// heads' norm with gate; stream's sum and next norm, with and without the block's norm, its gate and its scale; a norm alone.
 template <typename T, int VEC, int NV>
 int launch_norm(bool back, const tdx::NormParams& p, const NormPlan& plan, cudaStream_t st) {
-    const int threads = plan.warps * plan.sets * 32;
-    return back ? launch_seq(tdx::norm_bwd_kernel<T, VEC, NV>, plan.grid, 1, threads, plan.smem, st, p)
-                : launch_seq(tdx::norm_fwd_kernel<T, VEC, NV>, plan.grid, 1, threads, plan.smem, st, p);
+    if constexpr (VEC * sizeof(T) == 16 && NV == 1) {
+        const int has = (p.norm_in ? tdx::kNormIn : 0) | (p.gate ? tdx::kNormGate : 0) | (p.scale ? tdx::kNormScale : 0) | (p.residual ? tdx::kNormResidual : 0) |
+                        ((back ? p.dy : p.y) ? tdx::kNormY : 0) | ((back ? p.dsum : p.sum) ? tdx::kNormSum : 0);
+        constexpr int kHeads = tdx::kNormIn | tdx::kNormGate | tdx::kNormSum, kStream = tdx::kNormResidual | tdx::kNormY | tdx::kNormSum;
+        switch (has) {
+            case kHeads: return launch_norm_has<T, VEC, NV, kHeads>(back, p, plan, st);
+            case kStream: return launch_norm_has<T, VEC, NV, kStream>(back, p, plan, st);
+            case kStream | tdx::kNormIn: return launch_norm_has<T, VEC, NV, kStream | tdx::kNormIn>(back, p, plan, st);
+            case kStream | tdx::kNormIn | tdx::kNormScale: return launch_norm_has<T, VEC, NV, kStream | tdx::kNormIn | tdx::kNormScale>(back, p, plan, st);
+            case kStream | kHeads | tdx::kNormScale: return launch_norm_has<T, VEC, NV, kStream | kHeads | tdx::kNormScale>(back, p, plan, st);
+            case tdx::kNormY: return launch_norm_has<T, VEC, NV, static_cast<int>(tdx::kNormY)>(back, p, plan, st);
+            default: break;
+        }
+    }
+    return launch_norm_has<T, VEC, NV, -1>(back, p, plan, st);
 }
 template <typename T>
 int launch_norm_wide(bool back, const tdx::NormParams& p, const NormPlan& plan, cudaStream_t st) {

@@ -114,22 +114,72 @@ struct NormRow {
     }
 };
 
+// Channels are worked on in pairs (one instruction for two), or alone where rows allow no wider access.
+template <int VEC> struct NormLanes { typedef f32x2 type; static constexpr int kCount = VEC / 2; };
+template <> struct NormLanes<1> { typedef float type; static constexpr int kCount = 1; };
+__device__ __forceinline__ f32x2 nmul(f32x2 a, f32x2 b) { return mul2(a, b); }
+__device__ __forceinline__ float nmul(float a, float b) { return a * b; }
+__device__ __forceinline__ f32x2 nfma(f32x2 a, f32x2 b, f32x2 c) { return fma2(a, b, c); }
+__device__ __forceinline__ float nfma(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ void nall(float v, f32x2& r) { r = pack2(v, v); }
+__device__ __forceinline__ void nall(float v, float& r) { r = v; }
+__device__ __forceinline__ float nsum(f32x2 v) {
+    float a, b;
+    unpack2(v, a, b);
+    return a + b;
+}
+__device__ __forceinline__ float nsum(float v) { return v; }
+template <typename T>
+__device__ __forceinline__ f32x2 nsigmoid(f32x2 v) {
+    float a, b;
+    unpack2(v, a, b);
+    return pack2(sigmoid_f<T>(a), sigmoid_f<T>(b));
+}
+template <typename T>
+__device__ __forceinline__ float nsigmoid(float v) { return sigmoid_f<T>(v); }
+template <int VEC, int N>
+__device__ __forceinline__ void norm_unpack(const SeqVec<float, VEC>& r, f32x2 (&f)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = pack2(r.v[2 * i], r.v[2 * i + 1]);
+}
+// (through the words: one operation a value, where taking the halves out as bf16 is two)
+template <int VEC, int N>
+__device__ __forceinline__ void norm_unpack(const SeqVec<__nv_bfloat16, VEC>& r, f32x2 (&f)[N]) {
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(&r.bits);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = pack2(__uint_as_float(words[i] << 16), __uint_as_float(words[i] & 0xFFFF0000u));
+}
+template <typename T>
+__device__ __forceinline__ void norm_unpack(const SeqVec<T, 1>& r, float (&f)[1]) { f[0] = seq_to_float(r.v[0]); }
+template <int VEC, int N>
+__device__ __forceinline__ void norm_flat(const f32x2 (&f)[N], float (&r)[VEC]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) unpack2(f[i], r[2 * i], r[2 * i + 1]);
+}
 template <int VEC>
-__device__ __forceinline__ void norm_param(const float* p, int c, float (&f)[VEC]) {
+__device__ __forceinline__ void norm_flat(const float (&f)[1], float (&r)[VEC]) { r[0] = f[0]; }
+template <int VEC>
+__device__ __forceinline__ void norm_param(const float* p, int c, typename NormLanes<VEC>::type (&f)[NormLanes<VEC>::kCount]) {
+    constexpr int kN = NormLanes<VEC>::kCount, kStep = VEC >= 4 ? 4 : VEC;
     if (p == nullptr) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) f[i] = 1.0f;
+        for (int i = 0; i < kN; ++i) nall(1.0f, f[i]);
         return;
     }
-    constexpr int kStep = VEC >= 4 ? 4 : VEC;
 #pragma unroll
     for (int i = 0; i < VEC; i += kStep) {
-        float part[kStep];
-        seq_unpack(seq_load<float, kStep>(p + c + i), part);
+        const SeqVec<float, kStep> part = seq_load<float, kStep>(p + c + i);
+        typename NormLanes<kStep>::type g[NormLanes<kStep>::kCount];
+        norm_unpack(part, g);
 #pragma unroll
-        for (int j = 0; j < kStep; ++j) f[i + j] = part[j];
+        for (int j = 0; j < NormLanes<kStep>::kCount; ++j) f[i / 2 + j] = g[j];
     }
 }
+// What a call has.  Kernels for the usual combinations know it when they are compiled (HAS >= 0), which saves them the operations of
+// what is not there; the others look it up.
+enum : int { kNormIn = 1, kNormGate = 2, kNormScale = 4, kNormResidual = 8, kNormY = 16, kNormSum = 32 };
+template <int HAS>
+__device__ __forceinline__ bool norm_has(int flag, bool looked_up) { return HAS >= 0 ? (HAS & flag) != 0 : looked_up; }
 // One vector of every activation that a row has; what it lacks stays zero.
 template <typename T, int VEC>
 __device__ __forceinline__ SeqVec<T, VEC> norm_load(const void* base, long long ld, long long row, int c, bool there) {
@@ -140,8 +190,19 @@ __device__ __forceinline__ SeqVec<T, VEC> norm_load(const void* base, long long 
     return r;
 }
 template <typename T, int VEC>
-__device__ __forceinline__ void norm_store(void* base, long long ld, long long row, int c, const float (&f)[VEC]) {
-    seq_store<T, VEC>(static_cast<T*>(base) + row * ld + c, f);
+__device__ __forceinline__ void norm_store(void* base, long long ld, long long row, int c, const typename NormLanes<VEC>::type (&f)[NormLanes<VEC>::kCount]) {
+    float flat[VEC];
+    norm_flat<VEC>(f, flat);
+    T* to = static_cast<T*>(base) + row * ld + c;
+    if constexpr (sizeof(T) == 2 && VEC > 1) {
+        SeqVec<T, VEC> r;
+        __nv_bfloat162* pairs = reinterpret_cast<__nv_bfloat162*>(&r.bits);
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) pairs[i] = __floats2bfloat162_rn(flat[2 * i], flat[2 * i + 1]);
+        *reinterpret_cast<typename SeqVec<T, VEC>::bits_t*>(to) = r.bits;
+    } else {
+        seq_store<T, VEC>(to, flat);
+    }
 }
 __device__ __forceinline__ NormRow norm_row(const NormParams& p, float* shared) {
     NormRow r;
@@ -158,11 +219,15 @@ __device__ __forceinline__ NormRow norm_row(const NormParams& p, float* shared) 
     return r;
 }
 
-template <typename T, int VEC, int NV>
+template <typename T, int VEC, int NV, int HAS>
 __global__ void __launch_bounds__(kNormThreads, NV * VEC <= 8 ? 2 : 1) norm_fwd_kernel(const __grid_constant__ NormParams p) {
+    typedef typename NormLanes<VEC>::type Lane;
+    constexpr int N = NormLanes<VEC>::kCount;
     extern __shared__ float norm_shared[];
     NormRow r = norm_row(p, norm_shared);
     const int sets = (blockDim.x >> 5) / p.warps;
+    const bool in = norm_has<HAS>(kNormIn, p.norm_in), gate = norm_has<HAS>(kNormGate, p.gate != nullptr), scale = norm_has<HAS>(kNormScale, p.scale != nullptr),
+               residual = norm_has<HAS>(kNormResidual, p.residual != nullptr), out = norm_has<HAS>(kNormY, p.y != nullptr), sum = norm_has<HAS>(kNormSum, p.sum != nullptr);
     seq_grid_wait();
     const long long step = static_cast<long long>(gridDim.x) * sets;
     SeqVec<T, VEC> nx[NV], ng[NV], nr[NV];
@@ -172,72 +237,82 @@ __global__ void __launch_bounds__(kNormThreads, NV * VEC <= 8 ? 2 : 1) norm_fwd_
             const int c = (r.thread + i * r.threads) * VEC;
             const bool there = c < p.channels && row < p.rows;
             nx[i] = norm_load<T, VEC>(p.x, p.ld_x, row, c, there);
-            ng[i] = norm_load<T, VEC>(p.gate, p.ld_gate, row, c, there);
-            nr[i] = norm_load<T, VEC>(p.residual, p.ld_residual, row, c, there);
+            if (gate) ng[i] = norm_load<T, VEC>(p.gate, p.ld_gate, row, c, there);
+            if (residual) nr[i] = norm_load<T, VEC>(p.residual, p.ld_residual, row, c, there);
         }
     };
     constexpr bool kAhead = NV * VEC <= 8;                       // wider threads have no registers to spare
     long long row = static_cast<long long>(blockIdx.x) * sets + r.slot;
     if (kAhead) fetch(row);
     for (; row < p.rows; row += step) {
+        SeqVec<T, VEC> vg[NV], vr[NV];
+        Lane s[NV][N];
         if (!kAhead) fetch(row);
-        SeqVec<T, VEC> vx[NV], vg[NV], vr[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) { vx[i] = nx[i]; vg[i] = ng[i]; vr[i] = nr[i]; }
-        if (kAhead) fetch(row + step);                           // on its way while this row is worked on
-        float rstd[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float f[VEC];
-            seq_unpack(vx[i], f);
-            rstd[i] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) rstd[i] = fmaf(f[j], f[j], rstd[i]);
+            norm_unpack(nx[i], s[i]);
+            vg[i] = ng[i];
+            vr[i] = nr[i];
         }
-        if (p.norm_in) {
+        if (kAhead) fetch(row + step);                           // on its way while this row is worked on
+        float rstd[NV];
+        if (in) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                Lane square;
+                nall(0.0f, square);
+#pragma unroll
+                for (int j = 0; j < N; ++j) square = nfma(s[i][j], s[i][j], square);
+                rstd[i] = nsum(square);
+            }
             r.group_sum(p, rstd);
 #pragma unroll
             for (int i = 0; i < NV; ++i) rstd[i] = rsqrtf(fmaf(rstd[i], p.inv_group, p.eps));
         }
-        float s[NV][VEC], square = 0.0f;
+        Lane square;
+        nall(0.0f, square);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (r.thread + i * r.threads) * VEC;
             if (c < p.channels) {
-                seq_unpack(vx[i], s[i]);
-                if (p.norm_in) {
-                    float w[VEC];
-                    norm_param(p.weight_in, c, w);
+                if (in) {
+                    Lane w[N], rs;
+                    nall(rstd[i], rs);
+                    norm_param<VEC>(p.weight_in, c, w);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) s[i][j] = s[i][j] * rstd[i] * w[j];
+                    for (int j = 0; j < N; ++j) s[i][j] = nmul(nmul(s[i][j], rs), w[j]);
                 }
-                if (p.gate != nullptr) {
-                    float g[VEC];
-                    seq_unpack(vg[i], g);
+                if (gate) {
+                    Lane g[N];
+                    norm_unpack(vg[i], g);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) s[i][j] *= g[j] * sigmoid_f<T>(g[j]);
+                    for (int j = 0; j < N; ++j) s[i][j] = nmul(s[i][j], nmul(g[j], nsigmoid<T>(g[j])));
                 }
-                float k[VEC], add[VEC];
-                norm_param(p.scale, c, k);
-                seq_unpack(vr[i], add);
+                Lane k[N], add[N];
+                if (scale) norm_param<VEC>(p.scale, c, k);
+                if (residual) norm_unpack(vr[i], add);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    s[i][j] = fmaf(k[j], s[i][j], add[j]);
-                    square = fmaf(s[i][j], s[i][j], square);
+                for (int j = 0; j < N; ++j) {
+                    Lane one;
+                    nall(1.0f, one);
+                    if (scale && !residual) s[i][j] = nmul(k[j], s[i][j]);
+                    if (residual) s[i][j] = nfma(scale ? k[j] : one, s[i][j], add[j]);
+                    if (out) square = nfma(s[i][j], s[i][j], square);
                 }
-                if (p.sum != nullptr) norm_store<T, VEC>(p.sum, p.ld_sum, row, c, s[i]);
+                if (sum) norm_store<T, VEC>(p.sum, p.ld_sum, row, c, s[i]);
             }
         }
-        if (p.y != nullptr) {
-            const float rs = rsqrtf(fmaf(r.row_sum(square), p.inv_channels, p.eps));
+        if (out) {
+            Lane rs;
+            nall(rsqrtf(fmaf(r.row_sum(nsum(square)), p.inv_channels, p.eps)), rs);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (r.thread + i * r.threads) * VEC;
                 if (c < p.channels) {
-                    float w[VEC];
-                    norm_param(p.weight_out, c, w);
+                    Lane w[N];
+                    norm_param<VEC>(p.weight_out, c, w);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) w[j] *= s[i][j] * rs;
+                    for (int j = 0; j < N; ++j) w[j] = nmul(w[j], nmul(s[i][j], rs));
                     norm_store<T, VEC>(p.y, p.ld_y, row, c, w);
                 }
             }
@@ -251,21 +326,28 @@ __global__ void __launch_bounds__(kNormThreads, NV * VEC <= 8 ? 2 : 1) norm_fwd_
 //   dweight_out = sum over rows of dy sh,  dscale = of ds a,  dweight_in = of du xh.
 // s is computed again from x, gate and residual, which costs no more bytes than reading it and keeps its 32 bits.  A thread keeps
 // its channels' parameter sums in registers over all rows of its set; a second kernel adds the sets in a fixed order.
-template <typename T, int VEC, int NV>
+template <typename T, int VEC, int NV, int HAS>
 __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_constant__ NormParams p) {
+    typedef typename NormLanes<VEC>::type Lane;
+    constexpr int N = NormLanes<VEC>::kCount;
+    // with up to 8 channels a thread the registers hold the next row's vectors too
+    constexpr bool kAhead = NV * VEC <= 8;
     extern __shared__ float norm_shared[];
     NormRow r = norm_row(p, norm_shared);
     const int sets = (blockDim.x >> 5) / p.warps;
     const long long set = static_cast<long long>(blockIdx.x) * sets + r.slot;
-    float sum_in[NV][VEC], sum_scale[NV][VEC], sum_out[NV][VEC];
+    const bool in = norm_has<HAS>(kNormIn, p.norm_in), gate = norm_has<HAS>(kNormGate, p.gate != nullptr), scale = norm_has<HAS>(kNormScale, p.scale != nullptr),
+               residual = norm_has<HAS>(kNormResidual, p.residual != nullptr), out = norm_has<HAS>(kNormY, p.dy != nullptr), sum = norm_has<HAS>(kNormSum, p.dsum != nullptr);
+    Lane sum_in[NV][N], sum_scale[NV][N], sum_out[NV][N], zero, one, minus;
+    nall(0.0f, zero);
+    nall(1.0f, one);
+    nall(-1.0f, minus);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) sum_in[i][j] = sum_scale[i][j] = sum_out[i][j] = 0.0f;
+        for (int j = 0; j < N; ++j) sum_in[i][j] = sum_scale[i][j] = sum_out[i][j] = zero;
     seq_grid_wait();
     const long long step = static_cast<long long>(gridDim.x) * sets;
-    // with up to 8 channels a thread the registers hold the next row's vectors and the parameters too
-    constexpr bool kAhead = NV * VEC <= 8;
     SeqVec<T, VEC> vx[NV], vg[NV], vr[NV], vs[NV], vy[NV], nx[NV], ng[NV], nr[NV], ns[NV], ny[NV];
     auto fetch = [&](long long row) {
 #pragma unroll
@@ -273,154 +355,142 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_con
             const int c = (r.thread + i * r.threads) * VEC;
             const bool there = c < p.channels && row < p.rows;
             nx[i] = norm_load<T, VEC>(p.x, p.ld_x, row, c, there);
-            ng[i] = norm_load<T, VEC>(p.gate, p.ld_gate, row, c, there);
-            nr[i] = norm_load<T, VEC>(p.residual, p.ld_residual, row, c, there && p.dy != nullptr);
-            ns[i] = norm_load<T, VEC>(p.dsum, p.ld_dsum, row, c, there);
-            ny[i] = norm_load<T, VEC>(p.dy, p.ld_dy, row, c, there);
+            if (gate) ng[i] = norm_load<T, VEC>(p.gate, p.ld_gate, row, c, there);
+            if (out && residual) nr[i] = norm_load<T, VEC>(p.residual, p.ld_residual, row, c, there);
+            if (sum) ns[i] = norm_load<T, VEC>(p.dsum, p.ld_dsum, row, c, there);
+            if (out) ny[i] = norm_load<T, VEC>(p.dy, p.ld_dy, row, c, there);
         }
     };
     if (kAhead) fetch(set);
-    float keep_in[NV][VEC], keep_scale[NV][VEC], keep_out[NV][VEC];
-    if (kAhead) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (r.thread + i * r.threads) * VEC;
-            if (c < p.channels) {
-                norm_param(p.norm_in ? p.weight_in : nullptr, c, keep_in[i]);
-                norm_param(p.scale, c, keep_scale[i]);
-                norm_param(p.weight_out, c, keep_out[i]);
-            }
-        }
-    }
-    auto param = [&](const float* from, const float (&kept)[VEC], int c, float (&f)[VEC]) {
-        if (kAhead) {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) f[j] = kept[j];
-        } else {
-            norm_param(from, c, f);
-        }
-    };
     for (long long row = set; row < p.rows; row += step) {
         if (!kAhead) fetch(row);
 #pragma unroll
         for (int i = 0; i < NV; ++i) { vx[i] = nx[i]; vg[i] = ng[i]; vr[i] = nr[i]; vs[i] = ns[i]; vy[i] = ny[i]; }
         if (kAhead) fetch(row + step);
         float rstd[NV];
-        if (p.norm_in) {
+        if (in) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                float f[VEC];
-                seq_unpack(vx[i], f);
-                rstd[i] = 0.0f;
+                Lane x[N], square = zero;
+                norm_unpack(vx[i], x);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) rstd[i] = fmaf(f[j], f[j], rstd[i]);
+                for (int j = 0; j < N; ++j) square = nfma(x[j], x[j], square);
+                rstd[i] = nsum(square);
             }
             r.group_sum(p, rstd);
 #pragma unroll
             for (int i = 0; i < NV; ++i) rstd[i] = rsqrtf(fmaf(rstd[i], p.inv_group, p.eps));
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) rstd[i] = 1.0f;
         }
-        // the way forward once more: xh = x rstd, a; then ds
-        float ds[NV][VEC], a[NV][VEC], sig[NV][VEC];
-        float square = 0.0f, inner = 0.0f;
+        // The way forward once more: u, a and, for y's part of ds, the sums of s^2 and t s.
+        Lane u[NV][N], sig[NV][N], squares = zero, inners = zero;
+        auto gated = [&](int i, int j, Lane g) { return gate ? nmul(u[i][j], nmul(g, sig[i][j])) : u[i][j]; };
+        auto total = [&](Lane k, Lane a, Lane add) { return residual ? nfma(scale ? k : one, a, add) : scale ? nmul(k, a) : a; };
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (r.thread + i * r.threads) * VEC;
             if (c < p.channels) {
-                float w[VEC];
-                seq_unpack(vx[i], a[i]);
-                param(p.norm_in ? p.weight_in : nullptr, keep_in[i], c, w);
+                Lane g[N];
+                norm_unpack(vx[i], u[i]);
+                if (in) {
+                    Lane w[N], rs;
+                    nall(rstd[i], rs);
+                    norm_param<VEC>(p.weight_in, c, w);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) a[i][j] *= rstd[i] * w[j];
-                if (p.gate != nullptr) {
-                    float g[VEC];
-                    seq_unpack(vg[i], g);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        sig[i][j] = sigmoid_f<T>(g[j]);
-                        a[i][j] *= g[j] * sig[i][j];
-                    }
+                    for (int j = 0; j < N; ++j) u[i][j] = nmul(nmul(u[i][j], rs), w[j]);
                 }
-                if (p.dy != nullptr) {
-                    float k[VEC], add[VEC], dy[VEC], wo[VEC];
-                    param(p.scale, keep_scale[i], c, k);
-                    param(p.weight_out, keep_out[i], c, wo);
-                    seq_unpack(vr[i], add);
-                    seq_unpack(vy[i], dy);
+                if (gate) {
+                    norm_unpack(vg[i], g);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        const float s = fmaf(k[j], a[i][j], add[j]);
-                        square = fmaf(s, s, square);
-                        inner = fmaf(dy[j] * wo[j], s, inner);
+                    for (int j = 0; j < N; ++j) sig[i][j] = nsigmoid<T>(g[j]);
+                }
+                if (out) {
+                    Lane k[N], add[N], dy[N], wo[N];
+                    if (scale) norm_param<VEC>(p.scale, c, k);
+                    norm_param<VEC>(p.weight_out, c, wo);
+                    if (residual) norm_unpack(vr[i], add);
+                    norm_unpack(vy[i], dy);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const Lane s = total(k[j], gated(i, j, g[j]), add[j]);
+                        squares = nfma(s, s, squares);
+                        inners = nfma(nmul(dy[j], wo[j]), s, inners);
                     }
                 }
             }
         }
-        float rs = 0.0f, mean = 0.0f;
-        if (p.dy != nullptr) {
+        Lane rs_out = zero, less = zero;                         // rstd_out, and -mean(t sh)
+        if (out) {
+            float square = nsum(squares), inner = nsum(inners);
             r.row_sums(square, inner);
-            rs = rsqrtf(fmaf(square, p.inv_channels, p.eps));
-            mean = inner * rs * p.inv_channels;                  // mean(t sh)
+            const float rs = rsqrtf(fmaf(square, p.inv_channels, p.eps));
+            nall(rs, rs_out);
+            nall(-inner * rs * p.inv_channels, less);
         }
+        Lane t[NV][N];
         float group[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (r.thread + i * r.threads) * VEC;
             group[i] = 0.0f;
             if (c < p.channels) {
-                float k[VEC], w[VEC], x[VEC];
-                param(p.scale, keep_scale[i], c, k);
-                seq_unpack(vs[i], ds[i]);
-                if (p.dy != nullptr) {
-                    float add[VEC], dy[VEC], wo[VEC];
-                    param(p.weight_out, keep_out[i], c, wo);
-                    seq_unpack(vr[i], add);
-                    seq_unpack(vy[i], dy);
+                Lane k[N], ds[N], g[N];
+                if (scale) norm_param<VEC>(p.scale, c, k);
+                if (sum) norm_unpack(vs[i], ds);
+                if (gate) norm_unpack(vg[i], g);
+                if (out) {
+                    Lane add[N], dy[N], wo[N];
+                    norm_param<VEC>(p.weight_out, c, wo);
+                    if (residual) norm_unpack(vr[i], add);
+                    norm_unpack(vy[i], dy);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        const float sh = fmaf(k[j], a[i][j], add[j]) * rs;
-                        ds[i][j] = fmaf(rs, fmaf(-sh, mean, dy[j] * wo[j]), ds[i][j]);
-                        sum_out[i][j] = fmaf(dy[j], sh, sum_out[i][j]);
+                    for (int j = 0; j < N; ++j) {
+                        const Lane sh = nmul(total(k[j], gated(i, j, g[j]), add[j]), rs_out), part = nfma(sh, less, nmul(dy[j], wo[j]));
+                        ds[j] = sum ? nfma(rs_out, part, ds[j]) : nmul(rs_out, part);
+                        sum_out[i][j] = nfma(dy[j], sh, sum_out[i][j]);
                     }
                 }
-                if (p.dresidual != nullptr) norm_store<T, VEC>(p.dresidual, p.ld_dresidual, row, c, ds[i]);
-                seq_unpack(vx[i], x);
-                param(p.norm_in ? p.weight_in : nullptr, keep_in[i], c, w);
-                float g[VEC], dg[VEC];
-                seq_unpack(vg[i], g);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    sum_scale[i][j] = fmaf(ds[i][j], a[i][j], sum_scale[i][j]);
-                    const float da = ds[i][j] * k[j], xh = x[j] * rstd[i];
-                    float du = da;
-                    if (p.gate != nullptr) {
-                        dg[j] = da * (xh * w[j]) * sig[i][j] * fmaf(g[j], 1.0f - sig[i][j], 1.0f);
-                        du = da * (g[j] * sig[i][j]);
-                    }
-                    sum_in[i][j] = fmaf(du, xh, sum_in[i][j]);
-                    ds[i][j] = du * w[j];                        // t' from here on
-                    group[i] = fmaf(ds[i][j], xh, group[i]);
+                if (residual) norm_store<T, VEC>(p.dresidual, p.ld_dresidual, row, c, ds);
+                Lane dg[N], groups = zero, w[N], x[N], rs;
+                if (in) {
+                    nall(rstd[i], rs);
+                    norm_param<VEC>(p.weight_in, c, w);
+                    norm_unpack(vx[i], x);
                 }
-                if (p.dgate != nullptr) norm_store<T, VEC>(p.dgate, p.ld_dgate, row, c, dg);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    if (scale || p.want_scale) sum_scale[i][j] = nfma(ds[j], gated(i, j, g[j]), sum_scale[i][j]);
+                    Lane d = scale ? nmul(ds[j], k[j]) : ds[j];
+                    if (gate) {
+                        // silu' = sig (1 + g (1 - sig))
+                        dg[j] = nmul(nmul(d, u[i][j]), nmul(sig[i][j], nfma(g[j], nfma(sig[i][j], minus, one), one)));
+                        d = nmul(d, nmul(g[j], sig[i][j]));
+                    }
+                    t[i][j] = d;
+                    if (in) {
+                        const Lane xh = nmul(x[j], rs);
+                        sum_in[i][j] = nfma(d, xh, sum_in[i][j]);
+                        t[i][j] = nmul(d, w[j]);
+                        groups = nfma(t[i][j], xh, groups);
+                    }
+                }
+                if (gate) norm_store<T, VEC>(p.dgate, p.ld_dgate, row, c, dg);
+                group[i] = nsum(groups);
             }
         }
-        if (p.norm_in) r.group_sum(p, group);
-        if (p.dx != nullptr) {
+        if (in) r.group_sum(p, group);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = (r.thread + i * r.threads) * VEC;
-                if (c < p.channels) {
-                    if (p.norm_in) {
-                        float x[VEC];
-                        seq_unpack(vx[i], x);
-                        const float m = group[i] * p.inv_group * rstd[i];
+        for (int i = 0; i < NV; ++i) {
+            const int c = (r.thread + i * r.threads) * VEC;
+            if (c < p.channels) {
+                if (in) {
+                    Lane x[N], m, rs;
+                    norm_unpack(vx[i], x);
+                    nall(-group[i] * p.inv_group * rstd[i], m);
+                    nall(rstd[i], rs);
 #pragma unroll
-                        for (int j = 0; j < VEC; ++j) ds[i][j] = rstd[i] * fmaf(-x[j], m, ds[i][j]);
-                    }
-                    norm_store<T, VEC>(p.dx, p.ld_dx, row, c, ds[i]);
+                    for (int j = 0; j < N; ++j) t[i][j] = nmul(rs, nfma(x[j], m, t[i][j]));
                 }
+                norm_store<T, VEC>(p.dx, p.ld_dx, row, c, t[i]);
             }
         }
     }
@@ -429,11 +499,15 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_con
     for (int i = 0; i < NV; ++i) {
         const int c = (r.thread + i * r.threads) * VEC;
         if (c < p.channels) {
+            float flat[3][VEC];
+            norm_flat<VEC>(sum_in[i], flat[0]);
+            norm_flat<VEC>(sum_scale[i], flat[1]);
+            norm_flat<VEC>(sum_out[i], flat[2]);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                if (p.want_in) part[c + j] = sum_in[i][j];
-                if (p.want_scale) part[p.channels + c + j] = sum_scale[i][j];
-                if (p.want_out) part[2 * p.channels + c + j] = sum_out[i][j];
+                if (p.want_in) part[c + j] = flat[0][j];
+                if (p.want_scale) part[p.channels + c + j] = flat[1][j];
+                if (p.want_out) part[2 * p.channels + c + j] = flat[2][j];
             }
         }
     }
