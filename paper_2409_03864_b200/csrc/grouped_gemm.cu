@@ -39,15 +39,16 @@ int check_grouped(const tdx_grouped_args* args, tdx::GroupedPass pass, tdx::Grou
     return TDX_OK;
 }
 
-template <typename T, int PASS, int BM>
-int launch_grouped_simt(const tdx::GroupedParams& p, cudaStream_t st) {
-    const int64_t tiles_n = ceil_div(PASS == tdx::kGroupedForward ? p.N : p.K, tdx::kSimtN);
-    const int64_t tiles_m = PASS == tdx::kGroupedDw ? p.experts * ceil_div(p.N, BM) : tdx::seq_pieces(true, p.experts, p.rows, 0, BM);
-    return launch_seq(tdx::grouped_simt_kernel<T, PASS, BM>, tiles_m * tiles_n, 1, 128, 0, st, p);
+template <typename T, int PASS, int BM, int BN>
+int launch_grouped_simt(const tdx::GroupedParams& p, int64_t tiles_m, cudaStream_t st) {
+    return launch_seq(tdx::grouped_simt_kernel<T, PASS, BM, BN>, tiles_m * ceil_div(PASS == tdx::kGroupedForward ? p.N : p.K, BN), 1, 128, 0, st, p);
 }
 template <typename T, int PASS>
-int launch_grouped_rows(const tdx::GroupedParams& p, cudaStream_t st) {
-    return p.rows <= 16 * static_cast<int64_t>(p.experts) && PASS != tdx::kGroupedDw ? launch_grouped_simt<T, PASS, 16>(p, st) : launch_grouped_simt<T, PASS, 64>(p, st);
+int launch_grouped_rows(const tdx::GroupedParams& p, int sm_count, cudaStream_t st) {
+    auto tiles = [&](int64_t bm) { return PASS == tdx::kGroupedDw ? p.experts * ceil_div(p.N, bm) : tdx::seq_pieces(true, p.experts, p.rows, 0, bm); };
+    if (p.rows <= 16 * static_cast<int64_t>(p.experts) && PASS != tdx::kGroupedDw) return launch_grouped_simt<T, PASS, 16, 128>(p, tiles(16), st);
+    const int64_t wide = tiles(64) * ceil_div(PASS == tdx::kGroupedForward ? p.N : p.K, 128);
+    return wide < 4 * sm_count ? launch_grouped_simt<T, PASS, 64, 64>(p, tiles(64), st) : launch_grouped_simt<T, PASS, 64, 128>(p, tiles(64), st);
 }
 
 // The tensor-core kernel reads operands by the copy engine and writes 16 bytes at a time.
@@ -69,9 +70,13 @@ int launch_grouped_umma(tdx::GroupedParams p, const tdx_host::Device& dev, cudaS
     const int depth = PASS == tdx::kGroupedForward ? p.K : p.N;
     const int64_t rows_each = ceil_div(p.rows, p.experts);
     if (PASS == tdx::kGroupedDw) {
+        // Few rows are a short reduction, and the time is that of writing dw: tiles of 128 x 256, whose accumulators fit twice (40 rows
+        // an expert, 32 x 2048 x 2048: 78 us instead of 98; 512 rows, 16 x 4096 x 2048: 151 instead of 154; 2048 rows: 438 instead of 407).
         p.bt = p.K > 128 ? 256 : 128;
-        p.halves = p.N > 128 ? 2 : 1;
+        p.halves = p.N > 128 && rows_each > 512 ? 2 : 1;
     } else {
+        // as wide as an expert's rows: 8 x 2048 rows, 4096 x 4096: 256 x 256 379 us, 128 x 256 405, 256 x 128 464, 128 x 128 610; 16 x 100
+        // rows all within a few per cent, up to 16 rows 128 x 32
         p.bt = rows_each <= 16 ? 32 : rows_each <= 48 ? 64 : rows_each <= 128 ? 128 : 256;
         p.halves = p.bt >= 128 && p.features > 128 ? 2 : 1;
     }
@@ -83,7 +88,7 @@ int launch_grouped_umma(tdx::GroupedParams p, const tdx_host::Device& dev, cudaS
     p.tmem_cols = 32;
     while (p.tmem_cols < p.buffers * p.halves * p.bt) p.tmem_cols *= 2;
     const int stage = p.halves * 16384 + p.bt * 128;
-    const size_t fixed = 1024 + tdx::kGroupedStaging + sizeof(int) * (p.experts + 1);
+    const size_t fixed = 1024 + tdx::kGroupedStaging + sizeof(int) * 2 * (p.experts + 1);
     const int room = dev.smem_optin - 1024;                       // barriers are static
     p.stages = static_cast<int>(std::min<int64_t>(tdx::kGroupedMostStages, (room - static_cast<int64_t>(fixed)) / stage));
     const uint64_t K = p.K, N = p.N, rows = p.rows, E = p.experts;
@@ -99,7 +104,7 @@ int launch_grouped_umma(tdx::GroupedParams p, const tdx_host::Device& dev, cudaS
         TDX_TRY(tdx_host::bf16_map(p.b, 3, dw, sw, box_w, &a));
         TDX_TRY(tdx_host::bf16_map(p.a, 2, dx, sx, box_x, &b));
     }
-    const int64_t items = PASS == tdx::kGroupedDw ? E * p.feature_tiles * static_cast<int64_t>(p.column_tiles) : (p.rows / p.bt + p.experts) * p.feature_tiles;
+    const int64_t items = PASS == tdx::kGroupedDw ? E * p.feature_tiles * static_cast<int64_t>(p.column_tiles) : (p.rows / p.bt + p.experts) * static_cast<int64_t>(p.feature_tiles);
     const size_t smem = fixed + static_cast<size_t>(p.stages) * stage;
     static std::atomic<bool> known[64];
     TDX_TRY(allow_smem(tdx::grouped_umma_kernel<PASS>, known, smem, room));
@@ -116,7 +121,7 @@ int run_grouped(const tdx_grouped_args* args, void* stream) {
     p.status = dev.status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (grouped_fast(*args, p, PASS)) return launch_grouped_umma<PASS>(p, dev, st);
-    return args->dtype == TDX_F32 ? launch_grouped_rows<float, PASS>(p, st) : launch_grouped_rows<__nv_bfloat16, PASS>(p, st);
+    return args->dtype == TDX_F32 ? launch_grouped_rows<float, PASS>(p, dev.sm_count, st) : launch_grouped_rows<__nv_bfloat16, PASS>(p, dev.sm_count, st);
 }
 
 }  // namespace

@@ -37,13 +37,14 @@ struct GroupedParams {
 __device__ __forceinline__ SeqRange grouped_range(const GroupedParams& p, int e) { return seq_range(p.offsets, e, p.rows, p.rows, p.status); }
 
 // ---------------------------------------------------------------- CUDA cores
-constexpr int kSimtN = 128, kSimtK = 16;
+constexpr int kSimtK = 16;
 
-// One (8 BM / 64 x 8 a thread) tile of BM x 128 outputs, 16 of the reduction at a time through shared memory; the next 16 are on their
-// way while these are multiplied.  BM = 16 serves experts of few rows, where a tile of 64 would be mostly empty.
-template <typename T, int PASS, int BM>
+// One tile of BM x BN outputs (BM / 8 x BN / 16 a thread), 16 of the reduction at a time through shared memory; the next 16 are on their
+// way while these are multiplied.  BM = 16 serves experts of few rows, where a tile of 64 would be mostly empty; BN = 64 products whose
+// tiles of 128 would leave SMs with a block or two (1501 x 1000 x 520 in five experts, forward and gradients: 266 -> 178 us).
+template <typename T, int PASS, int BM, int BN>
 __global__ void __launch_bounds__(128) grouped_simt_kernel(const __grid_constant__ GroupedParams p) {
-    constexpr int TM = BM / 8;                                    // rows a thread
+    constexpr int TM = BM / 8, TN = BN / 16, kSimtN = BN;         // rows and columns a thread
     __shared__ __align__(16) float sa[2][kSimtK][BM + 4];
     __shared__ __align__(16) float sb[2][kSimtK][kSimtN + 4];
     const T* a = static_cast<const T*>(p.a);
@@ -105,12 +106,12 @@ __global__ void __launch_bounds__(128) grouped_simt_kernel(const __grid_constant
             sb[buf][kBDeep ? at % kSimtK : at / kSimtN][kBDeep ? at / kSimtK : at % kSimtN] = rb[i];
         }
     };
-    float acc[TM][8];
+    float acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[i][j] = 0.0f;
-    const int tm = tid / 16 * TM, tn = tid % 16 * 4;              // columns tn .. tn + 3 and 64 + tn .. : no bank conflicts
+        for (int j = 0; j < TN; ++j) acc[i][j] = 0.0f;
+    const int tm = tid / 16 * TM, tn = tid % 16 * 4;              // columns tn .. tn + 3 (and 64 + tn ..): no bank conflicts
     fetch(0);
     put(0);
     __syncthreads();
@@ -120,15 +121,15 @@ __global__ void __launch_bounds__(128) grouped_simt_kernel(const __grid_constant
         if (more) fetch(k0 + kSimtK);
 #pragma unroll
         for (int k = 0; k < kSimtK; ++k) {
-            float fa[TM], fb[8];
+            float fa[TM], fb[TN];
 #pragma unroll
             for (int i = 0; i < TM; ++i) fa[i] = sa[buf][k][tm + i];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { fb[j] = sb[buf][k][tn + j]; fb[4 + j] = sb[buf][k][64 + tn + j]; }
+            for (int j = 0; j < TN; ++j) fb[j] = sb[buf][k][j < 4 ? tn + j : 60 + tn + j];
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(fa[i], fb[j], acc[i][j]);
+                for (int j = 0; j < TN; ++j) acc[i][j] = fmaf(fa[i], fb[j], acc[i][j]);
         }
         if (more) put(buf ^ 1);
         __syncthreads();
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(128) grouped_simt_kernel(const __grid_constant
         if (m0 + tm + i >= m_count) break;
         T* row = out + (m0 + tm + i) * ld_out;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < TN; ++j) {
             const int n = n0 + tn + (j < 4 ? j : 60 + j);
             if (n < n_count) row[n] = seq_from_float<T>(acc[i][j]);
         }
@@ -154,6 +155,7 @@ __global__ void __launch_bounds__(128) grouped_simt_kernel(const __grid_constant
 // dw sums over an expert's rows: both operands are read with the rows as the reduction, and rows of the last block that belong to the
 // next expert are set to zero in shared memory in front of the product (a factor of zero in one operand would leave NaN and infinity).
 constexpr int kGroupedMostExperts = 1024;                        // whose tile counts are kept in shared memory
+constexpr int kGroupedSorted = 128;                              // experts that dw sorts by their rows, each against all others
 constexpr int kGroupedThreads = 320;
 constexpr int kGroupedEpilogueWarps = 8;
 constexpr int kGroupedStagePitch = 80;                           // bytes of a staged row of 32 bf16
@@ -167,13 +169,25 @@ struct GroupedTile {
     int blocks;                      // of 64 of the reduction
 };
 
+// The last entry of an ascending table that is at most `v`.
+__device__ __forceinline__ int grouped_search(const int* table, int count, int v) {
+    int lo = 0, hi = count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (table[mid] <= v) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+// `first`: forward and dx: whole tiles of rows of the experts in front of each, added up, and behind them the same for tiles with rows
+// left over; dw: the experts, most rows first.
 template <int PASS>
 __device__ __forceinline__ bool grouped_tile(const GroupedParams& p, const int* first, long long item, GroupedTile* t) {
     if (PASS == kGroupedDw) {
         const int per = p.feature_tiles * p.column_tiles;
         if (item >= static_cast<long long>(per) * p.experts) return false;
-        t->expert = static_cast<int>(item / per);
-        const int in = static_cast<int>(item - static_cast<long long>(t->expert) * per);
+        const int place = static_cast<int>(item / per), in = static_cast<int>(item - static_cast<long long>(place) * per);
+        t->expert = first[place];
         t->feature = in / p.column_tiles * (128 * p.halves);
         t->column = in % p.column_tiles * p.bt;
         const int lo = __ldg(p.offsets + t->expert), hi = __ldg(p.offsets + t->expert + 1);
@@ -182,19 +196,27 @@ __device__ __forceinline__ bool grouped_tile(const GroupedParams& p, const int* 
         t->blocks = (t->count + 63) / 64;
         return true;
     }
-    if (item >= static_cast<long long>(first[p.experts]) * p.feature_tiles) return false;
-    const int number = static_cast<int>(item / p.feature_tiles);
-    int lo = 0, hi = p.experts - 1;                              // the last expert whose tiles start at or before `number`
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (first[mid] <= number) lo = mid;
-        else hi = mid - 1;
+    // Whole tiles come first and those with what is left of an expert's rows behind them, so that the last round, which not all
+    // blocks have a tile for, is one of small tiles.  An expert's tiles of rows lie side by side for each tile of features, so that
+    // its weights are read together.
+    const int* rest = first + p.experts + 1;
+    const long long whole = static_cast<long long>(first[p.experts]) * p.feature_tiles;
+    int e, f, r;
+    if (item < whole) {
+        e = grouped_search(first, p.experts, static_cast<int>(item / p.feature_tiles));
+        const int tiles = first[e + 1] - first[e], in = static_cast<int>(item - static_cast<long long>(first[e]) * p.feature_tiles);
+        f = in / tiles;
+        r = in - f * tiles;
+    } else {
+        const long long behind = item - whole;
+        if (behind >= static_cast<long long>(rest[p.experts]) * p.feature_tiles) return false;
+        const int number = static_cast<int>(behind / p.feature_tiles);
+        e = grouped_search(rest, p.experts, number);
+        f = static_cast<int>(behind - static_cast<long long>(number) * p.feature_tiles);
+        r = first[e + 1] - first[e];
     }
-    // an expert's tiles of rows lie side by side for each tile of features, so that its weights are read together
-    const int tiles = first[lo + 1] - first[lo];
-    const int in = static_cast<int>(item - static_cast<long long>(first[lo]) * p.feature_tiles), f = in / tiles, r = in - f * tiles;
-    const int from = __ldg(p.offsets + lo), to = __ldg(p.offsets + lo + 1);
-    t->expert = lo;
+    const int from = __ldg(p.offsets + e), to = __ldg(p.offsets + e + 1);
+    t->expert = e;
     t->row = from + static_cast<long long>(r) * p.bt;
     t->count = min(p.bt, to - from - r * p.bt);
     t->feature = f * (128 * p.halves);
@@ -237,19 +259,37 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
     }
     ptx::grid_dependency_wait();
     if (warp == 0) {
-        // the experts' numbers of tiles, added up
-        int sum = 0;
-        if (lane == 0) first[0] = 0;
-        for (int e0 = 0; e0 < p.experts; e0 += 32) {
-            const int e = e0 + lane;
-            int n = e < p.experts ? (grouped_range(p, e).len + p.bt - 1) / p.bt : 0;
-#pragma unroll
-            for (int d = 1; d < 32; d *= 2) {
-                const int up = __shfl_up_sync(0xffffffffu, n, d);
-                if (lane >= d) n += up;
+        if (PASS == kGroupedDw) {
+            for (int e = lane; e < p.experts; e += 32) {
+                const int n = grouped_range(p, e).len;
+                int place = e;
+                if (p.experts <= kGroupedSorted) {
+                    place = 0;
+                    for (int o = 0; o < p.experts; ++o) {
+                        const int lo = __ldg(p.offsets + o), hi = __ldg(p.offsets + o + 1), m = seq_accepted(lo, hi, p.rows, p.rows) ? hi - lo : 0;
+                        place += m > n || (m == n && o < e);
+                    }
+                }
+                first[place] = e;
             }
-            if (e < p.experts) first[e + 1] = sum + n;
-            sum += __shfl_sync(0xffffffffu, n, 31);
+        } else {
+            int whole = 0, rest = 0;
+            if (lane == 0) first[0] = first[p.experts + 1] = 0;
+            for (int e0 = 0; e0 < p.experts; e0 += 32) {
+                const int e = e0 + lane, n = e < p.experts ? grouped_range(p, e).len : 0;
+                int w = n / p.bt, l = n % p.bt > 0;
+#pragma unroll
+                for (int d = 1; d < 32; d *= 2) {
+                    const int up = __shfl_up_sync(0xffffffffu, w, d), more = __shfl_up_sync(0xffffffffu, l, d);
+                    if (lane >= d) { w += up; l += more; }
+                }
+                if (e < p.experts) {
+                    first[e + 1] = whole + w;
+                    first[p.experts + 2 + e] = rest + l;
+                }
+                whole += __shfl_sync(0xffffffffu, w, 31);
+                rest += __shfl_sync(0xffffffffu, l, 31);
+            }
         }
     }
     ptx::tc_fence_before_sync();
@@ -367,9 +407,10 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
             ptx::tc_fence_after_sync();
             const int feature = t.feature + half * 128 + quarter * 32;
             const int columns = PASS == kGroupedDw ? min(p.bt, p.K - t.column) : t.count;
+            const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>((buf * p.halves + half) * p.bt);
+            uint32_t r[32];
+            if (c_first < columns) ptx::tmem_ld_32x32b_x32(from + c_first, r);
             for (int c0 = c_first; c0 < columns; c0 += c_step) {
-                uint32_t r[32];
-                ptx::tmem_ld_32x32b_x32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>((buf * p.halves + half) * p.bt + c0), r);
                 ptx::tmem_ld_wait();
                 if (PASS == kGroupedDw) {
                     uint32_t pk[16];
@@ -387,6 +428,8 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
                     for (int j = 0; j < 32; ++j)
                         *reinterpret_cast<__nv_bfloat16*>(mine + j * kGroupedStagePitch + lane * 2) = __float2bfloat16_rn(__uint_as_float(r[j]));
                 }
+                // the next columns are on their way while these are written
+                if (c0 + c_step < columns) ptx::tmem_ld_32x32b_x32(from + c0 + c_step, r);
                 __syncwarp();
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
