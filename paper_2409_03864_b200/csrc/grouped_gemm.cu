@@ -92,23 +92,29 @@ int launch_grouped_umma(tdx::GroupedParams p, const tdx_host::Device& dev, cudaS
     const int room = dev.smem_optin - 1024;                       // barriers are static
     p.stages = static_cast<int>(std::min<int64_t>(tdx::kGroupedMostStages, (room - static_cast<int64_t>(fixed)) / stage));
     const uint64_t K = p.K, N = p.N, rows = p.rows, E = p.experts;
-    CUtensorMap a, b;
+    CUtensorMap a, b, out;
     if (PASS == tdx::kGroupedDw) {
         const uint64_t da[2] = {N, rows}, sa[1] = {static_cast<uint64_t>(p.ld_a) * 2}, db[2] = {K, rows}, sb[1] = {static_cast<uint64_t>(p.ld_b) * 2};
         const uint32_t box[2] = {64, 64};
         TDX_TRY(tdx_host::bf16_map(p.a, 2, da, sa, box, &a));
         TDX_TRY(tdx_host::bf16_map(p.b, 2, db, sb, box, &b));
+        const uint64_t dw[3] = {K, N, E}, sw[2] = {K * 2, K * N * 2};
+        const uint32_t box_out[3] = {32, 32, 1};
+        TDX_TRY(tdx_host::bf16_map(p.out, 3, dw, sw, box_out, &out, 64));
     } else {
         const uint64_t dw[3] = {K, N, E}, sw[2] = {K * 2, K * N * 2}, dx[2] = {static_cast<uint64_t>(depth), rows}, sx[1] = {static_cast<uint64_t>(p.ld_a) * 2};
         const uint32_t box_w[3] = {64, PASS == tdx::kGroupedForward ? 128u : 64u, 1}, box_x[2] = {64, static_cast<uint32_t>(p.box)};
         TDX_TRY(tdx_host::bf16_map(p.b, 3, dw, sw, box_w, &a));
         TDX_TRY(tdx_host::bf16_map(p.a, 2, dx, sx, box_x, &b));
+        const uint64_t dy[2] = {static_cast<uint64_t>(p.features), rows}, sy[1] = {static_cast<uint64_t>(p.ld_out) * 2};
+        const uint32_t box_y[2] = {32, 16};
+        TDX_TRY(tdx_host::bf16_map(p.out, 2, dy, sy, box_y, &out, 64));
     }
     const int64_t items = PASS == tdx::kGroupedDw ? E * p.feature_tiles * static_cast<int64_t>(p.column_tiles) : (p.rows / p.bt + p.experts) * static_cast<int64_t>(p.feature_tiles);
     const size_t smem = fixed + static_cast<size_t>(p.stages) * stage;
     static std::atomic<bool> known[64];
     TDX_TRY(allow_smem(tdx::grouped_umma_kernel<PASS>, known, smem, room));
-    return launch_seq(tdx::grouped_umma_kernel<PASS>, std::min<int64_t>(items, dev.sm_count), 1, tdx::kGroupedThreads, smem, st, a, b, p);
+    return launch_seq(tdx::grouped_umma_kernel<PASS>, std::min<int64_t>(items, dev.sm_count), 1, tdx::kGroupedThreads, smem, st, a, b, out, p);
 }
 
 template <int PASS>

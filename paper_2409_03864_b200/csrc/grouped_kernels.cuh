@@ -159,7 +159,8 @@ constexpr int kGroupedSorted = 128;                              // experts that
 constexpr int kGroupedThreads = 320;
 constexpr int kGroupedEpilogueWarps = 8;
 constexpr int kGroupedStagePitch = 80;                           // bytes of a staged row of 32 bf16
-constexpr int kGroupedStaging = kGroupedEpilogueWarps * 32 * kGroupedStagePitch;
+constexpr int kGroupedStageWarp = 3072;                          // a warp's part: 32 such rows, or 2 KB for the copy engine
+constexpr int kGroupedStaging = kGroupedEpilogueWarps * kGroupedStageWarp;
 constexpr int kGroupedMostStages = 10;
 
 struct GroupedTile {
@@ -227,6 +228,7 @@ __device__ __forceinline__ bool grouped_tile(const GroupedParams& p, const int* 
 
 template <int PASS>
 __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
+                                                                          const __grid_constant__ CUtensorMap tm_out,
                                                                           const __grid_constant__ GroupedParams p) {
     extern __shared__ uint8_t grouped_smem[];
     __shared__ __align__(8) uint64_t full_bar[kGroupedMostStages], empty_bar[kGroupedMostStages], tfull_bar[2], tempty_bar[2];
@@ -252,6 +254,7 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
         ptx::fence_barrier_init();
         ptx::tma_prefetch_desc(&tm_a);
         ptx::tma_prefetch_desc(&tm_b);
+        ptx::tma_prefetch_desc(&tm_out);
     }
     if (warp == 1) {
         ptx::tmem_alloc(&s_tmem, static_cast<uint32_t>(p.tmem_cols));
@@ -397,7 +400,7 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
     } else {
         const int ew = warp - 2, quarter = warp & 3, half = p.halves == 2 ? ew >> 2 : 0;
         const int c_first = p.halves == 2 ? 0 : (ew >> 2) * 32, c_step = p.halves == 2 ? 32 : 64;
-        uint8_t* const mine = staging + ew * 32 * kGroupedStagePitch;
+        uint8_t* const mine = staging + ew * kGroupedStageWarp;
         __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out);
         int local = 0;
         GroupedTile t;
@@ -412,6 +415,37 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
             if (c_first < columns) ptx::tmem_ld_32x32b_x32(from + c_first, r);
             for (int c0 = c_first; c0 < columns; c0 += c_step) {
                 ptx::tmem_ld_wait();
+                if (PASS != kGroupedDw && t.count == p.bt) {
+                    // A whole tile leaves through the copy engine in blocks of 16 rows x 32 features (64-byte swizzle), two of them taking turns: stores
+                    // from registers took 13 of the 124 us of 16 x 512 rows, 4096 x 2048, and the accumulators wait for them.  (It would also
+                    // write the rows behind a tile that is not whole.)
+                    uint32_t half_pairs[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+                        half_pairs[j] = *reinterpret_cast<uint32_t*>(&h);
+                    }
+                    if (c0 + c_step < columns) ptx::tmem_ld_32x32b_x32(from + c0 + c_step, r);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        if (lane == 0) ptx::tma_store_wait_read<1>();
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const uint32_t pair = half_pairs[b * 8 + j / 2];
+                            *reinterpret_cast<uint16_t*>(mine + b * 1024 + j * 64 + (((lane >> 3) ^ (j >> 1 & 3)) << 4) + (lane & 7) * 2) = static_cast<uint16_t>(j & 1 ? pair >> 16 : pair);
+                        }
+                        ptx::fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0 && feature < p.features) {
+                            ptx::tma_store_2d(&tm_out, mine + b * 1024, feature, static_cast<int>(t.row) + c0 + b * 16);
+                            ptx::tma_store_commit();
+                        }
+                    }
+                    continue;
+                }
+                if (PASS != kGroupedDw && lane == 0) ptx::tma_store_wait_read<0>();   // of a whole tile in front of this one
+                __syncwarp();
                 if (PASS == kGroupedDw) {
                     uint32_t pk[16];
 #pragma unroll
@@ -419,9 +453,19 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
                         __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
                         pk[j] = t.blocks > 0 ? *reinterpret_cast<uint32_t*>(&h) : 0u;     // an expert without rows
                     }
+                    if (c0 + c_step < columns) ptx::tmem_ld_32x32b_x32(from + c0 + c_step, r);
+                    if (lane == 0) ptx::tma_store_wait_read<0>();
+                    __syncwarp();
 #pragma unroll
                     for (int g = 0; g < 4; ++g)
-                        *reinterpret_cast<uint4*>(mine + lane * kGroupedStagePitch + g * 16) = make_uint4(pk[4 * g], pk[4 * g + 1], pk[4 * g + 2], pk[4 * g + 3]);
+                        *reinterpret_cast<uint4*>(mine + lane * 64 + ((g ^ (lane >> 1 & 3)) << 4)) = make_uint4(pk[4 * g], pk[4 * g + 1], pk[4 * g + 2], pk[4 * g + 3]);
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0 && feature < p.N) {
+                        ptx::tma_store_3d(&tm_out, mine, t.column + c0, feature, t.expert);
+                        ptx::tma_store_commit();
+                    }
+                    continue;
                 } else {
                     // a lane has a feature, an output row wants them side by side
 #pragma unroll
@@ -435,13 +479,8 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
                 for (int i = 0; i < 4; ++i) {
                     const int row = lane / 4 + i * 8, part = lane % 4 * 8;
                     const uint4 v = *reinterpret_cast<const uint4*>(mine + row * kGroupedStagePitch + part * 2);
-                    if (PASS == kGroupedDw) {
-                        const int column = t.column + c0 + part;
-                        if (feature + row < p.N && column < p.K)
-                            *reinterpret_cast<uint4*>(out + (static_cast<long long>(t.expert) * p.N + feature + row) * p.K + column) = v;
-                    } else if (c0 + row < t.count && feature + part < p.features) {
+                    if (c0 + row < t.count && feature + part < p.features)
                         *reinterpret_cast<uint4*>(out + (t.row + c0 + row) * p.ld_out + feature + part) = v;
-                    }
                 }
                 __syncwarp();
             }
@@ -449,6 +488,7 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&tempty_bar[buf]);
         }
+        if (lane == 0) ptx::tma_store_wait_all<0>();             // shared memory stays until it has been read
     }
     ptx::tc_fence_before_sync();
     __syncthreads();

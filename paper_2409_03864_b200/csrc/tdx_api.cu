@@ -1917,9 +1917,9 @@ int get_device(Device* out) {
     out->status = ctx->status_ptr;
     return TDX_OK;
 }
-int bf16_map(const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides_bytes, const uint32_t* box, CUtensorMap* out) {
+int bf16_map(const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides_bytes, const uint32_t* box, CUtensorMap* out, int swizzle_bytes) {
     DeviceCtx* ctx;
     TDX_TRY(get_ctx(&ctx));
-    return get_tensor_map(ctx, ptr, rank, dims, strides_bytes, box, out);
+    return get_tensor_map(ctx, ptr, rank, dims, strides_bytes, box, out, swizzle_bytes);
 }
 }  // namespace tdx_host
