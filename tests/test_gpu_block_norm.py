@@ -190,3 +190,15 @@ def test_captured_and_replayed_on_another_stream():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(again, dw) and bool(torch.isfinite(dw).all())
+
+
+def test_workspace_refusals():
+    c = Case("bf16", 5, 128)
+    out = {"d" + k: c.rows_of(np.zeros((5, 128)), fill=-5.0) for k in ("x", "gate", "residual")}
+    a = c.args(dy=c.rows_of(np.zeros((5, 128))), **out)
+    ws = workspace(tdx.tdx_block_norm_workspace_size(a))
+    for change, status in ((dict(workspace=None, workspace_bytes=1 << 30), tdx.TDX_ERR_WORKSPACE), (dict(workspace=ws, workspace_bytes=ws.numel() - 1), tdx.TDX_ERR_WORKSPACE),
+                           (dict(workspace=ws.data_ptr() + 16, workspace_bytes=1 << 30), tdx.TDX_ERR_ALIGNMENT)):
+        assert tdx.tdx_block_norm_bwd(a.set(**change)) == status
+    torch.cuda.synchronize()
+    assert all((v.host() == -5.0).all() for v in out.values())

@@ -276,3 +276,16 @@ def test_captured_and_replayed():
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(x, v.full) for x, v in zip(first, (out, *g.values())))
+
+
+def test_workspace_refusals():
+    c = Case("bf16", [1100], 1, 64, 64)
+    out = c.rows_of(np.zeros((1100, 1, 64)), fill=-5.0)
+    a = c.args(out=out, state_in=c.cache, state_out=c.slots_of())
+    ws = c.keep[-1]
+    assert ws.numel() > 0
+    for change, status in ((dict(workspace=None, workspace_bytes=1 << 30), tdx.TDX_ERR_WORKSPACE), (dict(workspace=ws, workspace_bytes=ws.numel() // 2 - 1), tdx.TDX_ERR_WORKSPACE),
+                           (dict(workspace=ws.data_ptr() + 16, workspace_bytes=1 << 30), tdx.TDX_ERR_ALIGNMENT)):
+        assert tdx.tdx_decay_attention(a.set(**change)) == status, change
+    torch.cuda.synchronize()
+    assert (out.host() == -5.0).all()
