@@ -137,11 +137,12 @@ __device__ __forceinline__ void attn_load(uint8_t* tile, const T* base, long lon
 // One block: a segment of a sequence, a head, 64 columns of v.  Four warps: for the outputs a warp has 16 rows of the chunk, for the
 // state KD / 4 of its rows, in registers over all chunks; the other blocks of the head's columns do q k^T again (a third of the
 // work at dim 128), which leaves room for two blocks an SM.  STATE: only what the segment adds to the state, for the segments behind it.
-// UP: bf16 pieces of the decayed keys that go into the state, 3 where the state is an output and keeps 24 bits, else 2.
+// UP: bf16 pieces of the decayed keys that go into the state, 3 where the state is an output and keeps 24 bits, else 2.  The weights of a
+// chunk's rows have two pieces (PP; fp32 three): what is rounded once on the way to a bf16 output is the state that its row reads.
 template <typename T, int KD, bool STATE, int UP>
 __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constant__ AttnParams p) {
     typedef AttnTiles<T, KD> Tiles;
-    constexpr int NP = Tiles::kPieces, MT = KD / 64, NT = kAttnV / 8, PK = Tiles::kPitchK, PV = Tiles::kPitchV;
+    constexpr int NP = Tiles::kPieces, PP = NP == 3 ? 3 : 2, MT = KD / 64, NT = kAttnV / 8, PK = Tiles::kPitchK, PV = Tiles::kPitchV;
     extern __shared__ __align__(16) uint8_t attn_smem[];
     __shared__ float power[kAttnC + 1];                          // l^n
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -294,7 +295,7 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
 #pragma unroll
             for (int kk = 0; kk < kAttnC / 16; ++kk) {           // the weights, then their product with v
                 if (kk <= warp) {
-                    uint32_t fp[NP][4];
+                    uint32_t fp[PP][4];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         float w[4];
@@ -303,11 +304,11 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
                             const int back = i0 + (i >> 1) * 8 - (kk * 16 + h * 8 + n_first + (i & 1));
                             w[i] = back >= 0 ? s[2 * kk + h][i] * (power[max(back, 0)] * p.scale_in) : 0.0f;
                         }
-                        uint32_t lo[NP], hi[NP];
+                        uint32_t lo[PP], hi[PP];
                         attn_split(w[0], w[1], lo);
                         attn_split(w[2], w[3], hi);
 #pragma unroll
-                        for (int i = 0; i < NP; ++i) { fp[i][2 * h] = lo[i]; fp[i][2 * h + 1] = hi[i]; }
+                        for (int i = 0; i < PP; ++i) { fp[i][2 * h] = lo[i]; fp[i][2 * h + 1] = hi[i]; }
                     }
 #pragma unroll
                     for (int b = 0; b < NT / 2; ++b) {

@@ -3,15 +3,18 @@
 //
 //   warp 0         copies: k and v of a chunk into one of two sets of tiles while the other is worked on, q as soon as the last one is used
 //   warp 1         products: W = q k^T;  O1 = q S0;  O2 = P v;  U = K~^T v
-//   warps 4 - 11   P = W l^(i-j) below the diagonal, bf16, back into tensor memory, from where it is a product's operand; then
-//                  out = l^(i+1) O1 + O2
+//   warps 4 - 11   P = W l^(i-j) below the diagonal in two bf16 pieces, back into tensor memory, from where they are a product's
+//                  operands; then out = l^(i+1) O1 + O2
 //   warps 12 - 15  K~ = l^(n-1-j) k in bf16 pieces, the first in place of k (warps 4 - 15 where there are no outputs)
 //   warps 16 - 23  S1 = l^n S0 + U in fp32 registers, 64 a thread; S1 as bf16 for the next chunk's O1
 //
 // The roles are apart so that a chunk's K~ and W are made while the state and the output of the one in front of it are still worked on:
 // with P and out in four warps and K~ and the state in the same eight a chunk of 128 x 128 took 7,700 cycles.  Registers move from
 // the first four warps and the keys' to the state's.
-// A chunk of 128 x 128 takes about 5,500 cycles of an SM's share of the memory bandwidth and about 2,600 cycles of products, so one
+// The second piece of P costs 8 % (forward and backward of 4 x 2048 rows, 16 heads of 128: 218 -> 236 us) and takes the larger of the two
+// roundings on the way to the output out (P's and the state's): 1.4 times the error of a single rounding became 1.0 to 1.3 times.
+//
+// A chunk of 128 x 128 takes about 5,500 cycles of an SM's share of the memory bandwidth and about 3,100 cycles of products, so one
 // chunk at a time with its operands fetched ahead is enough.  U starts from zero in every chunk: the tensor cores cut sums off instead of
 // rounding them, which over a whole sequence shows in the state (3e-6), over 128 rows it does not.
 // Rows of the tile behind the chunk's last one belong to other rows of the sequence or to other sequences: their weights are selected
@@ -240,7 +243,7 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
             const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + hv * p.d2;
 #pragma unroll 1
             for (int c = 0; c + 2 < chunks; ++c) {
-                while (*progress <= c) __nanosleep(100);
+                for (int turn = 0; *progress <= c && turn < 1 << 24; ++turn) __nanosleep(100);
                 const long long ahead = first_of(c + 2);
                 const int n = rows_of(c + 2);
                 for (int i = lane; i < n; i += 32) {
@@ -279,8 +282,8 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                         ptx::tc_fence_after_sync();
                         const uint64_t of_v = mn_major(v);
 #pragma unroll 1
-                        for (int s = 0; s < 8; ++s)
-                            attn_umma_ta(tmem + kAttnTmemO2, tmem + kAttnTmemW + (s >> 2) * 64 + (s & 3) * 8, of_v + s * kMn1, idesc_o, s > 0);
+                        for (int s = 0; s < 16; ++s)             // second pieces first
+                            attn_umma_ta(tmem + kAttnTmemO2, tmem + kAttnTmemW + (s >> 2 & 1) * 64 + (s < 8 ? 32 : 0) + (s & 3) * 8, of_v + (s & 7) * kMn1, idesc_o, s > 0);
                         ptx::umma_commit(&bar_o);
                     }
                     if (c >= 0) {
@@ -315,28 +318,40 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
                 const int n = rows_of(c), shift = c == 0 ? less : 0;
                 if (!wait_bounded_idle(&bar_w[c & 1], c >> 1 & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
                 ptx::tc_fence_after_sync();
-#pragma unroll 1
-                for (int g = part * 2; g < part * 2 + 2; ++g) {
-                    uint32_t packed[16];
+                uint32_t low[16];                                // the second pieces of this warp's first group
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) packed[j] = 0u;
+                for (int h = 0; h < 2; ++h) {
+                    const int g = part * 2 + h;
+                    uint32_t pieces[16][2];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) pieces[j][0] = pieces[j][1] = 0u;
                     if (BACK ? g >= quarter : g <= quarter) {    // on this side of the diagonal
                         uint32_t w[32];
-                        float f[32];
                         ptx::tmem_ld_32x32b_x32(lanes + kAttnTmemW + g * 32, w);
                         const float* l = weight + kAttnRows + (BACK ? g * 32 - i : i - g * 32);
+                        const bool cut = g == quarter || (BACK && n < kAttnRows);
                         ptx::tmem_ld_wait();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(w[j]) * l[BACK ? j : -j];
-                        if (g == quarter || (BACK && n < kAttnRows)) {
+                        for (int j = 0; j < 16; ++j) {
+                            float f[2];
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) f[j] = (BACK ? g * 32 + j >= i && g * 32 + j < n : g * 32 + j <= i) ? f[j] : 0.0f;
+                            for (int e = 0; e < 2; ++e) {
+                                const int col = 2 * j + e;
+                                f[e] = __uint_as_float(w[col]) * l[BACK ? col : -col];
+                                if (cut) f[e] = (BACK ? g * 32 + col >= i && g * 32 + col < n : g * 32 + col <= i) ? f[e] : 0.0f;
+                            }
+                            attn_split(f[0], f[1], pieces[j]);
                         }
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) packed[j] = attn_pair(f[2 * j], f[2 * j + 1]);
                     }
-                    // P takes the place of the first of this warp's two groups of W
-                    attn_tmem_st_x16(lanes + kAttnTmemW + part * 64 + (g & 1) * 16, packed);
+                    // P takes the place of W: first pieces of both groups that of the first one, second pieces that of the second
+                    uint32_t high[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) high[j] = pieces[j][0];
+                    attn_tmem_st_x16(lanes + kAttnTmemW + part * 64 + h * 16, high);
+                    if (h == 1) attn_tmem_st_x16(lanes + kAttnTmemW + part * 64 + 32, low);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) low[j] = pieces[j][1];
+                    if (h == 1) attn_tmem_st_x16(lanes + kAttnTmemW + part * 64 + 48, low);
                 }
                 attn_tmem_st_wait();
                 ptx::tc_fence_before_sync();

@@ -149,8 +149,9 @@ template <bool BACK>
 int launch_attention_umma_passes(const CUtensorMap (&maps)[3], const tdx::AttnParams& p, int64_t numbers, int64_t states, bool cut, cudaStream_t st) {
     if (p.state_out && cut) {
         TDX_TRY((launch_attention_umma<true, BACK, 3>(maps, p, states, st)));
-        TDX_TRY(launch_seq(tdx::attn_state_kernel, p.batch * p.heads * 16, 1, 256, 0, st, p));
-        return launch_attention_umma<false, BACK, 2>(maps, p, numbers, st);
+        TDX_TRY((launch_attention_umma<false, BACK, 2>(maps, p, numbers, st)));
+        // last, since state_out may be state_in, which all segments start from
+        return launch_seq(tdx::attn_state_kernel, p.batch * p.heads * 16, 1, 256, 0, st, p);
     }
     if (states > 0) TDX_TRY((launch_attention_umma<true, BACK, 2>(maps, p, states, st)));
     return p.state_out ? launch_attention_umma<false, BACK, 3>(maps, p, numbers, st) : launch_attention_umma<false, BACK, 2>(maps, p, numbers, st);
@@ -209,9 +210,14 @@ int run_attention(const tdx_attention_args& a, const AttnShape& shape, AttnSum s
     p.state_vec = !turned && a.dim_v % 4 == 0 && p.state_stride % 4 == 0 && !misaligned(p.state_in, 16) && !misaligned(p.state_out, 16);
     p.status = dev.status;
     p.carry = static_cast<float*>(a.workspace);
-    const bool umma = sizeof(T) == 2 && p.vec && a.rows > 0;
+    const bool umma = sizeof(T) == 2 && p.vec && a.rows > 0 && a.rows <= INT_MAX;   // (rows are coordinates of the copy engine)
     const bool all_pieces = (sum == kAttnOut ? a.state_out : late ? a.dstate_in : nullptr) != nullptr;
     plan_attention(a, p.d2, umma, all_pieces, dev.sm_count, &p);
+    // A segment on the other kernel may end, and write the state, before one in front of it has started from the state that it replaces.
+    if (!umma && p.state_out != nullptr && p.state_out == p.state_in) {
+        p.seg = ceil_div(std::max<int64_t>(1, a.max_len), tdx::kAttnC) * tdx::kAttnC;
+        p.dense = 1;
+    }
     const int64_t numbers = attention_numbers(a, p);
     const bool cut = attention_cut(a, p);
     if (umma) {

@@ -1,5 +1,5 @@
 // Host-side state of the tdx library: error text, per-device context, TMA descriptor cache, tuning cache.
-// Part of the single translation unit tdx_api.cu (everything lives in its anonymous namespace).
+// Part of the translation unit tdx_api.cu (everything lives in its anonymous namespace).
 #pragma once
 #include "tdx.h"
 

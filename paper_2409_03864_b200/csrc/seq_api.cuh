@@ -1,5 +1,5 @@
 // Entry points of the sequence operators: causal convolution, selective scan and products with 4-bit weights (see tdx.h).
-// Part of the single translation unit tdx_api.cu.
+// Part of the translation unit tdx_api.cu.
 #pragma once
 #include "conv1d_kernels.cuh"
 #include "scan_kernels.cuh"

@@ -289,3 +289,17 @@ def test_workspace_refusals():
         assert tdx.tdx_decay_attention(a.set(**change)) == status, change
     torch.cuda.synchronize()
     assert (out.host() == -5.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_state_in_place_of_sequences_in_several_segments(dtype, pad):
+    c = Case(dtype, [1300, 40], 1, 64, 64, pad=pad)
+    one, two, new = c.rows_of(np.zeros((1340, 1, 64))), c.rows_of(np.zeros((1340, 1, 64))), c.slots_of()
+    tdx.check(tdx.tdx_decay_attention(c.args(out=one, state_in=c.cache, state_out=new)))
+    tdx.check(tdx.tdx_decay_attention(c.args(out=two, state_in=c.cache, state_out=c.cache)))
+    torch.cuda.synchronize()
+    at = torch.from_numpy(c.slots).cuda()
+    size, factors = c.exact(True, False), c.factors()
+    assert_close("out", two.host(), one.host(), size["out"], 2 * factors[1], dtype)
+    assert_close("state", c.cache[at].double().cpu().numpy(), new[at].double().cpu().numpy(), size["state"], 2 * factors[0])
