@@ -39,29 +39,33 @@ int check_grouped(const tdx_grouped_args* args, tdx::GroupedPass pass, tdx::Grou
     return TDX_OK;
 }
 
-template <typename T, int PASS, int BM, int BN>
-int launch_grouped_simt(const tdx::GroupedParams& p, int64_t tiles_m, cudaStream_t st) {
-    return launch_seq(tdx::grouped_simt_kernel<T, PASS, BM, BN>, tiles_m * ceil_div(PASS == tdx::kGroupedForward ? p.N : p.K, BN), 1, 128, 0, st, p);
+template <typename T, int PASS, int BM, int VEC>
+int launch_grouped_simt(const tdx::GroupedParams& p, cudaStream_t st) {
+    const int64_t tiles_m = PASS == tdx::kGroupedDw ? p.experts * ceil_div(p.N, BM) : tdx::seq_pieces(true, p.experts, p.rows, 0, BM);
+    return launch_seq(tdx::grouped_simt_kernel<T, PASS, BM, VEC>, tiles_m * ceil_div(PASS == tdx::kGroupedForward ? p.N : p.K, tdx::kSimtColumns), 1, tdx::kSimtThreads, 0, st, p);
 }
-template <typename T, int PASS>
-int launch_grouped_rows(const tdx::GroupedParams& p, int sm_count, cudaStream_t st) {
-    auto tiles = [&](int64_t bm) { return PASS == tdx::kGroupedDw ? p.experts * ceil_div(p.N, bm) : tdx::seq_pieces(true, p.experts, p.rows, 0, bm); };
-    if (p.rows <= 16 * static_cast<int64_t>(p.experts) && PASS != tdx::kGroupedDw) return launch_grouped_simt<T, PASS, 16, 128>(p, tiles(16), st);
-    const int64_t wide = tiles(64) * ceil_div(PASS == tdx::kGroupedForward ? p.N : p.K, 128);
-    return wide < 4 * sm_count ? launch_grouped_simt<T, PASS, 64, 64>(p, tiles(64), st) : launch_grouped_simt<T, PASS, 64, 128>(p, tiles(64), st);
+template <typename T, int PASS, int VEC>
+int launch_grouped_rows(const tdx::GroupedParams& p, cudaStream_t st) {
+    if constexpr (PASS != tdx::kGroupedDw)
+        if (p.rows <= 16 * static_cast<int64_t>(p.experts)) return launch_grouped_simt<T, PASS, 16, VEC>(p, st);
+    return launch_grouped_simt<T, PASS, 64, VEC>(p, st);
 }
 
-// The tensor-core kernel reads operands by the copy engine and writes 16 bytes at a time.
-bool grouped_fast(const tdx_grouped_args& a, const tdx::GroupedParams& p, int pass) {
-    if (a.dtype != TDX_BF16 || a.rows == 0 || a.N == 0 || a.K == 0 || a.experts > tdx::kGroupedMostExperts) return false;
+// Every row of every operand starts at 16 bytes and has a multiple of 16.
+bool grouped_aligned(const tdx_grouped_args& a, const tdx::GroupedParams& p, int pass) {
+    const int el = a.dtype == TDX_F32 ? 4 : 2;
     Widest w(16);
-    w.stride(a.K, 2);
-    w.stride(a.N, 2);
-    w.ptr(p.a); w.stride(p.ld_a, 2);
+    w.stride(a.K, el);
+    w.stride(a.N, el);
+    w.ptr(p.a); w.stride(p.ld_a, el);
     w.ptr(p.b); w.ptr(p.out);
-    if (pass == tdx::kGroupedDw) w.stride(p.ld_b, 2);
-    else w.stride(p.ld_out, 2);
+    if (pass == tdx::kGroupedDw) w.stride(p.ld_b, el);
+    else w.stride(p.ld_out, el);
     return w.bytes == 16;
+}
+// The tensor-core kernel reads (aligned) operands by the copy engine and writes 16 bytes at a time; no rows, for dw, are zeros to write.
+bool grouped_fast(const tdx_grouped_args& a) {
+    return a.dtype == TDX_BF16 && a.rows != 0 && a.N != 0 && a.K != 0 && a.experts <= tdx::kGroupedMostExperts;
 }
 
 template <int PASS>
@@ -126,8 +130,10 @@ int run_grouped(const tdx_grouped_args* args, void* stream) {
     TDX_TRY(tdx_host::get_device(&dev));
     p.status = dev.status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (grouped_fast(*args, p, PASS)) return launch_grouped_umma<PASS>(p, dev, st);
-    return args->dtype == TDX_F32 ? launch_grouped_rows<float, PASS>(p, dev.sm_count, st) : launch_grouped_rows<__nv_bfloat16, PASS>(p, dev.sm_count, st);
+    const bool aligned = grouped_aligned(*args, p, PASS);
+    if (aligned && grouped_fast(*args)) return launch_grouped_umma<PASS>(p, dev, st);
+    if (args->dtype != TDX_F32) return launch_grouped_rows<__nv_bfloat16, PASS, 1>(p, st);
+    return aligned ? launch_grouped_rows<float, PASS, 4>(p, st) : launch_grouped_rows<float, PASS, 1>(p, st);
 }
 
 }  // namespace

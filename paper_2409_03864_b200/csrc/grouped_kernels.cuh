@@ -10,6 +10,8 @@
 #include "bounded_wait.cuh"
 #include "seq_common.cuh"
 
+#include <type_traits>
+
 namespace tdx {
 
 enum GroupedPass { kGroupedForward, kGroupedDx, kGroupedDw };
@@ -37,16 +39,28 @@ struct GroupedParams {
 __device__ __forceinline__ SeqRange grouped_range(const GroupedParams& p, int e) { return seq_range(p.offsets, e, p.rows, p.rows, p.status); }
 
 // ---------------------------------------------------------------- CUDA cores
-constexpr int kSimtK = 16;
+constexpr int kSimtThreads = 256;
+constexpr int kSimtColumns = 64;
+constexpr int kSimtGroups = 4;                                  // of 64 threads
+constexpr int kSimtEach = 8;                                    // of the reduction for each group
+constexpr int kSimtK = kSimtGroups * kSimtEach;
 
-// One tile of BM x BN outputs (BM / 8 x BN / 16 a thread), 16 of the reduction at a time through shared memory; the next 16 are on their
-// way while these are multiplied.  BM = 16 serves experts of few rows, where a tile of 64 would be mostly empty; BN = 64 products whose
-// tiles of 128 would leave SMs with a block or two (1501 x 1000 x 520 in five experts, forward and gradients: 266 -> 178 us).
-template <typename T, int PASS, int BM, int BN>
-__global__ void __launch_bounds__(128) grouped_simt_kernel(const __grid_constant__ GroupedParams p) {
-    constexpr int TM = BM / 8, TN = BN / 16, kSimtN = BN;         // rows and columns a thread
-    __shared__ __align__(16) float sa[2][kSimtK][BM + 4];
-    __shared__ __align__(16) float sb[2][kSimtK][kSimtN + 4];
+// One tile of BM x 64 outputs, 32 of the reduction at a time through shared memory; the next 32 are on their way while these are
+// multiplied.  What bounds it is the scheduler and shared memory: 8 x 8 outputs a thread take two 16-byte reads of each operand for 64
+// multiply-adds, and pairs of columns take one instruction for two.  A tile has 64 such threads, and products of a few thousand rows and
+// columns have two or three tiles an SM; so four groups of threads take eight of the reduction each, and their sums are added up at the
+// end, always in the same order.  1501 x 1000 x 520 in five experts, forward and both gradients: 183 us (25.6 TFLOP/s of the CUDA cores'
+// 74); one column an instruction 222 us; 8 x 4 outputs a thread and one group 247 us.  BM = 16 serves experts of few rows, where a
+// tile of 64 would be mostly empty.  VEC = 4 moves 16 bytes at a time.
+// In shared memory the groups of four columns of a line k are exchanged by k / 4 (exclusive or), so that operands whose contiguous
+// dimension is the reduction are written to different banks.
+template <typename T, int PASS, int BM, int VEC>
+__global__ void __launch_bounds__(kSimtThreads, 2) grouped_simt_kernel(const __grid_constant__ GroupedParams p) {
+    constexpr int BN = kSimtColumns, kSide = BM == 64 ? 8 : 16;   // threads of a group along the columns
+    constexpr int TM = BM == 64 ? 8 : 4, TN = BN / kSide, kTile = kSimtK * (BM + BN);
+    static_assert(BM / TM * kSide == kSimtThreads / kSimtGroups, "a group covers a tile");
+    static_assert(TM * TN * (kSimtThreads / 2) <= 2 * kTile, "two groups' sums fit");
+    __shared__ __align__(16) float shared[2 * kTile];
     const T* a = static_cast<const T*>(p.a);
     const T* b = static_cast<const T*>(p.b);
     T* out = static_cast<T*>(p.out);
@@ -55,18 +69,18 @@ __global__ void __launch_bounds__(128) grouped_simt_kernel(const __grid_constant
     int m_count, n_count, m0, n0;
     long long depth;
     if (PASS == kGroupedDw) {
-        const int tiles_n = (p.K + kSimtN - 1) / kSimtN, tiles_m = (p.N + BM - 1) / BM;
-        const long long item = blockIdx.x;
-        const int e = static_cast<int>(item / (static_cast<long long>(tiles_n) * tiles_m)), in = static_cast<int>(item - static_cast<long long>(e) * tiles_n * tiles_m);
+        const int tiles_n = (p.K + BN - 1) / BN, tiles_m = (p.N + BM - 1) / BM;
+        const long long item = blockIdx.x, per = static_cast<long long>(tiles_n) * tiles_m;
+        const int e = static_cast<int>(item / per), in = static_cast<int>(item - e * per);
         const SeqRange r = grouped_range(p, e);
-        m0 = in / tiles_n * BM; n0 = in % tiles_n * kSimtN;
+        m0 = in / tiles_n * BM; n0 = in % tiles_n * BN;
         m_count = p.N; n_count = p.K; depth = r.len;
         a += r.first * p.ld_a; b += r.first * p.ld_b; out += static_cast<long long>(e) * p.N * p.K;
     } else {
         n_count = PASS == kGroupedForward ? p.N : p.K;
-        const int tiles_n = (n_count + kSimtN - 1) / kSimtN;
+        const int tiles_n = (n_count + BN - 1) / BN;
         const long long number = blockIdx.x / tiles_n;
-        n0 = (blockIdx.x - number * tiles_n) * kSimtN;
+        n0 = static_cast<int>(blockIdx.x - number * tiles_n) * BN;
         if (n0 == 0) seq_check(p.offsets, number, p.experts, p.rows, p.rows, p.status);
         const SeqPiece piece = seq_piece(p.offsets, p.experts, 1, BM, number);
         const SeqRange r = grouped_range(p, static_cast<int>(piece.b));
@@ -76,73 +90,121 @@ __global__ void __launch_bounds__(128) grouped_simt_kernel(const __grid_constant
     }
     const long long ld_b = PASS == kGroupedDw ? p.ld_b : p.K, ld_out = PASS == kGroupedDw ? p.K : p.ld_out;
     constexpr bool kADeep = PASS != kGroupedDw, kBDeep = PASS == kGroupedForward;   // the reduction is the contiguous dimension
-    constexpr int kAOf = BM * kSimtK / 128, kBOf = kSimtN * kSimtK / 128;
-    float ra[kAOf], rb[kBOf];
+    constexpr int kAOf = (BM * kSimtK / VEC + kSimtThreads - 1) / kSimtThreads, kBOf = BN * kSimtK / VEC / kSimtThreads;
+    SeqVec<T, VEC> ra[kAOf], rb[kBOf];
+    // VEC elements of an operand of `count` lines or columns (from `first` on), number `at` of what the block copies
+    auto place = [&](auto deep, int width, int at, int* c, int* k) {
+        if (decltype(deep)::value) { *c = at / (kSimtK / VEC); *k = at % (kSimtK / VEC) * VEC; }
+        else { *c = at % (width / VEC) * VEC; *k = at / (width / VEC); }
+    };
+    auto get = [&](auto deep, int width, int at, const T* from, long long ld, int first, int count, long long k0, SeqVec<T, VEC>* r) {
+        int c, k;
+        place(deep, width, at, &c, &k);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) r->v[i] = seq_from_float<T>(0.0f);
+        if (c < count - first && k < depth - k0) *r = seq_load<T, VEC>(from + (decltype(deep)::value ? (first + c) * ld + k0 + k : (k0 + k) * ld + first + c));
+    };
+    auto put = [&](auto deep, int width, int at, float* to, const SeqVec<T, VEC>& r) {
+        int c, k;
+        place(deep, width, at, &c, &k);
+        const int mask = width / 4 < 8 ? width / 4 - 1 : 7;
+        float f[VEC];
+        seq_unpack<T, VEC>(r, f);
+        float* at_k = to + k * width + (((c / 4) ^ (k / 4 & mask)) * 4 + c % 4);
+        if (decltype(deep)::value) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) at_k[i * width] = f[i];       // VEC of four start at a multiple of four: one k / 4
+        } else {
+            seq_store<float, VEC>(at_k, f);
+        }
+    };
+    typedef typename std::conditional<kADeep, SeqYes, SeqNo>::type ADeep;
+    typedef typename std::conditional<kBDeep, SeqYes, SeqNo>::type BDeep;
     auto fetch = [&](long long k0) {
 #pragma unroll
-        for (int i = 0; i < kAOf; ++i) {
-            const int at = tid + i * 128;
-            const int m = kADeep ? at / kSimtK : at % BM, k = kADeep ? at % kSimtK : at / BM;
-            const bool there = m0 + m < m_count && k0 + k < depth;
-            ra[i] = there ? seq_to_float(kADeep ? a[(m0 + m) * p.ld_a + k0 + k] : a[(k0 + k) * p.ld_a + m0 + m]) : 0.0f;
-        }
+        for (int i = 0; i < kAOf; ++i)
+            if (BM * kSimtK / VEC >= kSimtThreads || tid < BM * kSimtK / VEC) get(ADeep(), BM, tid + i * kSimtThreads, a, p.ld_a, m0, m_count, k0, &ra[i]);
 #pragma unroll
-        for (int i = 0; i < kBOf; ++i) {
-            const int at = tid + i * 128;
-            const int n = kBDeep ? at / kSimtK : at % kSimtN, k = kBDeep ? at % kSimtK : at / kSimtN;
-            const bool there = n0 + n < n_count && k0 + k < depth;
-            rb[i] = there ? seq_to_float(kBDeep ? b[(n0 + n) * ld_b + k0 + k] : b[(k0 + k) * ld_b + n0 + n]) : 0.0f;
-        }
+        for (int i = 0; i < kBOf; ++i) get(BDeep(), BN, tid + i * kSimtThreads, b, ld_b, n0, n_count, k0, &rb[i]);
     };
-    auto put = [&](int buf) {
+    auto keep = [&](int buf) {
+        float* sa = shared + buf * kTile;
 #pragma unroll
-        for (int i = 0; i < kAOf; ++i) {
-            const int at = tid + i * 128;
-            sa[buf][kADeep ? at % kSimtK : at / BM][kADeep ? at / kSimtK : at % BM] = ra[i];
-        }
+        for (int i = 0; i < kAOf; ++i)
+            if (BM * kSimtK / VEC >= kSimtThreads || tid < BM * kSimtK / VEC) put(ADeep(), BM, tid + i * kSimtThreads, sa, ra[i]);
 #pragma unroll
-        for (int i = 0; i < kBOf; ++i) {
-            const int at = tid + i * 128;
-            sb[buf][kBDeep ? at % kSimtK : at / kSimtN][kBDeep ? at / kSimtK : at % kSimtN] = rb[i];
-        }
+        for (int i = 0; i < kBOf; ++i) put(BDeep(), BN, tid + i * kSimtThreads, sa + kSimtK * BM, rb[i]);
     };
-    float acc[TM][TN];
+    f32x2 acc[TM][TN / 2];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = 0.0f;
-    const int tm = tid / 16 * TM, tn = tid % 16 * 4;              // columns tn .. tn + 3 (and 64 + tn ..): no bank conflicts
+        for (int j = 0; j < TN / 2; ++j) acc[i][j] = 0;
+    // rows tm .. tm + 3 and 32 + tm .., columns tn .. tn + 3 and 32 + tn ..: neighbours read neighbours
+    const int group = tid / (kSimtThreads / kSimtGroups), in_group = tid % (kSimtThreads / kSimtGroups);
+    const int tm = in_group / kSide * 4, tn = in_group % kSide * 4;
+    constexpr int kAMask = BM / 4 < 8 ? BM / 4 - 1 : 7;
     fetch(0);
-    put(0);
+    keep(0);
     __syncthreads();
     int buf = 0;
     for (long long k0 = 0; k0 < depth; k0 += kSimtK) {
         const bool more = k0 + kSimtK < depth;
         if (more) fetch(k0 + kSimtK);
+        const float* sa = shared + buf * kTile + group * kSimtEach * BM;
+        const float* sb = shared + buf * kTile + kSimtK * BM + group * kSimtEach * BN;
 #pragma unroll
-        for (int k = 0; k < kSimtK; ++k) {
-            float fa[TM], fb[TN];
+        for (int k = 0; k < kSimtEach; ++k) {
+            const int turn = group * (kSimtEach / 4) + k / 4;
+            float fa[TM];
+            f32x2 fb[TN / 2];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[i] = sa[buf][k][tm + i];
+            for (int i = 0; i < TM; i += 4) *reinterpret_cast<float4*>(fa + i) = *reinterpret_cast<const float4*>(sa + k * BM + ((tm / 4 + i * 2) ^ (turn & kAMask)) * 4);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = sb[buf][k][j < 4 ? tn + j : 60 + tn + j];
+            for (int j = 0; j < TN; j += 4) *reinterpret_cast<ulonglong2*>(fb + j / 2) = *reinterpret_cast<const ulonglong2*>(sb + k * BN + ((tn / 4 + j * 2) ^ (turn & 7)) * 4);
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+            for (int i = 0; i < TM; ++i) {
+                const f32x2 twice = pack2(fa[i], fa[i]);
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = fmaf(fa[i], fb[j], acc[i][j]);
+                for (int j = 0; j < TN / 2; ++j) acc[i][j] = fma2(twice, fb[j], acc[i][j]);
+            }
         }
-        if (more) put(buf ^ 1);
+        if (more) keep(buf ^ 1);
         __syncthreads();
         buf ^= 1;
     }
+    // groups 2 and 3 give their sums to 0 and 1, and 1 gives its to 0
+#pragma unroll
+    for (int half = kSimtGroups / 2; half > 0; half /= 2) {
+        f32x2* mine = reinterpret_cast<f32x2*>(shared) + tid % (half * (kSimtThreads / kSimtGroups));
+        constexpr int kOne = kSimtThreads / kSimtGroups;
+        if (group >= half && group < 2 * half) {
+#pragma unroll
+            for (int i = 0; i < TM * TN / 2; ++i) mine[i * half * kOne] = acc[i * 2 / TN][i % (TN / 2)];
+        }
+        __syncthreads();
+        if (group < half) {
+#pragma unroll
+            for (int i = 0; i < TM * TN / 2; ++i) acc[i * 2 / TN][i % (TN / 2)] = add2(acc[i * 2 / TN][i % (TN / 2)], mine[i * half * kOne]);
+        }
+        __syncthreads();
+    }
+    if (group > 0) return;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        if (m0 + tm + i >= m_count) break;
-        T* row = out + (m0 + tm + i) * ld_out;
+        const int m = tm + i % 4 + i / 4 * 32;
+        if (m >= m_count - m0) continue;
+        T* row = out + (m0 + m) * ld_out;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int n = n0 + tn + (j < 4 ? j : 60 + j);
-            if (n < n_count) row[n] = seq_from_float<T>(acc[i][j]);
+        for (int j = 0; j < TN; j += VEC) {
+            float sums[TN];
+            unpack2(acc[i][j / 2], sums[j / 2 * 2], sums[j / 2 * 2 + 1]);
+            if (VEC == 4) unpack2(acc[i][j / 2 + 1], sums[j / 2 * 2 + 2], sums[j / 2 * 2 + 3]);
+            const int n = tn + j % 4 + j / 4 * 32;
+            float f[VEC];
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) f[v] = sums[j + v];
+            if (n < n_count - n0) seq_store<T, VEC>(row + n0 + n, f);
         }
     }
 }
