@@ -49,8 +49,8 @@ constexpr int kSimtK = kSimtGroups * kSimtEach;
 // multiplied.  What bounds it is the scheduler and shared memory: 8 x 8 outputs a thread take two 16-byte reads of each operand for 64
 // multiply-adds, and pairs of columns take one instruction for two.  A tile has 64 such threads, and products of a few thousand rows and
 // columns have two or three tiles an SM; so four groups of threads take eight of the reduction each, and their sums are added up at the
-// end, always in the same order.  1501 x 1000 x 520 in five experts, forward and both gradients: 183 us (25.6 TFLOP/s of the CUDA cores'
-// 74); one column an instruction 222 us; 8 x 4 outputs a thread and one group 247 us.  BM = 16 serves experts of few rows, where a
+// end, always in the same order.  1501 x 1000 x 520 in five experts, forward and both gradients: 174 us (27 TFLOP/s of the CUDA cores'
+// 74); addresses made anew for every 32: 183 us; one column an instruction: 222 us; 8 x 4 outputs a thread and one group: 247 us.  BM = 16 serves experts of few rows, where a
 // tile of 64 would be mostly empty.  VEC = 4 moves 16 bytes at a time.
 // In shared memory the groups of four columns of a line k are exchanged by k / 4 (exclusive or), so that operands whose contiguous
 // dimension is the reduction are written to different banks.
@@ -92,17 +92,24 @@ __global__ void __launch_bounds__(kSimtThreads, 2) grouped_simt_kernel(const __g
     constexpr bool kADeep = PASS != kGroupedDw, kBDeep = PASS == kGroupedForward;   // the reduction is the contiguous dimension
     constexpr int kAOf = (BM * kSimtK / VEC + kSimtThreads - 1) / kSimtThreads, kBOf = BN * kSimtK / VEC / kSimtThreads;
     SeqVec<T, VEC> ra[kAOf], rb[kBOf];
-    // VEC elements of an operand of `count` lines or columns (from `first` on), number `at` of what the block copies
+    // VEC elements of an operand, number `at` of what the block copies: line or column c, line k of the reduction
     auto place = [&](auto deep, int width, int at, int* c, int* k) {
         if (decltype(deep)::value) { *c = at / (kSimtK / VEC); *k = at % (kSimtK / VEC) * VEC; }
         else { *c = at % (width / VEC) * VEC; *k = at / (width / VEC); }
     };
-    auto get = [&](auto deep, int width, int at, const T* from, long long ld, int first, int count, long long k0, SeqVec<T, VEC>* r) {
+    // the thread's first, from where its others are a fixed distance apart
+    auto start = [&](auto deep, int width, const T* from, long long ld, int first) {
         int c, k;
-        place(deep, width, at, &c, &k);
+        place(deep, width, tid, &c, &k);
+        return from + (decltype(deep)::value ? (static_cast<long long>(first) + c) * ld + k : k * ld + first + c);
+    };
+    auto get = [&](auto deep, int width, int i, const T* from, long long ld, int count, long long left, SeqVec<T, VEC>* r) {
+        int c, k;
+        place(deep, width, tid + i * kSimtThreads, &c, &k);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) r->v[i] = seq_from_float<T>(0.0f);
-        if (c < count - first && k < depth - k0) *r = seq_load<T, VEC>(from + (decltype(deep)::value ? (first + c) * ld + k0 + k : (k0 + k) * ld + first + c));
+        for (int v = 0; v < VEC; ++v) r->v[v] = seq_from_float<T>(0.0f);
+        const int apart = kSimtThreads / ((decltype(deep)::value ? kSimtK : width) / VEC);
+        if (c < count && k < left) *r = seq_load<T, VEC>(from + i * apart * ld);
     };
     auto put = [&](auto deep, int width, int at, float* to, const SeqVec<T, VEC>& r) {
         int c, k;
@@ -120,12 +127,16 @@ __global__ void __launch_bounds__(kSimtThreads, 2) grouped_simt_kernel(const __g
     };
     typedef typename std::conditional<kADeep, SeqYes, SeqNo>::type ADeep;
     typedef typename std::conditional<kBDeep, SeqYes, SeqNo>::type BDeep;
-    auto fetch = [&](long long k0) {
+    const T* next_a = start(ADeep(), BM, a, p.ld_a, m0);
+    const T* next_b = start(BDeep(), BN, b, ld_b, n0);
+    auto fetch = [&](long long left) {
 #pragma unroll
         for (int i = 0; i < kAOf; ++i)
-            if (BM * kSimtK / VEC >= kSimtThreads || tid < BM * kSimtK / VEC) get(ADeep(), BM, tid + i * kSimtThreads, a, p.ld_a, m0, m_count, k0, &ra[i]);
+            if (BM * kSimtK / VEC >= kSimtThreads || tid < BM * kSimtK / VEC) get(ADeep(), BM, i, next_a, p.ld_a, m_count - m0, left, &ra[i]);
 #pragma unroll
-        for (int i = 0; i < kBOf; ++i) get(BDeep(), BN, tid + i * kSimtThreads, b, ld_b, n0, n_count, k0, &rb[i]);
+        for (int i = 0; i < kBOf; ++i) get(BDeep(), BN, i, next_b, ld_b, n_count - n0, left, &rb[i]);
+        next_a += kADeep ? kSimtK : kSimtK * p.ld_a;
+        next_b += kBDeep ? kSimtK : kSimtK * ld_b;
     };
     auto keep = [&](int buf) {
         float* sa = shared + buf * kTile;
@@ -144,13 +155,13 @@ __global__ void __launch_bounds__(kSimtThreads, 2) grouped_simt_kernel(const __g
     const int group = tid / (kSimtThreads / kSimtGroups), in_group = tid % (kSimtThreads / kSimtGroups);
     const int tm = in_group / kSide * 4, tn = in_group % kSide * 4;
     constexpr int kAMask = BM / 4 < 8 ? BM / 4 - 1 : 7;
-    fetch(0);
+    fetch(depth);
     keep(0);
     __syncthreads();
     int buf = 0;
     for (long long k0 = 0; k0 < depth; k0 += kSimtK) {
         const bool more = k0 + kSimtK < depth;
-        if (more) fetch(k0 + kSimtK);
+        if (more) fetch(depth - k0 - kSimtK);
         const float* sa = shared + buf * kTile + group * kSimtEach * BM;
         const float* sb = shared + buf * kTile + kSimtK * BM + group * kSimtEach * BN;
 #pragma unroll
@@ -214,6 +225,10 @@ __global__ void __launch_bounds__(kSimtThreads, 2) grouped_simt_kernel(const __g
 // tcgen05 products, eight warps turn accumulators into bf16.  The features are the product's M (128 or two times 128) and the rows of an
 // expert its N: an expert's last tile then costs what its rows need, in steps of 16, instead of a whole tile of 128, and a few rows cost
 // 32 columns of a product that streams the weights.  Accumulators are held twice, so a tile's epilogue runs under the next tile's products.
+// Measured: 8 x 2048 rows, 4096 x 4096: 381 us (1443 of the 1664 TFLOP/s of a library's product), bound by the products; 8192 rows unevenly
+// over 16 experts, 4096 x 2048: 143 (958), bound by the last round of tiles (blocks take tiles in turn; taking them from a counter instead
+// was 3 % faster here, 10 % slower for few rows, and would need a workspace); 128 rows over 32 experts, 2048 x 2048: 41 us, which is the weights'
+// 269 MB at the copy rate.
 // dw sums over an expert's rows: both operands are read with the rows as the reduction, and rows of the last block that belong to the
 // next expert are set to zero in shared memory in front of the product (a factor of zero in one operand would leave NaN and infinity).
 constexpr int kGroupedMostExperts = 1024;                        // whose tile counts are kept in shared memory
