@@ -480,7 +480,7 @@ int tdx_gemm_grouped_workspace_size(const tdx_grouped_args* args, size_t* bytes)
  * q, k and v have q_heads, k_heads and v_heads heads side by side in a row, each a divisor of `heads` (0: heads); head h reads head
  * h / (heads / q_heads) of q, and so on.  log_decay is a constant of the layer and has no gradient; values above 0 grow.  Prompts run in
  * chunks of rows (inside a chunk as products of matrices), so a value of q, k or v that is not finite may also reach the rows of its
- * chunk in front of it, up to 63, and their gradients.
+ * chunk in front of it, up to 127, and their gradients.
  * bf16: products of bf16 values with fp32 sums; the states that a row reads are rounded to bf16 in front of their product, attention weights
  * and the keys that go into a state keep 16 bits, and the states that are handed on (state_out, dstate_in) and all sums 24.
  * Backward: dq, dk, dv (summed over the heads that share one) and dstate_in from q, k, v, state_in, dout and dstate_out.

@@ -6,6 +6,9 @@
 //
 // The gradients are the same sum with the roles exchanged, dq with (dout, v, k) and S^T, dv and dk from the last row to the first with
 // (k, q, dout) and (v, dout, q) and the gradient of the state, so one kernel serves all four ("q", "k", "v" below are roles).
+//
+// This file: mma.sync, for fp32 (three bf16 pieces of every operand) and bf16 rows of any alignment.  A chunk is a chain of products, each
+// waiting for the one in front, with 8 warps an SM: that latency bounds it, not the bytes.  So sequences are cut into many segments.
 #pragma once
 #include "seq_common.cuh"
 
@@ -453,7 +456,8 @@ __global__ void __launch_bounds__(256) attn_share_kernel(long long batch, long l
 }
 
 // One token: a block has one row of the batch and one head.  Threads lie along dim_v, VEC values each, and in groups along dim_k; the
-// state goes through registers once, which is what bounds it (8 dim_k dim_v bytes a head).
+// state goes through registers once, which is what bounds it (8 dim_k dim_v bytes a head).  128 rows, 32 heads of 64 x 64: 24.5 us for 128 MB
+// (5.2 of the copy's 6.6 TB/s).
 constexpr int kAttnStepThreads = 128;
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kAttnStepThreads) attn_step_kernel(const __grid_constant__ AttnParams p) {

@@ -14,6 +14,9 @@
 // The second piece of P costs 8 % (forward and backward of 4 x 2048 rows, 16 heads of 128: 218 -> 236 us) and takes the larger of the two
 // roundings on the way to the output out (P's and the state's): 1.4 times the error of a single rounding became 1.0 to 1.3 times.
 //
+// Measured, bf16, heads of 128: one prompt of 4096 rows with 32 heads 83 us (171 with the kernel on mma.sync), forward and backward of 4 x
+// 2048 rows with 16 heads 236 us (577).  The schedulers issue in 38 to 40 % of the cycles and memory runs at 28 to 30 % of its rate: a chunk
+// of 4 us is the chain W, P, O2, out and the chain of states from one chunk to the next.
 // A chunk of 128 x 128 takes about 5,500 cycles of an SM's share of the memory bandwidth and about 3,100 cycles of products, so one
 // chunk at a time with its operands fetched ahead is enough.  U starts from zero in every chunk: the tensor cores cut sums off instead of
 // rounding them, which over a whole sequence shows in the state (3e-6), over 128 rows it does not.

@@ -6,6 +6,8 @@
 // Bandwidth bounds both directions, so a row is read once: `warps` warps hold it in registers, NV vectors of VEC channels a
 // thread, all loads issued before the first use.  Sums over a row go through shuffles and one barrier of the row's own warps;
 // sums over groups of channels through shuffles alone where a group is 1, 2, 4, ... 32 vectors, else through shared memory.
+// Measured, bf16, rows of 4096: norm and gate of heads of 128, 8192 rows, 37.5 us (201 MB: 5.4 of the 6.6 TB/s that a copy reaches); 4 rows 7 us,
+// which is the call itself.
 #pragma once
 #include "seq_common.cuh"
 
@@ -326,6 +328,9 @@ __global__ void __launch_bounds__(kNormThreads, NV * VEC <= 8 ? 2 : 1) norm_fwd_
 //   dweight_out = sum over rows of dy sh,  dscale = of ds a,  dweight_in = of du xh.
 // s is computed again from x, gate and residual, which costs no more bytes than reading it and keeps its 32 bits.  A thread keeps
 // its channels' parameter sums in registers over all rows of its set; a second kernel adds the sets in a fixed order.
+// Sixteen warps an SM is all that 128 registers leave (8 channels a thread with three sums each and the next row on its way), so
+// latency bounds it, at half the issue rate and a third of the memory's.  Everything at once (norm in and out, gate, scale, residual),
+// 8192 x 4096 in bf16, forward and backward: 252 us for 873 MB; without the next row's loads 336.
 template <typename T, int VEC, int NV, int HAS>
 __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_constant__ NormParams p) {
     typedef typename NormLanes<VEC>::type Lane;
