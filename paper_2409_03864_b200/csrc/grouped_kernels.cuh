@@ -225,14 +225,13 @@ __global__ void __launch_bounds__(kSimtThreads, 2) grouped_simt_kernel(const __g
 // tcgen05 products, eight warps turn accumulators into bf16.  The features are the product's M (128 or two times 128) and the rows of an
 // expert its N: an expert's last tile then costs what its rows need, in steps of 16, instead of a whole tile of 128, and a few rows cost
 // 32 columns of a product that streams the weights.  Accumulators are held twice, so a tile's epilogue runs under the next tile's products.
-// Measured: 8 x 2048 rows, 4096 x 4096: 381 us (1443 of the 1664 TFLOP/s of a library's product), bound by the products; 8192 rows unevenly
-// over 16 experts, 4096 x 2048: 143 (958), bound by the last round of tiles (blocks take tiles in turn; taking them from a counter instead
-// was 3 % faster here, 10 % slower for few rows, and would need a workspace); 128 rows over 32 experts, 2048 x 2048: 41 us, which is the weights'
-// 269 MB at the copy rate.
+// Measured: 8 x 2048 rows, 4096 x 4096: 382 us (1440 of the 1664 TFLOP/s of a library's product), bound by the products; 8192 rows unevenly
+// over 16 experts, 4096 x 2048: 137 (1002), bound by the last round of tiles; 128 rows over 32 experts, 2048 x 2048: 42 us, which is the
+// weights' 269 MB at the copy rate.
 // dw sums over an expert's rows: both operands are read with the rows as the reduction, and rows of the last block that belong to the
 // next expert are set to zero in shared memory in front of the product (a factor of zero in one operand would leave NaN and infinity).
 constexpr int kGroupedMostExperts = 1024;                        // whose tile counts are kept in shared memory
-constexpr int kGroupedSorted = 128;                              // experts that dw sorts by their rows, each against all others
+constexpr int kGroupedSorted = 128;                              // experts that are sorted by their rows, each against all others
 constexpr int kGroupedThreads = 320;
 constexpr int kGroupedEpilogueWarps = 8;
 constexpr int kGroupedStagePitch = 80;                           // bytes of a staged row of 32 bf16
@@ -257,8 +256,8 @@ __device__ __forceinline__ int grouped_search(const int* table, int count, int v
     }
     return lo;
 }
-// `first`: forward and dx: whole tiles of rows of the experts in front of each, added up, and behind them the same for tiles with rows
-// left over; dw: the experts, most rows first.
+// `first`: forward and dx: whole tiles of rows of the experts in front of each, added up, and behind them the experts with rows left over,
+// most of them first, and their number; dw: the experts, most rows first.
 template <int PASS>
 __device__ __forceinline__ bool grouped_tile(const GroupedParams& p, const int* first, long long item, GroupedTile* t) {
     if (PASS == kGroupedDw) {
@@ -274,8 +273,8 @@ __device__ __forceinline__ bool grouped_tile(const GroupedParams& p, const int* 
         t->blocks = (t->count + 63) / 64;
         return true;
     }
-    // Whole tiles come first and those with what is left of an expert's rows behind them, so that the last round, which not all
-    // blocks have a tile for, is one of small tiles.  An expert's tiles of rows lie side by side for each tile of features, so that
+    // Whole tiles come first and those with what is left of an expert's rows behind them, large ones first, so that the last round, which
+    // not all blocks have a tile for, is one of small tiles.  An expert's tiles of rows lie side by side for each tile of features, so that
     // its weights are read together.
     const int* rest = first + p.experts + 1;
     const long long whole = static_cast<long long>(first[p.experts]) * p.feature_tiles;
@@ -288,9 +287,9 @@ __device__ __forceinline__ bool grouped_tile(const GroupedParams& p, const int* 
     } else {
         const long long behind = item - whole;
         if (behind >= static_cast<long long>(rest[p.experts]) * p.feature_tiles) return false;
-        const int number = static_cast<int>(behind / p.feature_tiles);
-        e = grouped_search(rest, p.experts, number);
-        f = static_cast<int>(behind - static_cast<long long>(number) * p.feature_tiles);
+        const int place = static_cast<int>(behind / p.feature_tiles);
+        e = rest[place];
+        f = static_cast<int>(behind - static_cast<long long>(place) * p.feature_tiles);
         r = first[e + 1] - first[e];
     }
     const int from = __ldg(p.offsets + e), to = __ldg(p.offsets + e + 1);
@@ -339,43 +338,59 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
     }
     ptx::grid_dependency_wait();
     if (warp == 0) {
+        // where an expert stands among those with more rows (left over)
+        auto rows_of = [&](int e) {
+            const int lo = __ldg(p.offsets + e), hi = __ldg(p.offsets + e + 1), n = seq_accepted(lo, hi, p.rows, p.rows) ? hi - lo : 0;
+            return PASS == kGroupedDw ? n : n % p.bt;
+        };
+        auto place_of = [&](int e, int n) {
+            int place = 0;
+            for (int o = 0; o < p.experts; ++o) {
+                const int m = rows_of(o);
+                place += m > n || (m == n && o < e);
+            }
+            return place;
+        };
+        // (narrow tiles cost the weights that they read, whatever their rows are)
+        const bool sorted = p.experts <= kGroupedSorted && (PASS == kGroupedDw || p.bt > 64);
         if (PASS == kGroupedDw) {
             for (int e = lane; e < p.experts; e += 32) {
                 const int n = grouped_range(p, e).len;
-                int place = e;
-                if (p.experts <= kGroupedSorted) {
-                    place = 0;
-                    for (int o = 0; o < p.experts; ++o) {
-                        const int lo = __ldg(p.offsets + o), hi = __ldg(p.offsets + o + 1), m = seq_accepted(lo, hi, p.rows, p.rows) ? hi - lo : 0;
-                        place += m > n || (m == n && o < e);
-                    }
-                }
-                first[place] = e;
+                first[sorted ? place_of(e, n) : e] = e;
             }
         } else {
-            int whole = 0, rest = 0;
-            if (lane == 0) first[0] = first[p.experts + 1] = 0;
+            int* const rest = first + p.experts + 1;
+            int whole = 0, count = 0;
+            if (lane == 0) first[0] = 0;
             for (int e0 = 0; e0 < p.experts; e0 += 32) {
-                const int e = e0 + lane, n = e < p.experts ? grouped_range(p, e).len : 0;
-                int w = n / p.bt, l = n % p.bt > 0;
+                const int e = e0 + lane, n = e < p.experts ? grouped_range(p, e).len : 0, left = n % p.bt;
+                int w = n / p.bt;
 #pragma unroll
                 for (int d = 1; d < 32; d *= 2) {
-                    const int up = __shfl_up_sync(0xffffffffu, w, d), more = __shfl_up_sync(0xffffffffu, l, d);
-                    if (lane >= d) { w += up; l += more; }
+                    const int up = __shfl_up_sync(0xffffffffu, w, d);
+                    if (lane >= d) w += up;
                 }
-                if (e < p.experts) {
-                    first[e + 1] = whole + w;
-                    first[p.experts + 2 + e] = rest + l;
-                }
+                const uint32_t there = __ballot_sync(0xffffffffu, left > 0);
+                if (e < p.experts) first[e + 1] = whole + w;
+                if (left > 0) rest[sorted ? place_of(e, left) : count + __popc(there & ((1u << lane) - 1u))] = e;
+                __syncwarp();
                 whole += __shfl_sync(0xffffffffu, w, 31);
-                rest += __shfl_sync(0xffffffffu, l, 31);
+                count += __popc(there);
             }
+            if (lane == 0) rest[p.experts] = count;
         }
     }
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = s_tmem;
+    // A block's tiles: rounds go through the blocks forwards and backwards in turn, so that with tiles from large to small all blocks
+    // get about as much (8192 rows unevenly over 16 experts, 4096 x 2048: 154 -> 147 us with large ones first; taking tiles from a counter
+    // is no faster and needs a workspace).  Narrow tiles cost the same all of them.
+    auto tile_of = [&](int local, GroupedTile* t) {
+        const unsigned at = (local & 1) != 0 && p.bt > 64 ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+        return grouped_tile<PASS>(p, first, static_cast<long long>(local) * gridDim.x + at, t);
+    };
 
     if (warp == 0) {
         if (ptx::elect_one()) {
@@ -383,7 +398,7 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
             uint32_t phase = 0;
             bool ok = true;
             GroupedTile t;
-            for (long long item = blockIdx.x; ok && grouped_tile<PASS>(p, first, item, &t); item += gridDim.x) {
+            for (int local = 0; ok && tile_of(local, &t); ++local) {
                 const int boxes = PASS == kGroupedDw ? p.bt / 64 : (t.count + p.box - 1) / p.box;
                 const uint32_t bytes = a_bytes + static_cast<uint32_t>(boxes) * (PASS == kGroupedDw ? 8192u : static_cast<uint32_t>(p.box) * 128u);
                 for (int kb = 0; kb < t.blocks; ++kb) {
@@ -424,11 +439,11 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
         const uint64_t a_desc0 = ptx::make_smem_desc_sw128(ptx::smem_u32(ring), kATurned ? 8192u : 16u, 1024u);
         const uint64_t b_desc0 = ptx::make_smem_desc_sw128(ptx::smem_u32(ring) + a_bytes, kBTurned ? 8192u : 16u, 1024u);
         constexpr uint64_t a_k16 = (kATurned ? 2048u : 32u) >> 4, b_k16 = (kBTurned ? 2048u : 32u) >> 4;
-        int stage = 0, local = 0;
+        int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
         GroupedTile t;
-        for (long long item = blockIdx.x; ok && grouped_tile<PASS>(p, first, item, &t); item += gridDim.x, ++local) {
+        for (int local = 0; ok && tile_of(local, &t); ++local) {
             const int buf = local % p.buffers, use = local / p.buffers;
             if (!wait_bounded(&tempty_bar[buf], (use & 1) ^ 1u, abort_flag, p.status, kTimeoutMma)) break;
             ptx::tc_fence_after_sync();
@@ -479,9 +494,8 @@ __global__ void __launch_bounds__(kGroupedThreads, 1) grouped_umma_kernel(const 
         const int c_first = p.halves == 2 ? 0 : (ew >> 2) * 32, c_step = p.halves == 2 ? 32 : 64;
         uint8_t* const mine = staging + ew * kGroupedStageWarp;
         __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out);
-        int local = 0;
         GroupedTile t;
-        for (long long item = blockIdx.x; grouped_tile<PASS>(p, first, item, &t); item += gridDim.x, ++local) {
+        for (int local = 0; tile_of(local, &t); ++local) {
             const int buf = local % p.buffers, use = local / p.buffers;
             if (!wait_bounded(&tfull_bar[buf], use & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
             ptx::tc_fence_after_sync();
