@@ -422,7 +422,8 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
                     const int at = first + q * kWorkers, row = at / 8 % kAttnRows;
-                    const float w = weight[kAttnRows + (BACK ? row : n - 1 - row)];
+                    // (rows that the chunk does not have: zero, not their weight, which may have grown beyond fp32)
+                    const float w = row < n ? weight[kAttnRows + (BACK ? row : n - 1 - row)] : 0.0f;
                     if (row >= n) in[q] = make_uint4(0u, 0u, 0u, 0u);
                     const f32x2 ww = pack2(w, w), minus = pack2(-1.0f, -1.0f);
                     const uint32_t pair[4] = {in[q].x, in[q].y, in[q].z, in[q].w};

@@ -303,3 +303,9 @@ def test_state_in_place_of_sequences_in_several_segments(dtype, pad):
     size, factors = c.exact(True, False), c.factors()
     assert_close("out", two.host(), one.host(), size["out"], 2 * factors[1], dtype)
     assert_close("state", c.cache[at].double().cpu().numpy(), new[at].double().cpu().numpy(), size["state"], 2 * factors[0])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_decays_that_leave_fp32_only_behind_a_short_sequence(dtype):
+    # e^19 is small enough for every sum; e^127, of rows of the tile that the sequence does not have, is not
+    Case(dtype, [20, 7], 1, 16, 16, decay=1.0).check()
