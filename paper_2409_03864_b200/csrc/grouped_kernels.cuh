@@ -235,7 +235,7 @@ constexpr int kGroupedSorted = 128;                              // experts that
 constexpr int kGroupedThreads = 320;
 constexpr int kGroupedEpilogueWarps = 8;
 constexpr int kGroupedStagePitch = 80;                           // bytes of a staged row of 32 bf16
-constexpr int kGroupedStageWarp = 3072;                          // a warp's part: 32 such rows, or 2 KB for the copy engine
+constexpr int kGroupedStageWarp = 3 * 1024;                      // a warp's part: 32 such rows, or 2 KB for the copy engine
 constexpr int kGroupedStaging = kGroupedEpilogueWarps * kGroupedStageWarp;
 constexpr int kGroupedMostStages = 10;
 

@@ -164,3 +164,13 @@ def test_captured_and_replayed_with_other_offsets():
         graph.replay()
         torch.cuda.synchronize()
         close("y", y.host(), ref.grouped(c.x, c.w, offsets), ref.grouped(abs(c.x), abs(c.w), offsets), c.k, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [
+    ([(37 * i) % 700 for i in range(24)], 2304, 64),             # several rounds of tiles, leftovers of every size
+    ([(53 * i) % 151 for i in range(140)], 64, 72),              # more experts than are sorted
+    ([i % 3 for i in range(1030)], 40, 64),                      # more experts than the tensor-core kernel takes
+], ids=["rounds", "unsorted", "thousand"])
+def test_many_tiles_and_experts(shape, dtype):
+    Case(dtype, *shape).check()
