@@ -200,8 +200,9 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     __syncthreads();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = s_tmem;
-    // Each barrier completes once a chunk (those of a set of tiles once a use of the set), and whoever waits for a completion takes part in
-    // what the one after it depends on, so that no waiting warp can be two behind; W runs a chunk ahead of the keys' warps and has two.
+    // Each barrier completes once a chunk (those of a set of tiles once a use of the set).  A wait goes by the parity, so it must not begin before the
+    // completion in front of the one that it is for.  Most waiters wait for every completion; W runs a chunk ahead of the keys' warps and has
+    // two barriers; the keys' warps wait for v only where the chunk is short, behind bar_u, which says that the v in front was there.
     if (warp < 4) {
         attn_fewer_registers<40>();
         if (warp == 0) {
@@ -406,10 +407,11 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
         for (int c = 0; c < chunks; ++c) {
             const int n = rows_of(c);
             if (!wait_bounded_idle(&full_k[c & 1], c >> 1 & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
-            if (n < kAttnRows && !wait_bounded_idle(&full_v[c % Lay::kVs], c / Lay::kVs & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
             // q k^T has been read from k before it is overwritten, and U of the chunk before from the other pieces
             if (!STATE && !wait_bounded_idle(&bar_w[c & 1], c >> 1 & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
             if (c > 0 && !wait_bounded_idle(&bar_u, (c - 1) & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
+            // (behind bar_u: with U of the chunk before done, that chunk's v had landed, so this completion is the next one)
+            if (n < kAttnRows && !wait_bounded_idle(&full_v[c % Lay::kVs], c / Lay::kVs & 1, abort_flag, p.status, kTimeoutEpilogue)) break;
             uint8_t* const k = smem + Lay::kK + (c & 1) * kAttnTile;
             // twice 16 bytes a thread at a time
             const int parts = halves1 * (kAttnHalf / 16);

@@ -309,3 +309,45 @@ def test_state_in_place_of_sequences_in_several_segments(dtype, pad):
 def test_decays_that_leave_fp32_only_behind_a_short_sequence(dtype):
     # e^19 is small enough for every sum; e^127, of rows of the tile that the sequence does not have, is not
     Case(dtype, [20, 7], 1, 16, 16, decay=1.0).check()
+
+
+def run_all(c):
+    """Every output of the call and its backward pass, with and without states handed on."""
+    outs = {}
+    for tag, store in (("", c.slots_of()), (" alone", None)):
+        out = c.rows_of(np.zeros((c.rows, c.heads, c.dv)), fill=-5.0)
+        tdx.check(tdx.tdx_decay_attention(c.args(out=out, state_in=c.cache, state_out=store)))
+        outs["out" + tag] = out.view
+        if store is not None:
+            outs["state"] = store
+        g = {"d" + name: c.rows_of(np.zeros(v.shape), fill=-5.0) for name, v in (("q", c.q), ("k", c.k), ("v", c.v))}
+        grad = None if store is None else c.slots_of()
+        tdx.check(tdx.tdx_decay_attention_bwd(c.args(**g, state_in=c.cache, dstate_out=c.dcache, dstate_in=grad)))
+        outs.update({k + tag: v.view for k, v in g.items()})
+        if grad is not None:
+            outs["dstate"] = grad
+    torch.cuda.synchronize()
+    return {k: v.clone() for k, v in outs.items()}
+
+
+# two heads: the longer sequences are cut into segments; 150: a block has all chunks of a sequence
+@pytest.mark.parametrize("heads", [2, 150])
+@pytest.mark.parametrize("length", [5, 133, 261, 773, 901])      # a short chunk of 5 rows behind 0, 1, 2, 6 and 7 whole ones
+@pytest.mark.parametrize("dtype,pad", [("bf16", 0), ("bf16", 1), ("f32", 0)])
+def test_rows_of_others_that_are_not_finite_do_not_show(dtype, pad, length, heads):
+    c = Case(dtype, [70, length, 90], heads, 16, 24, pad=pad, spare=130)
+    before = tdx.tdx_kernel_launch_count()
+    clean = run_all(c)
+    cut = heads == 2 and length > 700                            # (the passes over the states and the kernel that joins them)
+    assert (tdx.tdx_kernel_launch_count() - before > 8) == cut
+    mine = slice(70, 70 + length)
+    for name in ("q", "k", "v", "dout"):
+        v = c.dev[name].view
+        for part in (v[:70], v[70 + length:]):
+            part[::3], part[1::3], part[2::3] = float("nan"), float("inf"), float("-inf")
+    got = run_all(c)
+    for k in clean:
+        at = int(c.slots[1]) if k in ("state", "dstate") else mine
+        assert bool(torch.isfinite(got[k][at]).all()), k
+        assert torch.equal(got[k][at], clean[k][at]), k
+    tdx.check(tdx.tdx_check_device_status())
