@@ -36,13 +36,39 @@ struct AttnParams {
     int state_vec;                          // attn_umma_kernel: states are read and written 16 bytes at a time along d2
     int s1, s2;                             // strides of a state's d1 and d2
     long long seg, dense;                   // rows of a segment; segments of a dense sequence
-    float* carry;                           // [number][head][slice][KD][kAttnV]: what a segment adds to the state
-    long long sub, sub_dense;               // attn_umma_kernel: rows of a piece of a segment, and pieces of a dense sequence
+    float* carry;                           // [slot][head][slice][KD][kAttnV]: what a piece of a segment adds to the state
+    long long sub, sub_dense;               // rows of a piece of a segment (all of them but in attn_umma_kernel), and pieces of a dense sequence
     int all_pieces;                         // attn_umma_kernel: the last segment's pieces are wanted too, for state_out
+    int every;                              // sequences of one segment have slots in carry too
     int carry_turned;                       // attn_umma_kernel: carry was written by a sum with d1 and d2 exchanged
     int slices;                             // of kAttnV columns of v
     int* status;
 };
+
+// What the pieces of sequences add to the state has slots in `carry`, by which the blocks of the pass over the states are numbered.  Where a
+// batch has more sequences than its rows have segments, sequences of one segment have no slots, so that their number goes by the rows.
+// Packed (rows are int): sequence b, from `row` on, has its slots from this number on.  Behind a sequence with slots it is floor(len / sub) + 1 more at
+// least, which is no less than ceil(len / sub): with `every` since b is, else since it has more than seg rows.
+__host__ __device__ __forceinline__ long long attn_slots_before(int row, long long b, int sub, int seg, bool every) {
+    return row / sub + (every || b < row / seg ? b : row / seg);
+}
+__device__ __forceinline__ long long attn_first_slot(const AttnParams& p, long long b) {
+    return p.offsets == nullptr ? b * p.sub_dense : attn_slots_before(__ldg(p.offsets + b), b, static_cast<int>(p.sub), static_cast<int>(p.seg), p.every);
+}
+// The piece of a slot: of the last sequence whose slots begin at or before it (those without begin where the next ones do).
+__device__ __forceinline__ SeqPiece attn_slot_piece(const AttnParams& p, long long slot) {
+    if (p.offsets == nullptr) return seq_piece(nullptr, p.batch, p.sub_dense, p.sub, slot);
+    SeqPiece r;
+    r.b = 0;
+    for (long long hi = p.batch - 1; r.b < hi;) {
+        const long long mid = (r.b + hi + 1) / 2;
+        if (attn_first_slot(p, mid) <= slot) r.b = mid;
+        else hi = mid - 1;
+    }
+    const long long index = slot - attn_first_slot(p, r.b);
+    r.index = index < 0 || index > kNoPiece ? kNoPiece : static_cast<int>(index);
+    return r;
+}
 
 constexpr int kAttnC = 64;                  // rows of a chunk
 constexpr int kAttnV = 64;                  // columns of v that a block works on
@@ -156,7 +182,7 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
     const int head = static_cast<int>(rest % p.heads);
     const long long number = rest / p.heads;
     if (!STATE && head == 0 && slice == 0) seq_check(p.offsets, number, p.batch, p.max_len, p.rows, p.status);
-    const SeqPiece piece = seq_piece(p.offsets, p.batch, p.dense, p.seg, number);
+    const SeqPiece piece = STATE ? attn_slot_piece(p, number) : seq_piece(p.offsets, p.batch, p.dense, p.seg, number);
     const SeqRange r = seq_range(p.offsets, piece.b, p.max_len, p.rows, p.status);
     const long long start = piece.index * p.seg;
     const long long slot = !STATE && (p.state_in != nullptr || p.state_out != nullptr) ? state_slot(p.slots, piece.b, p.n_slots, p.status) : -1;
@@ -174,7 +200,6 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
     float st[MT][NT][4];
     const int m_first = warp * (KD / 4) + lane / 4, n_first = lane % 4 * 2;
     const long long carry_size = static_cast<long long>(KD) * kAttnV;
-    const float* carry = p.carry + ((number * p.heads + head) * p.slices + slice) * carry_size;
     const long long carry_step = static_cast<long long>(p.heads) * p.slices * carry_size;
 #pragma unroll
     for (int a = 0; a < MT; ++a)
@@ -187,8 +212,8 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
             }
     if (!STATE && piece.index > 0) {
         const float far = static_cast<float>(exp(log_l * static_cast<double>(p.seg))), first = p.back ? static_cast<float>(exp(log_l * static_cast<double>(p.seg - 1))) : far;
-        for (int s = 0; s < piece.index; ++s) {
-            const float* from = carry + (s - piece.index) * carry_step;
+        const float* from = p.carry + ((attn_first_slot(p, piece.b) * p.heads + head) * p.slices + slice) * carry_size;
+        for (int s = 0; s < piece.index; ++s, from += carry_step) {
             const float f = s == 0 ? first : far;
 #pragma unroll
             for (int a = 0; a < MT; ++a)

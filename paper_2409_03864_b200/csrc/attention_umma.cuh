@@ -98,11 +98,6 @@ struct AttnUmma {
     static constexpr int kBytes = kLow + (UP - 1) * kAttnTile;
 };
 
-// number of the first piece of a sequence
-__device__ __forceinline__ long long attn_first_piece(const AttnParams& p, long long b) {
-    return p.offsets == nullptr ? b * p.sub_dense : __ldg(p.offsets + b) / p.sub + b;
-}
-
 template <bool STATE, bool BACK, int UP>
 __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     attn_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -135,14 +130,15 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     if (!STATE && head == 0) seq_check(p.offsets, number, p.batch, p.max_len, p.rows, p.status);
     // segments, or for the pass over the states the shorter pieces that it cuts them into
     const long long seg = STATE ? p.sub : p.seg;
-    const SeqPiece piece = seq_piece(p.offsets, p.batch, STATE ? p.sub_dense : p.dense, seg, number);
+    const SeqPiece piece = STATE ? attn_slot_piece(p, number) : seq_piece(p.offsets, p.batch, p.dense, seg, number);
     const SeqRange r = seq_range(p.offsets, piece.b, p.max_len, p.rows, p.status);
     const long long start = piece.index * seg;
     const long long slot = !STATE && (p.state_in != nullptr || p.state_out != nullptr) ? state_slot(p.slots, piece.b, p.n_slots, p.status) : -1;
     const long long state_at = slot * p.state_stride + static_cast<long long>(head) * p.d1 * p.d2;
     const bool ends = start + seg >= r.len;
     if (start >= r.len && !(piece.index == 0 && !STATE)) return;
-    if (STATE && !p.all_pieces && start / p.seg == (r.len - 1) / p.seg) return;   // in the last segment: nobody asks for it
+    // of a sequence that has no slots, or in the last segment: nobody asks for it
+    if (STATE && ((!p.every && r.len <= p.seg) || (!p.all_pieces && start / p.seg == (r.len - 1) / p.seg))) return;
     const int count = static_cast<int>(ends ? r.len - start : seg);
     const int chunks = (count + kAttnRows - 1) / kAttnRows;
     const int less = BACK && piece.index == 0 ? 1 : 0;         // see attn_kernel
@@ -487,7 +483,7 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
         }
         if (!STATE && piece.index > 0 && mine) {
             const int pieces = piece.index * static_cast<int>(p.seg / p.sub);
-            const float* from = p.carry + (attn_first_piece(p, piece.b) * p.heads + head) * carry_size +
+            const float* from = p.carry + (attn_first_slot(p, piece.b) * p.heads + head) * carry_size +
                                 (p.carry_turned ? static_cast<long long>(m) * kAttnRows + side * 64 : static_cast<long long>(side) * 64 * kAttnRows + m);
             const float all = static_cast<float>(exp(log_l * static_cast<double>(p.sub))), first = BACK ? static_cast<float>(exp(log_l * static_cast<double>(p.sub - 1))) : all;
 #pragma unroll 1
@@ -547,7 +543,7 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
 #pragma unroll
                 for (int j = 0; j < 64; ++j) to[j * kAttnRows] = st[j];
             }
-        } else if (UP == 3 && ends && p.state_out != nullptr && slot >= 0 && m < p.d1) {
+        } else if (UP == 3 && r.len <= p.seg && p.state_out != nullptr && slot >= 0 && m < p.d1) {
             const float f = BACK && r.len > 0 ? static_cast<float>(exp(log_l)) : 1.0f;   // see attn_kernel
             float* to = p.state_out + state_at + static_cast<long long>(m) * p.s1 + static_cast<long long>(side) * 64 * p.s2;
             const int there = p.d2 - side * 64;
@@ -573,22 +569,34 @@ __global__ void __launch_bounds__(kAttnUmmaThreads, 1)
     }
 }
 
-// The states behind sequences in several segments, from what their pieces add (made of three pieces of the keys): a block has 32 x 32
-// of one head's state, its rows side by side while it adds, its columns for the states in and out.
+// The states behind sequences that have slots, from what their pieces add (made of three pieces of the keys): a block has 32 x 32 of
+// one head's state, its rows side by side while it adds, its columns for the states in and out.  Where only sequences of more than a segment
+// have slots, number i is the one that begins in the i-th `seg` rows: no two of them can.
 __global__ void __launch_bounds__(256) attn_state_kernel(const __grid_constant__ AttnParams p) {
     __shared__ float tile[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n0 = blockIdx.x % 4 * 32, m0 = blockIdx.x / 4 % 4 * 32;
     const int head = static_cast<int>(blockIdx.x / 16 % p.heads);
-    const long long b = blockIdx.x / 16 / p.heads;
+    long long b = blockIdx.x / 16 / p.heads;
     seq_grid_wait();
     if (m0 >= p.d1 || n0 >= p.d2) return;
+    if (!p.every) {
+        const long long number = b;
+        b = 0;
+        for (long long hi = p.batch - 1; b < hi;) {
+            const long long mid = (b + hi + 1) / 2;
+            if (__ldg(p.offsets + mid) / p.seg <= number) b = mid;
+            else hi = mid - 1;
+        }
+        if (__ldg(p.offsets + b) / p.seg != number) return;
+    }
     const SeqRange r = seq_range(p.offsets, b, p.max_len, p.rows, p.status);
+    if (!p.every && r.len <= p.seg) return;
     const long long slot = state_slot(p.slots, b, p.n_slots, p.status);
     if (slot < 0) return;
     const long long at = slot * p.state_stride + static_cast<long long>(head) * p.d1 * p.d2;
     const double log_l = static_cast<double>(__ldg(p.log_decay + head));
     const long long pieces = (r.len + p.sub - 1) / p.sub, last = r.len - (pieces - 1) * p.sub;
-    const float* carry = p.carry + (attn_first_piece(p, b) * p.heads + head) * kAttnRows * kAttnRows;
+    const float* carry = p.carry + (attn_first_slot(p, b) * p.heads + head) * kAttnRows * kAttnRows;
     for (int i = warp; i < 32; i += 8)
         tile[i][lane] = p.state_in != nullptr && m0 + i < p.d1 && n0 + lane < p.d2 ? __ldg(p.state_in + at + static_cast<long long>(m0 + i) * p.s1 + static_cast<long long>(n0 + lane) * p.s2) : 0.0f;
     __syncthreads();

@@ -351,3 +351,21 @@ def test_rows_of_others_that_are_not_finite_do_not_show(dtype, pad, length, head
         assert bool(torch.isfinite(got[k][at]).all()), k
         assert torch.equal(got[k][at], clean[k][at]), k
     tdx.check(tdx.tdx_check_device_status())
+
+
+@pytest.mark.parametrize("dtype,pad", [("bf16", 0), ("bf16", 1), ("f32", 0)])
+@pytest.mark.parametrize("lengths", [[1] * 9 + [1500] + [0, 1, 2] * 9, [1500, 300, 1, 0, 255, 256, 257, 1200], [0, 0, 700], [1200, 0, 0]], ids=["many", "some", "first", "last"])
+def test_long_sequences_among_short_ones(lengths, dtype, pad):
+    c = Case(dtype, lengths, 2, 24, 40, pad=pad, spare=70)
+    before = tdx.tdx_kernel_launch_count()
+    c.check()
+    assert tdx.tdx_kernel_launch_count() - before > 10           # (some sequences are cut)
+    # the states in place are the same bits
+    out, new = c.rows_of(np.zeros((c.rows, 2, 40))), c.slots_of()
+    again = c.cache.clone()
+    tdx.check(tdx.tdx_decay_attention(c.args(out=out, state_in=c.cache, state_out=new)))
+    tdx.check(tdx.tdx_decay_attention(c.args(out=out, state_in=again, state_out=again)))
+    torch.cuda.synchronize()
+    if dtype == "bf16" and pad == 0:
+        at = torch.from_numpy(c.slots).cuda()
+        assert torch.equal(again[at], new[at])

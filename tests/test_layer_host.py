@@ -119,3 +119,15 @@ def test_attention_sizes_and_empty_calls():
     assert tdx.tdx_decay_attention(attention(batch=0, rows=0)) == 0 and tdx.tdx_decay_attention_step(attention(batch=0)) == 0
     assert tdx.tdx_decay_attention_bwd(attention(heads=0, q_heads=0, k_heads=0, v_heads=0)) == 0
     assert tdx.lib().tdx_decay_attention(None, None) == INVALID and tdx.lib().tdx_decay_attention_step(None, None) == INVALID
+
+
+@pytest.mark.parametrize("dtype", [tdx.TDX_BF16, tdx.TDX_F32])
+def test_attention_workspace_goes_by_what_is_cut_and_not_by_the_batch(dtype):
+    many = dict(heads=32, q_heads=32, k_heads=32, v_heads=32, dim_k=128, dim_v=128, dtype=dtype, max_len=8192, seq_offsets=P, n_slots=1 << 20,
+                **{"ld_" + n: 4096 for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")})
+    for dout in (None, P):
+        status, one = tdx.tdx_decay_attention_workspace_size(attention(**many, batch=1, rows=8192, dout=dout))
+        assert status == 0 and one > 0
+        for short in (255, 4095):                                # sequences of one row beside the long one
+            status, size = tdx.tdx_decay_attention_workspace_size(attention(**many, batch=1 + short, rows=8192 + short, dout=dout))
+            assert status == 0 and size <= 2 * one * (8192 + short) / 8192, (short, one, size)
