@@ -7,8 +7,9 @@
 // The gradients are the same sum with the roles exchanged, dq with (dout, v, k) and S^T, dv and dk from the last row to the first with
 // (k, q, dout) and (v, dout, q) and the gradient of the state, so one kernel serves all four ("q", "k", "v" below are roles).
 //
-// This file: mma.sync, for fp32 (three bf16 pieces of every operand) and bf16 rows of any alignment.  A chunk is a chain of products, each
-// waiting for the one in front, with 8 warps an SM: that latency bounds it, not the bytes.  So sequences are cut into many segments.
+// This file: mma.sync, for fp32 (three bf16 pieces of every operand) and for bf16 rows that the copy engine cannot read.  A chunk is a chain
+// of products, each waiting for the one in front, with 8 warps an SM (4 where fp32 operands of more than 64 take the shared memory): that
+// latency bounds it, not the bytes.  So sequences are cut into many segments.
 #pragma once
 #include "seq_common.cuh"
 
@@ -24,7 +25,7 @@ struct AttnParams {
     long long ld_out;
     int out_f32;                            // out is fp32 for every head (its heads are summed afterwards)
     int wide;                               // rows of out are 32-byte aligned
-    int vec;                                // rows of q, k, v (and out) are 16-byte aligned, dims multiples of 16 bytes
+    int vec;                                // fp32: rows of q, k and v are read 16 bytes at a time
     float scale_in, scale_out;              // on k^T v and on out
     int back;                               // from the last row to the first
     const float* log_decay;
@@ -120,35 +121,26 @@ __device__ __forceinline__ void attn_mma_pieces(float (&d)[4], const uint32_t (&
 template <typename T, int KD>
 struct AttnTiles {
     static constexpr int kPieces = sizeof(T) == 4 ? 3 : 1;
-    static constexpr int kBuffers = sizeof(T) == 4 ? 1 : 2;
     static constexpr int kPitchK = KD * 2 + 16, kPitchV = kAttnV * 2 + 16;      // 16 bytes more than a row: ldmatrix without bank conflicts
     static constexpr int kK = kAttnC * kPitchK, kV = kAttnC * kPitchV, kS = KD * kPitchV;   // one piece
-    static constexpr int kBuffer = kPieces * (2 * kK + kV);
-    static constexpr int kBytes = kBuffers * kBuffer + kPieces * kS;
+    static constexpr int kState = kPieces * (2 * kK + kV), kBytes = kState + kPieces * kS;
 };
 
 // `count` rows of width d of a matrix into the pieces' tiles of WIDTH columns; rows behind the last and columns behind d become zero
 template <typename T, int WIDTH>
 __device__ __forceinline__ void attn_load(uint8_t* tile, const T* base, long long ld, int step, int count, int d, bool vec) {
     constexpr int kPieces = sizeof(T) == 4 ? 3 : 1, kPitch = WIDTH * 2 + 16, kPiece = kAttnC * kPitch;
-    if (vec) {
-        constexpr int E = 16 / sizeof(T), kPerRow = WIDTH / E;
+    if (sizeof(T) == 4 && vec) {
+        constexpr int kPerRow = WIDTH / 4;
 #pragma unroll 4
         for (int i = threadIdx.x; i < kAttnC * kPerRow; i += kAttnThreads) {
-            const int row = i / kPerRow, c = i % kPerRow * E;
-            const bool there = row < count && c < d;
-            const T* from = there ? base + row * step * ld + c : base;
-            if (sizeof(T) == 2) {
-                const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(tile + row * kPitch + c * 2));
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(there ? 16 : 0) : "memory");
-            } else {
-                const float4 v = there ? __ldg(reinterpret_cast<const float4*>(from)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                uint32_t lo[kPieces], hi[kPieces];
-                attn_split(v.x, v.y, lo);
-                attn_split(v.z, v.w, hi);
+            const int row = i / kPerRow, c = i % kPerRow * 4;
+            const float4 v = row < count && c < d ? __ldg(reinterpret_cast<const float4*>(base + row * step * ld + c)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            uint32_t lo[kPieces], hi[kPieces];
+            attn_split(v.x, v.y, lo);
+            attn_split(v.z, v.w, hi);
 #pragma unroll
-                for (int p = 0; p < kPieces; ++p) *reinterpret_cast<uint2*>(tile + p * kPiece + row * kPitch + c * 2) = make_uint2(lo[p], hi[p]);
-            }
+            for (int p = 0; p < kPieces; ++p) *reinterpret_cast<uint2*>(tile + p * kPiece + row * kPitch + c * 2) = make_uint2(lo[p], hi[p]);
         }
     } else {
         for (int i = threadIdx.x; i < kAttnC * WIDTH / 2; i += kAttnThreads) {
@@ -165,7 +157,7 @@ __device__ __forceinline__ void attn_load(uint8_t* tile, const T* base, long lon
 
 // One block: a segment of a sequence, a head, 64 columns of v.  Four warps: for the outputs a warp has 16 rows of the chunk, for the
 // state KD / 4 of its rows, in registers over all chunks; the other blocks of the head's columns do q k^T again (a third of the
-// work at dim 128), which leaves room for two blocks an SM.  STATE: only what the segment adds to the state, for the segments behind it.
+// work at dim 128), which leaves registers for two blocks an SM.  STATE: only what the segment adds to the state, for the segments behind it.
 // UP: bf16 pieces of the decayed keys that go into the state, 3 where the state is an output and keeps 24 bits, else 2.  The weights of a
 // chunk's rows have two pieces (PP; fp32 three): what is rounded once on the way to a bf16 output is the state that its row reads.
 template <typename T, int KD, bool STATE, int UP>
@@ -236,19 +228,17 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
     const int d2 = min(p.d2 - slice * kAttnV, kAttnV);
     const int chunks = (count + kAttnC - 1) / kAttnC;
     auto load = [&](int c) {
-        uint8_t* to = attn_smem + (Tiles::kBuffers == 2 ? c & 1 : 0) * Tiles::kBuffer;
         const int n = min(kAttnC, count - c * kAttnC);
         const long long row = row0 + static_cast<long long>(step) * c * kAttnC;
-        if (!STATE) attn_load<T, KD>(to, q + row * p.ld_q, p.ld_q, step, n, p.d1, p.vec);
-        attn_load<T, KD>(to + NP * Tiles::kK, k + row * p.ld_k, p.ld_k, step, n, p.d1, p.vec);
-        attn_load<T, kAttnV>(to + NP * 2 * Tiles::kK, v + row * p.ld_v, p.ld_v, step, n, d2, p.vec);
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (!STATE) attn_load<T, KD>(attn_smem, q + row * p.ld_q, p.ld_q, step, n, p.d1, p.vec);
+        attn_load<T, KD>(attn_smem + NP * Tiles::kK, k + row * p.ld_k, p.ld_k, step, n, p.d1, p.vec);
+        attn_load<T, kAttnV>(attn_smem + NP * 2 * Tiles::kK, v + row * p.ld_v, p.ld_v, step, n, d2, p.vec);
     };
-    constexpr uint32_t kStateAt = Tiles::kBuffers * Tiles::kBuffer;
+    constexpr uint32_t kStateAt = Tiles::kState;
+    const uint32_t tq = smem, tk = tq + NP * Tiles::kK, tv = tk + NP * Tiles::kK;
     if (chunks > 0) load(0);
     for (int c = 0; c < chunks; ++c) {
         const int n = min(kAttnC, count - c * kAttnC), shift = c == 0 ? less : 0;
-        const uint32_t tq = smem + (Tiles::kBuffers == 2 ? c & 1 : 0) * Tiles::kBuffer, tk = tq + NP * Tiles::kK, tv = tk + NP * Tiles::kK;
         if (!STATE) {
             // the state in front of the chunk for all warps; rounded to bf16 for the product with q (fp32: all 24 bits in three pieces)
 #pragma unroll
@@ -263,12 +253,6 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
                         for (int i = 0; i < NP; ++i)
                             *reinterpret_cast<uint32_t*>(attn_smem + kStateAt + i * Tiles::kS + (m_first + a * 16 + h * 8) * PV + (n_first + b * 8) * 2) = piece_of[i];
                     }
-        }
-        if (Tiles::kBuffers == 2 && c + 1 < chunks) {
-            load(c + 1);
-            asm volatile("cp.async.wait_group 1;" ::: "memory");
-        } else {
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
         }
         __syncthreads();
         if (!STATE) {
@@ -354,36 +338,17 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
             }
             // out
             const long long row = row0 + static_cast<long long>(step) * c * kAttnC;
-            if (sizeof(T) == 2 && !p.out_f32 && p.vec) {
-                // through this warp's own rows of q, which nobody reads any more, as whole 16-byte pieces
-                uint8_t* mine = attn_smem + (tq - smem) + warp * 16 * PK;
-                __syncwarp();
 #pragma unroll
-                for (int b = 0; b < NT; ++b)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        *reinterpret_cast<uint32_t*>(mine + (lane / 4 + h * 8) * PK + (n_first + b * 8) * 2) = attn_pair(o[b][2 * h] * p.scale_out, o[b][2 * h + 1] * p.scale_out);
-                __syncwarp();
+            for (int b = 0; b < NT; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int at = lane / 8 + i * 4, col = lane % 8 * 8;
-                    if (warp * 16 + at < n && col < d2)
-                        *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + (row + step * (warp * 16 + at)) * p.ld_out + static_cast<long long>(head) * p.d2 + slice * kAttnV + col) =
-                            *reinterpret_cast<const uint4*>(mine + at * PK + col * 2);
-                }
-            } else {
-#pragma unroll
-                for (int b = 0; b < NT; ++b)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int at = i0 + (i >> 1) * 8, col = n_first + b * 8 + (i & 1);
-                        if (at < n && col < d2) {
-                            const long long to = (row + step * at) * p.ld_out + static_cast<long long>(head) * p.d2 + slice * kAttnV + col;
-                            if (p.out_f32) static_cast<float*>(p.out)[to] = o[b][i] * p.scale_out;
-                            else static_cast<T*>(p.out)[to] = seq_from_float<T>(o[b][i] * p.scale_out);
-                        }
+                    const int at = i0 + (i >> 1) * 8, col = n_first + b * 8 + (i & 1);
+                    if (at < n && col < d2) {
+                        const long long to = (row + step * at) * p.ld_out + static_cast<long long>(head) * p.d2 + slice * kAttnV + col;
+                        if (p.out_f32) static_cast<float*>(p.out)[to] = o[b][i] * p.scale_out;
+                        else static_cast<T*>(p.out)[to] = seq_from_float<T>(o[b][i] * p.scale_out);
                     }
-            }
+                }
         }
         // the state behind the chunk
         const float all = power[n - shift];
@@ -437,7 +402,7 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const __grid_constan
             }
         }
         __syncthreads();
-        if (Tiles::kBuffers == 1 && c + 1 < chunks) load(c + 1);
+        if (c + 1 < chunks) load(c + 1);
     }
     if (STATE) {
         float* to = p.carry + ((number * p.heads + head) * p.slices + slice) * carry_size;

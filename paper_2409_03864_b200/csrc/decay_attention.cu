@@ -54,15 +54,25 @@ int check_attention(const tdx_attention_args* args, AttnPass pass, AttnShape* sh
     return TDX_OK;
 }
 
+int attention_padded(int d1) { return d1 > 64 ? 128 : 64; }
+// Blocks of the kernel on mma.sync that an SM holds: two by their registers, one where fp32 operands take more than half the shared memory
+// (a kilobyte of which goes with every block, next to what is static).
+int attention_blocks(int dtype, int d1) {
+    const bool wide = attention_padded(d1) == 128;
+    const int bytes = dtype == TDX_F32 ? (wide ? tdx::AttnTiles<float, 128>::kBytes : tdx::AttnTiles<float, 64>::kBytes)
+                                       : (wide ? tdx::AttnTiles<__nv_bfloat16, 128>::kBytes : tdx::AttnTiles<__nv_bfloat16, 64>::kBytes);
+    return 2 * (bytes + 2048) <= kSmemLimitDefault + 1024 ? 2 : 1;
+}
+
 // How a sum is spread over the SMs: the rows of a segment.  Heads (and, in the kernel on mma.sync, slices of 64 columns) and sequences
 // run side by side; where they do not fill the SMs evenly, sequences are cut into segments, which costs a look at k and v of all but the
 // last one for what they add to the state (about half a segment's time) and two chunks' time a block for its start.  The number of segments
 // with the least estimated time is taken, of two chunks at least (packed fp32 prompts, 2491 rows, 6 heads of 64 and 80: segments of 128
 // rows 44 us, of 256 rows 72).
-void plan_attention(const tdx_attention_args& a, int d2, bool umma, bool all_pieces, int sm_count, tdx::AttnParams* p) {
+void plan_attention(const tdx_attention_args& a, int d1, int d2, bool umma, bool all_pieces, int sm_count, tdx::AttnParams* p) {
     const int64_t longest = std::max<int64_t>(1, std::min(a.max_len, a.rows));
     const int64_t side = a.seq_offsets ? std::max<int64_t>(1, a.rows / longest) : std::max<int64_t>(1, a.batch);
-    const int64_t chunk = umma ? tdx::kAttnRows : tdx::kAttnC, slots = umma ? sm_count : 2 * sm_count;
+    const int64_t chunk = umma ? tdx::kAttnRows : tdx::kAttnC, slots = umma ? sm_count : attention_blocks(a.dtype, d1) * sm_count;
     p->slices = umma ? 1 : static_cast<int>(ceil_div(d2, tdx::kAttnV));
     const int64_t tiles = std::max<int64_t>(1, static_cast<int64_t>(p->slices) * a.heads) * side;
     double least = 0.0;
@@ -101,7 +111,6 @@ int64_t attention_slots(const tdx_attention_args& a, const tdx::AttnParams& p) {
     return a.seq_offsets ? tdx::attn_slots_before(static_cast<int>(a.rows), a.batch, static_cast<int>(p.sub), static_cast<int>(p.seg), p.every) : a.batch * p.sub_dense;
 }
 bool attention_cut(const tdx_attention_args& a, const tdx::AttnParams& p) { return std::min(a.max_len, a.rows) > p.seg; }
-int attention_padded(int d1) { return d1 > 64 ? 128 : 64; }
 
 struct AttnWorkspace { size_t carry, each, total; };
 AttnWorkspace attention_workspace(const tdx_attention_args& a, const AttnShape& shape, int sm_count, bool back) {
@@ -111,7 +120,7 @@ AttnWorkspace attention_workspace(const tdx_attention_args& a, const AttnShape& 
         const int d1 = sum == kAttnOut || sum == kAttnDv ? a.dim_k : a.dim_v, d2 = sum == kAttnOut || sum == kAttnDv ? a.dim_v : a.dim_k;
         for (int way = 0; way < 3; ++way) {                      // whichever the alignment allows, with and without state_out
             const bool umma = way > 0;
-            plan_attention(a, d2, umma, way == 2, sm_count, &p);
+            plan_attention(a, d1, d2, umma, way == 2, sm_count, &p);
             const size_t each = umma ? tdx::kAttnRows * tdx::kAttnRows : p.slices * attention_padded(d1) * tdx::kAttnV;
             if (attention_cut(a, p)) w.carry = std::max(w.carry, static_cast<size_t>(attention_slots(a, p)) * a.heads * each * sizeof(float));
         }
@@ -218,7 +227,7 @@ int run_attention(const tdx_attention_args& a, const AttnShape& shape, AttnSum s
     p.carry = static_cast<float*>(a.workspace);
     const bool umma = sizeof(T) == 2 && p.vec && a.rows > 0 && a.rows <= INT_MAX;   // (rows are coordinates of the copy engine)
     const bool all_pieces = (sum == kAttnOut ? a.state_out : late ? a.dstate_in : nullptr) != nullptr;
-    plan_attention(a, p.d2, umma, all_pieces, dev.sm_count, &p);
+    plan_attention(a, p.d1, p.d2, umma, all_pieces, dev.sm_count, &p);
     // A segment on the other kernel may end, and write the state, before one in front of it has started from the state that it replaces.
     if (!umma && p.state_out != nullptr && p.state_out == p.state_in) {
         p.seg = ceil_div(std::max<int64_t>(1, a.max_len), tdx::kAttnC) * tdx::kAttnC;
