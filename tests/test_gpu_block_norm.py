@@ -202,3 +202,40 @@ def test_workspace_refusals():
         assert tdx.tdx_block_norm_bwd(a.set(**change)) == status
     torch.cuda.synchronize()
     assert all((v.host() == -5.0).all() for v in out.values())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,group", [(512, 0), (2000, 40), (4096, 128), (9000, 0)])
+def test_dresidual_in_place_of_dsum(d, group, dtype):
+    c = Case(dtype, 700, d, group)                               # (several rows for every set of threads)
+    dsum, dy = (seeded(c.rng, (700, d), dtype) for _ in range(2))
+    dev_dy, results = c.rows_of(dy), []
+    for shared in (False, True):
+        own = c.rows_of(dsum)
+        outs = {"d" + k: c.rows_of(np.zeros((700, d)), fill=float("nan")) for k in ("x", "gate", "residual")}
+        if shared:
+            outs["dresidual"] = own
+        outs.update({"d" + k: torch.full((d,), float("nan"), device="cuda") for k in ("weight_in", "scale", "weight_out")})
+        a = c.args(dsum=own, dy=dev_dy, **outs)
+        ws = workspace(tdx.tdx_block_norm_workspace_size(a))
+        tdx.check(tdx.tdx_block_norm_bwd(a.set(workspace=ws, workspace_bytes=ws.numel())))
+        torch.cuda.synchronize()
+        results.append({k: v.full.clone() if isinstance(v, Rows) else v for k, v in outs.items()})
+    for k, v in results[0].items():
+        assert bool(torch.isfinite(v).all()) and torch.equal(v, results[1][k]), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(700, 4096, 0), (700, 8192, 0), (700, 4096, 128), (700, 2000, 40), (700, 2909, 0), (700, 9000, 0), (650, 9000, 90), (10000, 64, 16)])
+def test_many_rows_for_every_set_of_threads(shape, dtype):
+    c = Case(dtype, *shape)
+    c.forward()
+    c.backward()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("norm_in,gate,residual", [(0, False, False), (0, False, True), (1, True, False), (1, False, True)])
+def test_many_rows_of_the_usual_parts(norm_in, gate, residual, dtype):
+    c = Case(dtype, 700, 4096, 0, norm_in, gate, residual, scale=residual)
+    c.forward(("sum",) if norm_in and not residual else ("y",) if not residual else ("sum", "y"))
+    c.backward(with_sum=bool(norm_in or residual), with_y=not norm_in or residual)

@@ -369,3 +369,34 @@ def test_long_sequences_among_short_ones(lengths, dtype, pad):
     if dtype == "bf16" and pad == 0:
         at = torch.from_numpy(c.slots).cuda()
         assert torch.equal(again[at], new[at])
+
+
+# heads fill the SMs: a block has all chunks of a sequence; few heads: segments, and pieces of them, of several chunks
+@pytest.mark.parametrize("states", [False, True])
+@pytest.mark.parametrize("lengths,heads,dk,dv", [([1100], 150, 16, 16), ([700, 0, 1000], 160, 8, 24), ([4096], 32, 16, 16), ([4500], 30, 24, 8), ([2600, 1900], 40, 16, 16)])
+def test_many_chunks_a_block(lengths, heads, dk, dv, states):
+    Case("bf16", lengths, heads, dk, dv, states=states).check()
+
+
+@pytest.mark.parametrize("lengths,heads", [([700], 150), ([640, 597], 90), ([3000], 8), ([2500, 40], 24)])
+def test_many_chunks_of_wide_heads_against_fp32(lengths, heads):
+    c = Case("bf16", lengths, heads, 128, 128)
+    names = ("q", "k", "v", "dout", "state", "dstate")
+
+    def same_values(f):
+        d = Case("f32", lengths, heads, 128, 128)
+        for n in names:
+            setattr(d, n, f(getattr(c, n)))
+        d.slots = c.slots
+        d.dev = {n: d.rows_of(getattr(d, n)) for n in ("q", "k", "v", "dout")}
+        d.cache, d.dcache = d.slots_of(d.state), d.slots_of(d.dstate)
+        return run_all(d)
+
+    got, want, size = run_all(c), same_values(np.asarray), same_values(np.abs)
+    exact, rounded = c.factors()
+    at = torch.from_numpy(c.slots).cuda()
+    for k in got:
+        g, w, s = (v[k][at] if k.endswith("state") else v[k] for v in (got, want, size))
+        # both are off, the fp32 kernel by `exact`
+        factor, dtype = (2 * exact, "f32") if k.endswith("state") else (exact + rounded, "bf16")
+        assert_close(k, *(v.double().cpu().numpy() for v in (g, w, s)), factor, dtype)

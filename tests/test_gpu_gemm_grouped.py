@@ -174,3 +174,10 @@ def test_captured_and_replayed_with_other_offsets():
 ], ids=["rounds", "unsorted", "thousand"])
 def test_many_tiles_and_experts(shape, dtype):
     Case(dtype, *shape).check()
+
+
+# more than 512 rows an expert: tiles of 256 features for dw too; the last with more tiles than SMs
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [([600, 700, 513], 264, 264), ([900, 0, 1100], 264, 72), ([1300], 136, 520), ([601, 640, 560, 700], 2304, 1096)])
+def test_many_rows_an_expert(shape, dtype):
+    Case(dtype, *shape).check()
