@@ -408,7 +408,8 @@ int tdx_w4_quantize(int64_t N, int64_t K, int group_size, int dtype, const void*
  * norm and gate behind an attention is norm_in = 1 with group = a head's channels and only `sum`; the norm in front of a block is
  * norm_in = 0 with only `y`; the stream's sum behind a block with the next block's norm has all of it.
  * Backward: all gradients from x, gate, residual, dsum and dy (either may be NULL: zeros; dy stands for y); s is computed again.
- * dresidual may be dsum.  channels up to 2^20; rows of up to 8192 channels are read once, wider ones several times.
+ * dresidual may be dsum.  channels up to 2^20; rows of up to 8192 channels are read once, wider ones several times, and have at most
+ * 4096 groups.
  */
 typedef struct {
     int64_t rows, channels;
@@ -483,6 +484,7 @@ int tdx_gemm_grouped_workspace_size(const tdx_grouped_args* args, size_t* bytes)
  * chunk in front of it, up to 127, and their gradients.
  * bf16: products of bf16 values with fp32 sums; the states that a row reads are rounded to bf16 in front of their product, attention weights
  * and the keys that go into a state keep 16 bits, and the states that are handed on (state_out, dstate_in) and all sums 24.
+ * fp32, and bf16 rows that are not multiples of 16 bytes apart: long prompts of few heads are faster with state_out apart from state_in.
  * Backward: dq, dk, dv (summed over the heads that share one) and dstate_in from q, k, v, state_in, dout and dstate_out.
  */
 typedef struct {

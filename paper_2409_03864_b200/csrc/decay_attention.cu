@@ -228,7 +228,8 @@ int run_attention(const tdx_attention_args& a, const AttnShape& shape, AttnSum s
     const bool umma = sizeof(T) == 2 && p.vec && a.rows > 0 && a.rows <= INT_MAX;   // (rows are coordinates of the copy engine)
     const bool all_pieces = (sum == kAttnOut ? a.state_out : late ? a.dstate_in : nullptr) != nullptr;
     plan_attention(a, p.d1, p.d2, umma, all_pieces, dev.sm_count, &p);
-    // A segment on the other kernel may end, and write the state, before one in front of it has started from the state that it replaces.
+    // A segment on the other kernel may end, and write the state, before one in front of it has started from the state that it replaces: so
+    // sequences are not cut, which costs what the cuts gain (fp32, 4096 rows, 8 heads of 128: 944 us in place, 183 apart).
     if (!umma && p.state_out != nullptr && p.state_out == p.state_in) {
         p.seg = ceil_div(std::max<int64_t>(1, a.max_len), tdx::kAttnC) * tdx::kAttnC;
         p.dense = 1;

@@ -74,13 +74,14 @@ int launch_grouped_umma(tdx::GroupedParams p, const tdx_host::Device& dev, cudaS
     const int depth = PASS == tdx::kGroupedForward ? p.K : p.N;
     const int64_t rows_each = ceil_div(p.rows, p.experts);
     if (PASS == tdx::kGroupedDw) {
-        // Few rows are a short reduction, and the time is that of writing dw: tiles of 128 x 256, whose accumulators fit twice (40 rows
-        // an expert, 32 x 2048 x 2048: 78 us instead of 98; 512 rows, 16 x 4096 x 2048: 151 instead of 154; 2048 rows: 438 instead of 407).
+        // Few rows are a short reduction, and the time is that of writing dw: tiles of 128 x 256, whose accumulators fit twice (40 rows an
+        // expert, 32 x 2048 x 2048: 56 to 70 us instead of 70 to 87).  From about 500 rows on both take about the same: 512 rows, 16 x 4096 x
+        // 2048: 134 instead of 130; 600, 8 x 2304 x 2048: 64 instead of 61; 1024: 81 instead of 76; 2048, 8 x 4096 x 4096: 434 instead of 431 to 448.
         p.bt = p.K > 128 ? 256 : 128;
         p.halves = p.N > 128 && rows_each > 512 ? 2 : 1;
     } else {
-        // as wide as an expert's rows: 8 x 2048 rows, 4096 x 4096: 256 x 256 379 us, 128 x 256 405, 256 x 128 464, 128 x 128 610; 16 x 100
-        // rows all within a few per cent, up to 16 rows 128 x 32
+        // as wide as an expert's rows: 8 x 2048 rows, 4096 x 4096: 256 features x 256 rows 377 us, 128 x 256 444 to 470, 256 x 128 547 to 560, 128 x
+        // 128 656 to 673; 16 x 100 rows, 4096 x 2048: 256 x 128 52, 128 x 128 and 256 x 256 55, 128 x 256 59; up to 16 rows 128 x 32
         p.bt = rows_each <= 16 ? 32 : rows_each <= 48 ? 64 : rows_each <= 128 ? 128 : 256;
         p.halves = p.bt >= 128 && p.features > 128 ? 2 : 1;
     }

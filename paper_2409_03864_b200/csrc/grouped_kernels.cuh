@@ -224,10 +224,13 @@ __global__ void __launch_bounds__(kSimtThreads, 2) grouped_simt_kernel(const __g
 // Persistent, one block an SM: warp 0 copies 128-byte-swizzled tiles of 64 of the reduction into a ring of stages (TMA), warp 1 issues the
 // tcgen05 products, eight warps turn accumulators into bf16.  The features are the product's M (128 or two times 128) and the rows of an
 // expert its N: an expert's last tile then costs what its rows need, in steps of 16, instead of a whole tile of 128, and a few rows cost
-// 32 columns of a product that streams the weights.  Accumulators are held twice, so a tile's epilogue runs under the next tile's products.
-// Measured: 8 x 2048 rows, 4096 x 4096: 382 us (1440 of the 1664 TFLOP/s of a library's product), bound by the products; 8192 rows unevenly
-// over 16 experts, 4096 x 2048: 137 (1002), bound by the last round of tiles; 128 rows over 32 experts, 2048 x 2048: 42 us, which is the
-// weights' 269 MB at the copy rate.
+// 32 columns of a product that streams the weights.  Tiles of up to 256 of tensor memory's 512 columns hold their accumulators twice, so that
+// an epilogue runs under the next tile's products.  Tiles of 256 x 256 take all columns: their products wait for the epilogue in front,
+// about 5 us a tile beside 12 for every 1024 of the reduction (16 x 512 rows, 4096 features, four rounds of tiles: 72, 120, 220, 424 us at 1024,
+// 2048, 4096, 8192), and are still the fastest for many rows (grouped_gemm.cu).
+// Measured: 8 x 2048 rows, 4096 x 4096: 377 us (1458 of the 1664 TFLOP/s of a library's product); 8192 rows unevenly over 16 experts, 4096 x
+// 2048: 144 to 157 (875 to 955), bound by the epilogues between products and then by the last round of tiles; 128 rows over 32 experts, 2048 x
+// 2048: 42 us, which is the weights' 269 MB at the copy rate.
 // dw sums over an expert's rows: both operands are read with the rows as the reduction, and rows of the last block that belong to the
 // next expert are set to zero in shared memory in front of the product (a factor of zero in one operand would leave NaN and infinity).
 constexpr int kGroupedMostExperts = 1024;                        // whose tile counts are kept in shared memory

@@ -331,6 +331,8 @@ __global__ void __launch_bounds__(kNormThreads, NV * VEC <= 8 ? 2 : 1) norm_fwd_
 // Sixteen warps an SM is all that 128 registers leave (8 channels a thread with three sums each and the next row on its way), so
 // latency bounds it, at half the issue rate and a third of the memory's.  Everything at once (norm in and out, gate, scale, residual),
 // 8192 x 4096 in bf16, forward and backward: 252 us for 873 MB; without the next row's loads 336.
+// Wider threads (bf16 rows of more than 4096 channels, fp32 ones of more than 2048) and combinations that no instance knows spill: the
+// same bytes take 185 us backwards at 4096 channels, 465 there without dsum, 734, 657 and 641 at 5120, 6144 and 8192; fp32, 4096 x 4096: 474.
 template <typename T, int VEC, int NV, int HAS>
 __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_constant__ NormParams p) {
     typedef typename NormLanes<VEC>::type Lane;
