@@ -400,3 +400,47 @@ def test_many_chunks_of_wide_heads_against_fp32(lengths, heads):
         # both are off, the fp32 kernel by `exact`
         factor, dtype = (2 * exact, "f32") if k.endswith("state") else (exact + rounded, "bf16")
         assert_close(k, *(v.double().cpu().numpy() for v in (g, w, s)), factor, dtype)
+
+
+@pytest.mark.parametrize("dtype,pad", [("bf16", 0), ("bf16", 1), ("f32", 0)])
+@pytest.mark.parametrize("batch", [3, 12])                       # slots for every sequence; for those of several segments
+def test_bad_offsets_of_cut_sequences_are_reported(batch, dtype, pad):
+    for offsets in ([0, 900, 400, 1500], [0, 1300, 1501, 1600], [-900, 0, 800, 1500]):
+        c = Case(dtype, [700, 300, 500] + [0] * (batch - 3), 2, 16, 16, pad=pad)
+        out, new = c.rows_of(np.zeros((1500, 2, 16)), fill=-5.0), c.slots_of()
+        g = {"d" + n: c.rows_of(np.zeros(v.shape), fill=-5.0) for n, v in (("q", c.q), ("k", c.k), ("v", c.v))}
+        bad = i32(offsets + offsets[-1:] * (batch - 3))
+        grad = c.slots_of()
+        a = c.args(out=out, state_in=c.cache, state_out=new, **g, dstate_out=c.dcache, dstate_in=grad)
+        a.set(seq_offsets=bad, max_len=1400)
+        ws = workspace(tdx.tdx_decay_attention_workspace_size(a))
+        a.set(workspace=ws, workspace_bytes=ws.numel())
+        for call in (tdx.tdx_decay_attention, tdx.tdx_decay_attention_bwd):
+            tdx.check(call(a))
+            assert tdx.tdx_check_device_status() == tdx.TDX_ERR_BOUNDS
+        assert out.guards_intact() and all(v.guards_intact() for v in g.values())
+        others = np.setdiff1d(np.arange(c.n_slots), c.slots)
+        assert bool((new[torch.from_numpy(others).cuda()] == CANARY).all())
+
+
+def test_captured_once_and_replayed_with_other_lengths():
+    lengths = [900, 5, 300] + [1] * 12
+    c = Case("bf16", lengths, 2, 32, 16)
+    out, new = c.rows_of(np.zeros((c.rows, 2, 16))), c.slots_of()
+    a = c.args(out=out, state_in=c.cache, state_out=new)
+    offsets = c.keep[1]
+    tdx.check(tdx.tdx_decay_attention(a))
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=stream):
+        tdx.check(tdx.tdx_decay_attention(a, torch.cuda.current_stream()))
+    for lengths in ([1] * 12 + [300, 5, 900], [80] * 14 + [97], [0] * 7 + [900, 0, 317] + [0] * 5):
+        c.lengths = lengths
+        offsets.copy_(torch.from_numpy(offsets_of(lengths)))
+        out.view.fill_(-5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, size = c.exact(grads=False), c.exact(True, False)
+        exact, rounded = c.factors()
+        assert_close("out", out.host(), want["out"], size["out"], rounded, "bf16")
+        assert_close("state", new.double().cpu().numpy()[c.slots], want["state"], size["state"], exact)
+    tdx.check(tdx.tdx_check_device_status())
